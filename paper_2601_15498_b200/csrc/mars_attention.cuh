@@ -1,0 +1,237 @@
+// Pieces shared by the tree-attention kernels: call parameters, the split of a ragged batch's work
+// over the thread blocks, the draft tree's ancestor masks, partial results and their merge.
+//
+// Work is cut along the keys, evenly over the grid.  An item is (sequence, KV head, tile of query
+// rows); its keys come in units of `kUnit`; the units of all items, laid end to end, are dealt to the
+// blocks in equal contiguous ranges.  Lengths live on the device, so every block works the split out
+// by itself (one pass over seq_len).  A block's range begins and ends anywhere, so the first and the
+// last item of it may be shared with neighbours: such a block leaves a partial result (unnormalised
+// output, maximum, sum) in the workspace, and the last one to arrive merges them in block order.
+// Results therefore depend on the sizes alone.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "mars_kv.cuh"
+#include "mars_stream.cuh"
+
+namespace mars {
+
+constexpr int kUnit = 64;            // keys per unit of the split
+
+struct AttnParams {
+    KvView kv;
+    unsigned char *layer;            // this layer's pages
+    const float *scales;             // this layer's [2][kv_heads]
+    const unsigned char *q;
+    unsigned char *out;
+    int64_t q_row, q_head, out_row, out_head;   // elements
+    const int32_t *parent;           // or null: chains
+    const int32_t *count;            // or null
+    int32_t *status;                 // or null
+    int shared_parent;
+    int B, N, group;
+    float scale_log2;                // softmax scale * log2(e)
+    unsigned *counters;              // [grid]
+    float *partial;                  // [2 * grid] slots of rows * (d + 2) floats
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Nodes of sequence b that take part, and whether its pages hold them; len < 0 counts as no room.
+__device__ __forceinline__ int attn_nodes(const AttnParams &p, int b, int *len, int *status)
+{
+    const int n = p.count ? min(max(p.count[b], 0), p.N) : p.N;
+    *len = p.kv.seq_len[b];
+    *status = MARS_SEQ_OK;
+    if (n == 0) return 0;
+    if (*len < 0 || (int64_t)*len + n > kv_capacity(p.kv, b)) { *status = MARS_SEQ_NO_ROOM; return 0; }
+    return n;
+}
+
+// Keys that the rows of tile mt (rows mt*M .. of n*group) may see: all nodes of a tree, the nodes up
+// to the tile's last one of a chain.
+template <int M>
+__device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, int mt)
+{
+    if (p.parent) return len + n;
+    return len + min(n, ((mt + 1) * M - 1) / p.group + 1);
+}
+
+__device__ __forceinline__ int attn_units(int keys) { return (keys + kUnit - 1) / kUnit; }
+
+template <int M>
+__device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + M - 1) / M; }
+
+// Units of one KV head of a sequence.
+template <int M>
+__device__ __forceinline__ int64_t attn_head_units(const AttnParams &p, int len, int n)
+{
+    const int tiles = attn_tiles<M>(p, n);
+    if (p.parent || tiles <= 1) return (int64_t)tiles * (n ? attn_units(attn_keys<M>(p, len, n, 0)) : 0);
+    int64_t u = 0;
+    for (int mt = 0; mt < tiles; ++mt) u += attn_units(attn_keys<M>(p, len, n, mt));
+    return u;
+}
+
+struct AttnRange {
+    int64_t begin, end;     // this block's units
+    int64_t per;            // units per block
+    int64_t at;             // first unit of sequence b
+    int b;                  // sequence of unit `begin`
+};
+
+// The block's share of the batch (all threads call; kThreads = blockDim.x).  Block 0 also reports the
+// status of sequences that have no work.
+template <int M, int kThreads>
+__device__ AttnRange attn_split(const AttnParams &p)
+{
+    __shared__ int64_t s_sum[kThreads / 32 + 1];
+    __shared__ int64_t s_at;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int chunk = (p.B + kThreads - 1) / kThreads;
+    const int lo = min(tid * chunk, p.B), hi = min(lo + chunk, p.B);
+    int64_t sum = 0;
+    for (int b = lo; b < hi; ++b) {
+        int len, st;
+        const int n = attn_nodes(p, b, &len, &st);
+        sum += attn_head_units<M>(p, len, n) * p.kv.kv_heads;
+        if (n == 0 && p.status && blockIdx.x == 0) p.status[b] = st;
+    }
+    int64_t inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+    }
+    if (lane == 31) s_sum[warp] = inc;
+    __syncthreads();
+    int64_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) before += s_sum[w];
+        total += s_sum[w];
+    }
+    AttnRange r;
+    r.per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    r.begin = min(r.per * blockIdx.x, total);
+    r.end = min(r.begin + r.per, total);
+    int64_t at = before + inc - sum;
+    if (r.begin < r.end && at <= r.begin && r.begin < at + sum) {
+        for (int b = lo; b < hi; ++b) {
+            int len, st;
+            const int n = attn_nodes(p, b, &len, &st);
+            const int64_t u = attn_head_units<M>(p, len, n) * p.kv.kv_heads;
+            if (r.begin < at + u) { s_b = b; s_at = at; break; }
+            at += u;
+        }
+    }
+    __syncthreads();
+    r.b = s_b;
+    r.at = s_at;
+    return r;
+}
+
+// One stretch of an item that a block works on.
+struct AttnSegment {
+    int b, head, tile;
+    int len, n, keys;        // committed tokens, nodes, keys of the tile
+    int unit0, unit1;        // this block's units of the item, of `units`
+    int units;
+    int64_t item;            // first unit of the item in the whole batch
+};
+
+// Decodes the segment that begins at unit u (block-uniform); moves r.b / r.at on as sequences end.
+template <int M>
+__device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRange &r, int64_t u)
+{
+    AttnSegment s;
+    int st;
+    int64_t hu;
+    for (;;) {
+        s.n = attn_nodes(p, r.b, &s.len, &st);
+        hu = attn_head_units<M>(p, s.len, s.n);
+        if (u < r.at + hu * p.kv.kv_heads) break;
+        r.at += hu * p.kv.kv_heads;
+        ++r.b;
+    }
+    s.b = r.b;
+    const int64_t in_seq = u - r.at;
+    s.head = (int)(in_seq / hu);
+    int64_t rest = in_seq - s.head * hu;
+    s.item = r.at + s.head * hu;
+    s.tile = 0;
+    s.keys = attn_keys<M>(p, s.len, s.n, 0);
+    s.units = attn_units(s.keys);
+    if (p.parent) {
+        s.tile = (int)(rest / s.units);
+        rest -= (int64_t)s.tile * s.units;
+        s.item += (int64_t)s.tile * s.units;
+    } else {
+        while (rest >= s.units) {
+            rest -= s.units;
+            s.item += s.units;
+            ++s.tile;
+            s.keys = attn_keys<M>(p, s.len, s.n, s.tile);
+            s.units = attn_units(s.keys);
+        }
+    }
+    s.unit0 = (int)rest;
+    s.unit1 = (int)min((int64_t)s.units, rest + (r.end - u));
+    return s;
+}
+
+// Ancestor-or-self masks of the nodes that a tile's rows belong to, and which of them are computed.
+//   mask   [nodes of the tile][words]  bit m of node i: m is i or an ancestor of i (trees only)
+//   live   [nodes of the tile]         1: node takes part; absent nodes (no way to the root) do not
+// Every thread of the block calls; par is scratch for N ints.  Returns MARS_SEQ_BAD_TREE if the
+// parents are no tree (then only the root is live).
+__device__ __forceinline__ int attn_tree_masks(const AttnParams &p, int b, int n, int first, int nodes, int *par,
+                                               uint32_t *mask, int words, unsigned char *live)
+{
+    const int tid = threadIdx.x, nthr = blockDim.x;
+    int bad = 0;
+    if (p.parent) {
+        const int32_t *g = p.shared_parent ? p.parent : p.parent + (int64_t)b * p.N;
+        for (int i = tid; i < n; i += nthr) {
+            const int x = g[i];
+            if (i == 0 ? x != -1 : (x >= i || x < -1)) bad = 1;
+            par[i] = x;
+        }
+    }
+    bad = __syncthreads_or(bad);
+    for (int i = tid; i < nodes; i += nthr) {
+        const int node = first + i;
+        bool ok = node < n;
+        if (p.parent) {
+            uint32_t *m = mask + i * words;
+            for (int w = 0; w < words; ++w) m[w] = 0u;
+            if (bad) {
+                ok = node == 0;
+                if (ok) m[0] = 1u;
+            } else if (ok) {
+                int x = node;
+                for (;;) {                      // parents fall strictly: at most n steps
+                    m[x >> 5] |= 1u << (x & 31);
+                    if (x <= 0) break;
+                    const int up = par[x];
+                    if (up < 0) { ok = false; break; }
+                    x = up;
+                }
+            }
+        }
+        live[i] = ok;
+    }
+    __syncthreads();
+    return bad ? MARS_SEQ_BAD_TREE : MARS_SEQ_OK;
+}
+
+}  // namespace mars

@@ -1,0 +1,820 @@
+// libmars: the calls that write, move and hand out the pages of the 4-bit KV cache.
+//
+// All of them move bytes; none computes enough to matter.  append and gather are one pass over
+// their rows with a thread per 16 values (one scale); commit and fork move packed rows with 16-byte
+// loads; resize and fork's bookkeeping run in one thread block cluster / block, since the page
+// tables are a few hundred kilobytes at most and a grid-wide step would cost more than it moves.
+#include "mars_kv.cuh"
+#include "mars_stream.cuh"
+#include "mars_hooks.cuh"
+
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "mars_kv.h"
+
+namespace mars {
+
+__host__ __device__ constexpr int elem_bytes(int dt) { return dt == MARS_FP32 ? 4 : 2; }
+
+inline bool kv_dtype_ok(int dt) { return dt == MARS_BF16 || dt == MARS_FP32 || dt == MARS_FP16; }
+
+// --------------------------------------------------------------------------------- append
+
+struct AppendParams {
+    KvView kv;
+    unsigned char *layer;
+    const float *scales;       // this layer's [2][kv_heads]
+    const unsigned char *src[2];
+    int64_t row[2], head[2];   // elements
+    const int32_t *count;
+    int32_t *status;
+    int N;
+};
+
+// 16 values of `DT` at p (16-byte aligned), widened exactly.
+template <int DT>
+__device__ __forceinline__ void load16(const unsigned char *p, float (&x)[16])
+{
+    const uint4 *q = reinterpret_cast<const uint4 *>(p);
+    if constexpr (DT == MARS_FP32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 u = ld_stream(q + i);
+            x[4 * i] = __uint_as_float(u.x); x[4 * i + 1] = __uint_as_float(u.y);
+            x[4 * i + 2] = __uint_as_float(u.z); x[4 * i + 3] = __uint_as_float(u.w);
+        }
+    } else {
+        const uint4 u[2] = {ld_stream(q), ld_stream(q + 1)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == MARS_BF16) {
+                    x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+                    x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                } else {
+                    const float2 f = f16x2_to_float2(w[j]);
+                    x[8 * i + 2 * j] = f.x;
+                    x[8 * i + 2 * j + 1] = f.y;
+                }
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t e4m3_from(float x)   // nearest even, saturating; x >= 0, not NaN
+{
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(x));
+    return r & 0xffu;
+}
+
+// Eight values -> eight E2M1 codes, element 0 in the lowest nibble; nearest even, saturating.
+__device__ __forceinline__ uint32_t e2m1x8_from(const float *t)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(r)
+        : "f"(t[0]), "f"(t[1]), "f"(t[2]), "f"(t[3]), "f"(t[4]), "f"(t[5]), "f"(t[6]), "f"(t[7]));
+    return r;
+}
+
+// One thread per 16 values: grid.y = sequence, x over (row, head, K or V, group of 16).
+// The quotient x / (s*g) is an IEEE division on purpose: with 8-bit significands and a power of two
+// as g many quotients lie exactly on the border of two codes, where a reciprocal's last bit decides.
+template <int D, int DT>
+__global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int kG = D / 16;   // groups of a row
+    const int b = blockIdx.y;
+    const int n = p.count ? min(max(p.count[b], 0), p.N) : p.N;
+    const int len = p.kv.seq_len[b];
+    const bool room = n == 0 || (len >= 0 && (int64_t)len + n <= kv_capacity(p.kv, b));
+    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (idx == 0 && p.status) p.status[b] = room ? MARS_SEQ_OK : MARS_SEQ_NO_ROOM;
+    if (!room) return;
+    const int per_row = p.kv.kv_heads * 2 * kG;
+    const int64_t row = idx / per_row;
+    if (row >= n) return;
+    const int in_row = (int)(idx - row * per_row);
+    const int h = in_row / (2 * kG), kv = (in_row / kG) & 1, grp = in_row % kG;
+    const int pos = len + (int)row;
+    const int id = kv_page_id(p.kv, b, pos);
+    if (id < 0) return;
+
+    float x[16];
+    load16<DT>(p.src[kv] + (((int64_t)b * p.N + row) * p.row[kv] + h * p.head[kv] + grp * 16) * elem_bytes(DT), x);
+    float a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        x[i] = x[i] == x[i] ? x[i] : 0.0f;
+        a = fmaxf(a, fabsf(x[i]));
+    }
+    const float g = p.scales[kv * p.kv.kv_heads + h];
+    const uint32_t s8 = e4m3_from(__fdiv_rn(__fdiv_rn(a, 6.0f), g));
+    const float sg = __fmul_rn(f16x2_to_float2(e4m3x2_to_f16x2(s8)).x, g);
+    uint2 codes = make_uint2(0u, 0u);
+    if (sg > 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], sg);
+        codes.x = e2m1x8_from(x);
+        codes.y = e2m1x8_from(x + 8);
+    }
+    unsigned char *blk = kv_block<D>(p.kv, p.layer, id, h, pos);
+    const int slot = pos & 15;
+    *reinterpret_cast<uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8) = codes;
+    blk[16 * D + D * kv + slot * kG + grp] = (unsigned char)s8;
+}
+
+// --------------------------------------------------------------------------------- gather
+
+struct GatherParams {
+    KvView kv;
+    int layer0;
+    const int32_t *start, *count;
+    unsigned char *dst[2];
+    int B, rows;
+};
+
+// One thread per 16 values: grid.y = sequence, grid.z = layer.
+template <int D, int DT>
+__global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int kG = D / 16;
+    const int b = blockIdx.y, lay = blockIdx.z;
+    const int n = p.count ? min(max(p.count[b], 0), p.rows) : p.rows;
+    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int per_row = p.kv.kv_heads * 2 * kG;
+    const int64_t row = idx / per_row;
+    if (row >= n) return;
+    const int in_row = (int)(idx - row * per_row);
+    const int kv = in_row / (p.kv.kv_heads * kG), h = (in_row / kG) % p.kv.kv_heads, grp = in_row % kG;
+    const int64_t pos64 = (int64_t)(p.start ? p.start[b] : 0) + row;
+    if (pos64 < 0 || pos64 >= kv_capacity(p.kv, b)) return;
+    const int pos = (int)pos64;
+    const int id = kv_page_id(p.kv, b, pos);
+    if (id < 0) return;
+    unsigned char *layer = p.kv.pages + (int64_t)(p.layer0 + lay) * p.kv.layer_bytes;
+    const unsigned char *blk = kv_block<D>(p.kv, layer, id, h, pos);
+    const int slot = pos & 15;
+    const uint2 codes = *reinterpret_cast<const uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8);
+    const float s = f16x2_to_float2(e4m3x2_to_f16x2(blk[16 * D + D * kv + slot * kG + grp])).x;
+    // code * scale has at most 6 significant bits, so the product with g is the only rounding
+    const float g = p.kv.scales[((int64_t)(p.layer0 + lay) * 2 + kv) * p.kv.kv_heads + h];
+    float x[16];
+    uint32_t hh[4];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        e2m1x8_to_f16x2(w ? codes.y : codes.x, hh);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = f16x2_to_float2(hh[j]);
+            x[8 * w + 2 * j] = f.x * s * g;
+            x[8 * w + 2 * j + 1] = f.y * s * g;
+        }
+    }
+    const int64_t at = ((((int64_t)lay * p.B + b) * p.rows + row) * p.kv.kv_heads + h) * D + grp * 16;
+    uint4 *o = reinterpret_cast<uint4 *>((kv ? p.dst[1] : p.dst[0]) + at * elem_bytes(DT));
+    if constexpr (DT == MARS_FP32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
+                              __float_as_uint(x[4 * i + 3]));
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = DT == MARS_BF16 ? bf16x2_from(x[2 * i], x[2 * i + 1]) : f16x2_from(x[2 * i], x[2 * i + 1]);
+        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// --------------------------------------------------------------------------------- commit
+
+struct CommitParams {
+    KvView kv;
+    const int32_t *path;       // or null
+    const int32_t *accept_len;
+    int32_t *new_len;
+    int32_t *status;
+    int path_width, B, layers;
+};
+
+// Whether sequence b's path is sound (warp-uniform), and its accepted drafts a (-1: none).
+__device__ bool commit_path_ok(const CommitParams &p, int b, int lane, int *a_out)
+{
+    const int a = p.accept_len[b], len = p.kv.seq_len[b];
+    *a_out = a;
+    if (a == -1) return true;
+    const int64_t cap = kv_capacity(p.kv, b);
+    bool ok = a >= 0 && len >= 0 && (p.path ? a < p.path_width : (int64_t)len + a < cap);
+    if (ok && p.path) {
+        const int32_t *path = p.path + (int64_t)b * p.path_width;
+        for (int j = lane; j <= a; j += 32) {
+            const int x = path[j], prev = j ? path[j - 1] : -1;
+            if (x <= prev || (j == 0 && x != 0) || (int64_t)len + x >= cap) ok = false;
+        }
+    }
+    return __all_sync(0xffffffffu, ok) != 0;
+}
+
+// A warp per (sequence, layer, head).  Node numbers rise along the path, so path[j] >= j and row j's
+// source is never a row that an earlier step wrote: a batch of rows is read into registers before any
+// of it is written, and later batches read behind everything written so far.
+template <int D>
+__global__ void __launch_bounds__(128) kv_commit_kernel(const CommitParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const int64_t per_seq = (int64_t)p.layers * p.kv.kv_heads;
+    const int b = (int)(w / per_seq);
+    if (b >= p.B) return;
+    const int rest = (int)(w - b * per_seq), lay = rest / p.kv.kv_heads, h = rest % p.kv.kv_heads;
+    int a;
+    const bool ok = commit_path_ok(p, b, lane, &a);
+    const int len = p.kv.seq_len[b];
+    if (rest == 0 && lane == 0) {
+        if (p.new_len && p.new_len != p.kv.seq_len) p.new_len[b] = ok ? len + a + 1 : len;
+        if (p.status) p.status[b] = ok ? MARS_SEQ_OK : MARS_SEQ_BAD_PATH;
+    }
+    if (!ok || a < 1 || !p.path) return;
+    const int32_t *path = p.path + (int64_t)b * p.path_width;
+    unsigned char *layer = p.kv.pages + lay * p.kv.layer_bytes;
+    // a row: 2 * D/32 pieces of 16 code bytes and 2 pieces of D/16 scale bytes
+    constexpr int kCode = D / 16, kPieces = kCode + 2, kPer = 4;
+    constexpr int kRows = 32 * kPer / kPieces;   // rows per batch
+    for (int j0 = 1; j0 <= a; j0 += kRows) {
+        uint4 v[kPer];
+        unsigned char *to[kPer];
+        const int rows = min(kRows, a + 1 - j0);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int i = u * 32 + lane, r = i / kPieces, c = i - r * kPieces;
+            to[u] = nullptr;
+            if (r < rows) {
+                const int j = j0 + r, src = len + path[j], dst = len + j;
+                const int ids = kv_page_id(p.kv, b, src), idd = kv_page_id(p.kv, b, dst);
+                if (src != dst && ids >= 0 && idd >= 0) {
+                    const unsigned char *sb = kv_block<D>(p.kv, layer, ids, h, src);
+                    unsigned char *db = kv_block<D>(p.kv, layer, idd, h, dst);
+                    const int ss = src & 15, ds = dst & 15;
+                    if (c < kCode) {
+                        const int half = c / (kCode / 2), in = c % (kCode / 2);
+                        v[u] = *reinterpret_cast<const uint4 *>(sb + 8 * D * half + ss * (D / 2) + in * 16);
+                        to[u] = db + 8 * D * half + ds * (D / 2) + in * 16;
+                    } else {
+                        const int off = 16 * D + D * (c - kCode);
+                        if constexpr (D == 128) {
+                            const uint2 t = *reinterpret_cast<const uint2 *>(sb + off + ss * 8);
+                            v[u].x = t.x; v[u].y = t.y;
+                        } else {
+                            v[u].x = *reinterpret_cast<const uint32_t *>(sb + off + ss * 4);
+                        }
+                        to[u] = db + off + ds * (D / 16);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            if (!to[u]) continue;
+            const int i = u * 32 + lane, c = i % kPieces;
+            if (c < kCode) *reinterpret_cast<uint4 *>(to[u]) = v[u];
+            else if constexpr (D == 128) *reinterpret_cast<uint2 *>(to[u]) = make_uint2(v[u].x, v[u].y);
+            else *reinterpret_cast<uint32_t *>(to[u]) = v[u].x;
+        }
+        __syncwarp();
+    }
+}
+
+// Lengths in place: only after every warp of the kernel above has read the old ones.
+__global__ void __launch_bounds__(256) kv_commit_len_kernel(const CommitParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, b = (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+    if (b >= p.B) return;
+    int a;
+    const bool ok = commit_path_ok(p, b, lane, &a);
+    const int len = p.kv.seq_len[b];
+    __syncwarp();
+    if (lane == 0 && ok) p.new_len[b] = len + a + 1;
+}
+
+// --------------------------------------------------------------------------------- page bookkeeping
+
+constexpr int kPoolThreads = 1024;
+constexpr int kPoolCluster = 8;
+
+// Exclusive prefix sums of need[0..n) in place (one thread block); returns the total.
+__device__ int block_exclusive_scan(int *need, int n, int *s_warp)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (n + kPoolThreads - 1) / kPoolThreads;
+    const int lo = min(tid * per, n), hi = min(lo + per, n);
+    int sum = 0;
+    for (int i = lo; i < hi; ++i) sum += need[i];
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        int w = s_warp[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += t;
+        }
+        s_warp[lane] = w;
+    }
+    __syncthreads();
+    const int total = s_warp[31];
+    int at = inc - sum + (warp ? s_warp[warp - 1] : 0);
+    for (int i = lo; i < hi; ++i) {
+        const int x = need[i];
+        need[i] = at;
+        at += x;
+    }
+    __syncthreads();
+    return total;
+}
+
+// Number of free pages, at least up to `enough` (one thread block; scans the set in order).
+__device__ int count_free(const uint32_t *bits, int words, int enough, int *s_warp)
+{
+    int have = 0;
+    for (int w0 = 0; w0 < words && have < enough; w0 += 4 * kPoolThreads) {
+        int c = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int w = w0 + u * kPoolThreads + threadIdx.x;
+            if (w < words) c += __popc(__ldcg(bits + w));
+        }
+        c = __reduce_add_sync(0xffffffffu, c);
+        if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = c;
+        __syncthreads();
+        int t = s_warp[threadIdx.x & 31];
+        have += __reduce_add_sync(0xffffffffu, t);
+        __syncthreads();
+    }
+    return have;
+}
+
+// The lowest free pages 0, 1, ... of the set go, in order, to `give(rank, page)` for rank < total, and
+// leave the set (one thread block; each word belongs to one thread).
+template <class Give>
+__device__ void take_free(uint32_t *bits, int words, int total, int *s_warp, Give give)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int base = 0;
+    for (int w0 = 0; w0 < words && base < total; w0 += kPoolThreads) {
+        const int w = w0 + tid;
+        uint32_t word = w < words ? __ldcg(bits + w) : 0u;
+        const int c = __popc(word);
+        int inc = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
+        }
+        if (lane == 31) s_warp[warp] = inc;
+        __syncthreads();
+        if (warp == 0) {
+            int x = s_warp[lane];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int t = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += t;
+            }
+            s_warp[lane] = x;
+        }
+        __syncthreads();
+        int rank = base + inc - c + (warp ? s_warp[warp - 1] : 0);
+        base += s_warp[31];
+        uint32_t left = word;
+        while (left && rank < total) {
+            const int bit = __ffs((int)left) - 1;
+            left &= left - 1;
+            give(rank, w * 32 + bit);
+            ++rank;
+        }
+        if (left != word) bits[w] = left;
+        __syncthreads();
+    }
+}
+
+// Request that rank r falls to: the last i with first[i] <= r (first = exclusive prefix sums).
+__device__ __forceinline__ int owner_of(const int *first, int n, int r)
+{
+    int lo = 0, hi = n;          // first[lo] <= r
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+struct PoolParams {
+    int32_t *table, *seq_len, *seq_pages, *refs;
+    uint32_t *bits;
+    const int32_t *extra;        // resize
+    const int32_t *src, *dst;    // fork
+    int32_t *status;
+    int n;                       // sequences (resize) or pairs (fork)
+    int seqs, num_pages, table_width, page_size, page_log2;
+};
+
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Pages that sequence b shall hold; -1: the request does not fit its table row; `leave`: no request.
+__device__ __forceinline__ int resize_want(const PoolParams &p, int b, int held, bool *leave)
+{
+    const int ex = p.extra[b];
+    *leave = ex < -1;
+    if (ex < -1) return held;
+    if (ex == -1) return 0;
+    const int64_t pages = ((int64_t)max(p.seq_len[b], 0) + ex + p.page_size - 1) >> p.page_log2;
+    return pages > p.table_width ? -1 : (int)pages;
+}
+
+// One cluster of eight blocks.  First all of it gives pages back (a warp per sequence; counts and free
+// bits are changed by commutative integer atomics, so the order is immaterial); the cluster barrier
+// makes that visible; then its first block serves the growing requests from the lowest free pages,
+// found by a prefix sum over the bit set.  No order of threads shows in the result.
+__global__ void __cluster_dims__(kPoolCluster, 1, 1) __launch_bounds__(kPoolThreads) kv_resize_kernel(const PoolParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    extern __shared__ int s_first[];   // [n]
+    __shared__ int s_warp[32];
+    const int lane = threadIdx.x & 31;
+    for (int b = blockIdx.x * (kPoolThreads / 32) + (threadIdx.x >> 5); b < p.n; b += kPoolCluster * (kPoolThreads / 32)) {
+        const int held = min(max(p.seq_pages[b], 0), p.table_width);
+        bool leave;
+        const int want = resize_want(p, b, held, &leave);
+        const int ex = p.extra[b];
+        __syncwarp();
+        if (!leave && want >= 0 && want < held) {
+            int32_t *row = p.table + (int64_t)b * p.table_width;
+            for (int c = want + lane; c < held; c += 32) {
+                const int id = row[c];
+                row[c] = -1;
+                if ((unsigned)id < (unsigned)p.num_pages && atomicSub(p.refs + id, 1) == 1)
+                    atomicOr(p.bits + (id >> 5), 1u << (id & 31));
+            }
+            if (lane == 0) p.seq_pages[b] = want;
+        }
+        if (lane == 0 && ex == -1) p.seq_len[b] = 0;
+        if (lane == 0 && p.status && (leave || want <= held))
+            p.status[b] = want < 0 ? MARS_SEQ_NO_ROOM : MARS_SEQ_OK;
+    }
+    __threadfence();
+    cluster_barrier();
+    if (blockIdx.x != 0) return;
+
+    for (int b = threadIdx.x; b < p.n; b += kPoolThreads) {
+        const int held = min(max(__ldcg(p.seq_pages + b), 0), p.table_width);
+        const int ex = p.extra[b];
+        int want = held;
+        if (ex >= 0) {
+            const int64_t pages = ((int64_t)max(__ldcg(p.seq_len + b), 0) + ex + p.page_size - 1) >> p.page_log2;
+            if (pages <= p.table_width) want = (int)pages;
+        }
+        s_first[b] = max(want - held, 0);
+    }
+    __syncthreads();
+    const int total = block_exclusive_scan(s_first, p.n, s_warp);
+    if (total == 0) return;
+    const int words = (p.num_pages + 31) >> 5;
+    const int have = count_free(p.bits, words, total, s_warp);
+    // requests are served in order while they fit: those whose pages end at or before `have`
+    auto need_of = [&](int i) { return (i + 1 < p.n ? s_first[i + 1] : total) - s_first[i]; };
+    int taken = total;
+    if (have < total) {      // the last request that fits ends the list
+        const int i = owner_of(s_first, p.n, have);          // have < total: i is the request that breaks off
+        taken = s_first[i];
+        // rank `have` may be the first of request i, or inside it; in both cases i is not served
+    }
+    take_free(p.bits, words, taken, s_warp, [&](int rank, int page) {
+        if (page >= p.num_pages) return;
+        const int i = owner_of(s_first, p.n, rank);
+        const int held = min(max(__ldcg(p.seq_pages + i), 0), p.table_width);
+        p.table[(int64_t)i * p.table_width + held + (rank - s_first[i])] = page;
+        p.refs[page] = 1;
+    });
+    __syncthreads();
+    for (int b = threadIdx.x; b < p.n; b += kPoolThreads) {
+        const int need = need_of(b);
+        if (need == 0) continue;
+        const bool ok = s_first[b] + need <= taken;
+        if (ok) p.seq_pages[b] = min(max(__ldcg(p.seq_pages + b), 0), p.table_width) + need;
+        if (p.status) p.status[b] = ok ? MARS_SEQ_OK : MARS_SEQ_OUT_OF_PAGES;
+    }
+}
+
+constexpr int kForkEmpty = -1;   // status inside the kernel: a sound pair whose source has no tokens
+
+// One block: validate and claim, find the new last pages, write tables and counts.
+__global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    extern __shared__ int s_first[];   // [n]
+    __shared__ int s_warp[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kWarps = kPoolThreads / 32;
+    // 1. what is wrong with a pair taken by itself (a warp per pair); sources as they stand
+    for (int i = warp; i < p.n; i += kWarps) {
+        const int s = p.src[i], d = p.dst[i];
+        bool ok = (unsigned)s < (unsigned)p.seqs && (unsigned)d < (unsigned)p.seqs && s != d;
+        int len = 0;
+        if (ok) {
+            const int held = p.seq_pages[s];
+            len = p.seq_len[s];
+            const int64_t pages = ((int64_t)len + p.page_size - 1) >> p.page_log2;
+            ok = len >= 0 && pages <= held && pages <= p.table_width && p.seq_pages[d] == 0;
+            if (ok)
+                for (int c = lane; c < (int)pages; c += 32)
+                    if ((unsigned)p.table[(int64_t)s * p.table_width + c] >= (unsigned)p.num_pages) ok = false;
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (lane == 0) p.status[i] = !ok ? MARS_SEQ_BAD_FORK : len == 0 ? kForkEmpty : MARS_SEQ_OK;
+    }
+    __syncthreads();
+    // 2. of several pairs with one destination the first claims it: its page count, 0 so far, takes
+    //    the smallest of the (negative) claim numbers
+    for (int i = threadIdx.x; i < p.n; i += kPoolThreads)
+        if (p.status[i] != MARS_SEQ_BAD_FORK) atomicMin(p.seq_pages + p.dst[i], i - 0x7fffffff);
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.n; i += kPoolThreads) {
+        int need = 0;
+        if (p.status[i] != MARS_SEQ_BAD_FORK) {
+            if (__ldcg(p.seq_pages + p.dst[i]) != i - 0x7fffffff) p.status[i] = MARS_SEQ_BAD_FORK;
+            else if (p.status[i] != kForkEmpty) need = (p.seq_len[p.src[i]] & (p.page_size - 1)) != 0;
+        }
+        s_first[i] = need;
+    }
+    __syncthreads();
+    const int total = block_exclusive_scan(s_first, p.n, s_warp);
+    const int words = (p.num_pages + 31) >> 5;
+    const int have = total ? count_free(p.bits, words, total, s_warp) : 0;
+    auto need_of = [&](int i) { return (i + 1 < p.n ? s_first[i + 1] : total) - s_first[i]; };
+    const int taken = min(have, total);    // needs are 0 or 1: every rank below `have` ends its request
+    take_free(p.bits, words, taken, s_warp, [&](int rank, int page) {
+        if (page >= p.num_pages) return;
+        const int i = owner_of(s_first, p.n, rank);
+        const int len = p.seq_len[p.src[i]];
+        p.table[(int64_t)p.dst[i] * p.table_width + (len >> p.page_log2)] = page;
+        p.refs[page] = 1;
+    });
+    __syncthreads();
+    // 3. shared pages: table entries and counts.  A source that is also a destination holds no pages,
+    //    so its pair is refused or marked empty, and nothing of it is read while it is written here.
+    for (int i = warp; i < p.n; i += kWarps) {
+        const int st = p.status[i];
+        if (st == MARS_SEQ_BAD_FORK) continue;
+        const int s = p.src[i], d = p.dst[i], need = need_of(i);
+        __syncwarp();
+        if (st == kForkEmpty) {
+            if (lane == 0) { p.status[i] = MARS_SEQ_OK; p.seq_len[d] = 0; p.seq_pages[d] = 0; }
+            continue;
+        }
+        if (need && s_first[i] >= taken) {
+            __syncwarp();
+            if (lane == 0) { p.status[i] = MARS_SEQ_OUT_OF_PAGES; p.seq_pages[d] = 0; }
+            continue;
+        }
+        const int len = p.seq_len[s], full = len >> p.page_log2;
+        __syncwarp();
+        for (int c = lane; c < full; c += 32) {
+            const int id = p.table[(int64_t)s * p.table_width + c];
+            p.table[(int64_t)d * p.table_width + c] = id;
+            atomicAdd(p.refs + id, 1);
+        }
+        if (lane == 0) {
+            p.seq_len[d] = len;
+            p.seq_pages[d] = full + need;
+        }
+    }
+}
+
+struct ForkCopyParams {
+    KvView kv;
+    const int32_t *src, *dst, *status;
+    int pairs;
+};
+
+// The ragged last page's rows, a block per (pair, layer), a warp per 16-token block of a head at a
+// time; partly filled blocks are copied row by row so that no byte behind the rows is touched.
+template <int D>
+__global__ void __launch_bounds__(256) kv_fork_copy_kernel(const ForkCopyParams p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int i = blockIdx.x, lay = blockIdx.y;
+    if (p.status[i] != MARS_SEQ_OK) return;
+    const int s = p.src[i], d = p.dst[i], len = p.kv.seq_len[d];
+    const int page = 1 << p.kv.page_log2, tail = len & (page - 1), first = len - tail;
+    if (!tail) return;
+    const int ids = kv_page_id(p.kv, s, first), idd = kv_page_id(p.kv, d, first);
+    if (ids < 0 || idd < 0) return;
+    unsigned char *layer = p.kv.pages + lay * p.kv.layer_bytes;
+    const int blocks = (tail + 15) >> 4;
+    const int lane = threadIdx.x & 31;
+    constexpr int kChunks = kv_block_bytes(D) / 16, kPer = (kChunks + 31) / 32;
+    for (int w = threadIdx.x >> 5; w < blocks * p.kv.kv_heads; w += blockDim.x >> 5) {
+        const int h = w / blocks, blk = w % blocks, rows = min(16, tail - 16 * blk);
+        const unsigned char *from = kv_block<D>(p.kv, layer, ids, h, first + 16 * blk);
+        unsigned char *to = kv_block<D>(p.kv, layer, idd, h, first + 16 * blk);
+        uint4 v[kPer];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u)
+            if (u * 32 + lane < kChunks) v[u] = reinterpret_cast<const uint4 *>(from)[u * 32 + lane];
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int at = (u * 32 + lane) * 16;
+            if (at >= kv_block_bytes(D)) continue;
+            // rows that the 16 bytes belong to: codes D/2 bytes a row, scales D/16
+            const bool code = at < 16 * D;
+            const int in = code ? at % (8 * D) : (at - 16 * D) % D, width = code ? D / 2 : D / 16;
+            const int r0 = in / width, r1 = (in + 15) / width;
+            if (r1 < rows) {
+                *reinterpret_cast<uint4 *>(to + at) = v[u];
+            } else if (r0 < rows) {        // scales: 2 or 4 rows share 16 bytes
+                const uint32_t q[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+                constexpr int kWords = D / 64;   // words of a row's scales
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (r0 + k / kWords < rows) reinterpret_cast<uint32_t *>(to + at)[k] = q[k];
+            }
+        }
+    }
+}
+
+template <class K, class P>
+static mars_status_t kv_launch(K kernel, dim3 grid, int block, size_t smem, cudaStream_t st, const P &p)
+{
+    const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, kernel, grid, dim3(block), smem, st, p);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
+    return MARS_OK;
+}
+
+// Rows and heads of a caller's tensor on 16-byte boundaries.
+static bool kv_rows_aligned(const void *p, int64_t row, int64_t head, int dt)
+{
+    const int es = elem_bytes(dt);
+    return !((uintptr_t)p & 15) && !((row * es) & 15) && !((head * es) & 15);
+}
+
+}  // namespace mars
+
+using namespace mars;
+
+extern "C" {
+
+size_t mars_kv_pool_bytes(int layers, int num_pages, int kv_heads, int head_dim, int page_size)
+{
+    if (layers < 1 || num_pages < 1 || kv_heads < 1 || (head_dim != 64 && head_dim != 128) || kv_page_log2(page_size) < 0 ||
+        num_pages > (1 << 30) || kv_heads > 1024 || layers > 4096)
+        return 0;
+    return (size_t)layers * num_pages * kv_heads * (page_size / kKvBlock) * kv_block_bytes(head_dim);
+}
+
+mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void *k, int64_t k_row, int64_t k_head,
+                             const void *v, int64_t v_row, int64_t v_head, int dt, int B, int N, const int32_t *count,
+                             int32_t *seq_status, void *cuda_stream)
+{
+    const mars_status_t cs = kv_check(cache);
+    if (cs != MARS_OK) return cs;
+    if (!k || !v || B < 1 || N < 1 || B > cache->seqs || layer < 0 || layer >= cache->layers) return MARS_ERR_INVALID_ARG;
+    if (!kv_dtype_ok(dt) || N > (1 << 24)) return MARS_ERR_UNSUPPORTED;
+    if (!kv_rows_aligned(k, k_row, k_head, dt) || !kv_rows_aligned(v, v_row, v_head, dt)) return MARS_ERR_INVALID_ARG;
+    AppendParams p;
+    p.kv = kv_view(cache);
+    p.layer = p.kv.pages + layer * p.kv.layer_bytes;
+    p.scales = cache->scales + (int64_t)layer * 2 * cache->kv_heads;
+    p.src[0] = (const unsigned char *)k; p.src[1] = (const unsigned char *)v;
+    p.row[0] = k_row; p.row[1] = v_row; p.head[0] = k_head; p.head[1] = v_head;
+    p.count = count; p.status = seq_status; p.N = N;
+    const int64_t threads = (int64_t)N * cache->kv_heads * 2 * (cache->head_dim / 16);
+    const int64_t blocks = (threads + 255) / 256;
+    if (blocks > 0x7fffffff) return MARS_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks, B);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (cache->head_dim == 128)
+        return dt == MARS_BF16   ? kv_launch(kv_append_kernel<128, MARS_BF16>, grid, 256, 0, st, p)
+               : dt == MARS_FP32 ? kv_launch(kv_append_kernel<128, MARS_FP32>, grid, 256, 0, st, p)
+                                 : kv_launch(kv_append_kernel<128, MARS_FP16>, grid, 256, 0, st, p);
+    return dt == MARS_BF16   ? kv_launch(kv_append_kernel<64, MARS_BF16>, grid, 256, 0, st, p)
+           : dt == MARS_FP32 ? kv_launch(kv_append_kernel<64, MARS_FP32>, grid, 256, 0, st, p)
+                             : kv_launch(kv_append_kernel<64, MARS_FP16>, grid, 256, 0, st, p);
+}
+
+mars_status_t mars_kv_commit(const mars_kv_cache_t *cache, const int32_t *path_nodes, int path_width,
+                             const int32_t *accept_len, int B, int32_t *new_len, int32_t *seq_status, void *cuda_stream)
+{
+    const mars_status_t cs = kv_check(cache);
+    if (cs != MARS_OK) return cs;
+    if (!accept_len || !new_len || B < 1 || B > cache->seqs || (path_nodes && path_width < 1)) return MARS_ERR_INVALID_ARG;
+    CommitParams p;
+    p.kv = kv_view(cache);
+    p.path = path_nodes; p.path_width = path_width; p.accept_len = accept_len;
+    p.new_len = new_len; p.status = seq_status; p.B = B; p.layers = path_nodes ? cache->layers : 1;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const int64_t warps = (int64_t)B * p.layers * cache->kv_heads, blocks = (warps + 3) / 4;
+    if (blocks > 0x7fffffff) return MARS_ERR_UNSUPPORTED;
+    const mars_status_t r = cache->head_dim == 128
+                                ? kv_launch(kv_commit_kernel<128>, dim3((unsigned)blocks), 128, 0, st, p)
+                                : kv_launch(kv_commit_kernel<64>, dim3((unsigned)blocks), 128, 0, st, p);
+    if (r != MARS_OK || new_len != cache->seq_len) return r;
+    return kv_launch(kv_commit_len_kernel, dim3((B + 7) / 8), 256, 0, st, p);
+}
+
+static PoolParams pool_params(const mars_kv_cache_t *c)
+{
+    PoolParams p = {};
+    p.table = c->block_table; p.seq_len = c->seq_len; p.seq_pages = c->seq_pages; p.refs = c->page_refs;
+    p.bits = c->free_bits; p.seqs = c->seqs; p.num_pages = c->num_pages; p.table_width = c->table_width;
+    p.page_size = c->page_size; p.page_log2 = kv_page_log2(c->page_size);
+    return p;
+}
+
+mars_status_t mars_kv_resize(const mars_kv_cache_t *cache, const int32_t *extra, int32_t *seq_status, void *cuda_stream)
+{
+    const mars_status_t cs = kv_check(cache);
+    if (cs != MARS_OK) return cs;
+    if (!extra) return MARS_ERR_INVALID_ARG;
+    PoolParams p = pool_params(cache);
+    p.extra = extra; p.status = seq_status; p.n = cache->seqs;
+    return kv_launch(kv_resize_kernel, dim3(kPoolCluster), kPoolThreads, sizeof(int) * cache->seqs, (cudaStream_t)cuda_stream, p);
+}
+
+mars_status_t mars_kv_fork(const mars_kv_cache_t *cache, const int32_t *src, const int32_t *dst, int pairs, int32_t *status,
+                           void *cuda_stream)
+{
+    const mars_status_t cs = kv_check(cache);
+    if (cs != MARS_OK) return cs;
+    if (!src || !dst || !status || pairs < 1) return MARS_ERR_INVALID_ARG;
+    if (pairs > MARS_KV_MAX_SEQS) return MARS_ERR_UNSUPPORTED;
+    PoolParams p = pool_params(cache);
+    p.src = src; p.dst = dst; p.status = status; p.n = pairs;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const mars_status_t r = kv_launch(kv_fork_kernel, dim3(1), kPoolThreads, sizeof(int) * pairs, st, p);
+    if (r != MARS_OK) return r;
+    ForkCopyParams c;
+    c.kv = kv_view(cache); c.src = src; c.dst = dst; c.status = status; c.pairs = pairs;
+    const dim3 grid(pairs, cache->layers);
+    return cache->head_dim == 128 ? kv_launch(kv_fork_copy_kernel<128>, grid, 256, 0, st, c)
+                                  : kv_launch(kv_fork_copy_kernel<64>, grid, 256, 0, st, c);
+}
+
+mars_status_t mars_kv_gather(const mars_kv_cache_t *cache, int layer0, int layers, int B, const int32_t *start,
+                             const int32_t *count, int rows, void *k_out, void *v_out, int dt, void *cuda_stream)
+{
+    const mars_status_t cs = kv_check(cache);
+    if (cs != MARS_OK) return cs;
+    if (!k_out || !v_out || B < 1 || B > cache->seqs || rows < 1 || layer0 < 0 || layers < 1 || layers > cache->layers - layer0)
+        return MARS_ERR_INVALID_ARG;
+    if (((uintptr_t)k_out & 15) || ((uintptr_t)v_out & 15)) return MARS_ERR_INVALID_ARG;
+    if (!kv_dtype_ok(dt) || rows > (1 << 30)) return MARS_ERR_UNSUPPORTED;
+    GatherParams p;
+    p.kv = kv_view(cache);
+    p.layer0 = layer0; p.start = start; p.count = count; p.B = B; p.rows = rows;
+    p.dst[0] = (unsigned char *)k_out; p.dst[1] = (unsigned char *)v_out;
+    const int64_t threads = (int64_t)rows * cache->kv_heads * 2 * (cache->head_dim / 16), blocks = (threads + 255) / 256;
+    if (blocks > 0x7fffffff) return MARS_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks, B, layers);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (cache->head_dim == 128)
+        return dt == MARS_BF16   ? kv_launch(kv_gather_kernel<128, MARS_BF16>, grid, 256, 0, st, p)
+               : dt == MARS_FP32 ? kv_launch(kv_gather_kernel<128, MARS_FP32>, grid, 256, 0, st, p)
+                                 : kv_launch(kv_gather_kernel<128, MARS_FP16>, grid, 256, 0, st, p);
+    return dt == MARS_BF16   ? kv_launch(kv_gather_kernel<64, MARS_BF16>, grid, 256, 0, st, p)
+           : dt == MARS_FP32 ? kv_launch(kv_gather_kernel<64, MARS_FP32>, grid, 256, 0, st, p)
+                             : kv_launch(kv_gather_kernel<64, MARS_FP16>, grid, 256, 0, st, p);
+}
+
+}  // extern "C"

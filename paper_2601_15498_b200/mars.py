@@ -110,6 +110,23 @@ def lib() -> ctypes.CDLL:
             L.mars_test_hook.restype = i32
             L.mars_device_check.argtypes = [ctypes.POINTER(i32), ctypes.POINTER(i32)]
             L.mars_device_check.restype = i32
+            L.mars_kv_pool_bytes.argtypes = [i32, i32, i32, i32, i32]
+            L.mars_kv_pool_bytes.restype = sz
+            L.mars_kv_append.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp]
+            L.mars_kv_append.restype = i32
+            L.mars_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+            L.mars_tree_attention_workspace_bytes.restype = sz
+            L.mars_tree_attention.argtypes = [vp, i32, vp, i64, i64, i32, i32, i32, i32, vp, vp, f32, u32, vp, i64,
+                                              i64, vp, vp, sz, vp]
+            L.mars_tree_attention.restype = i32
+            L.mars_kv_commit.argtypes = [vp, vp, i32, vp, i32, vp, vp, vp]
+            L.mars_kv_commit.restype = i32
+            L.mars_kv_fork.argtypes = [vp, vp, vp, i32, vp, vp]
+            L.mars_kv_fork.restype = i32
+            L.mars_kv_resize.argtypes = [vp, vp, vp, vp]
+            L.mars_kv_resize.restype = i32
+            L.mars_kv_gather.argtypes = [vp, i32, i32, i32, vp, vp, i32, vp, vp, i32, vp]
+            L.mars_kv_gather.restype = i32
             _lib = L
     return _lib
 

@@ -1,0 +1,504 @@
+"""The paged 4-bit KV cache on the device against the plain model: tables and stored bytes exactly,
+attention within bounds that count its roundings."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle as ko
+from paper_2601_15498_b200 import kv_cache as kv, mars, synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NP = {torch.bfloat16: np.float32, torch.float16: np.float32, torch.float32: np.float32}
+
+
+def i32(x):
+    return torch.as_tensor(np.asarray(x, np.int32), device=DEV)
+
+
+def host(t):
+    return t.float().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+class Pair:
+    """A device cache and its model, driven side by side."""
+
+    def __init__(self, layers=1, pages=64, heads=2, d=128, page=16, seqs=4, width=12, seed=0, scales="pow2"):
+        self.rng = np.random.default_rng(seed)
+        g = np.exp2(self.rng.integers(-3, 3, (layers, 2, heads))) if scales == "pow2" \
+            else self.rng.uniform(0.05, 3.0, (layers, 2, heads))
+        self.c = kv.KVCache.empty(layers, pages, heads, d, page, seqs, width, DEV, scales=g.astype(np.float32))
+        # what nobody wrote is garbage, NaN scales among it
+        self.c.pages.copy_(torch.as_tensor(self.rng.integers(0, 256, self.c.pages.shape, dtype=np.uint8)))
+        self.m = ko.Model(layers, pages, heads, d, page, seqs, width, g)
+
+    def resize(self, extra, check=True):
+        st = torch.full((self.c.seqs,), -7, dtype=torch.int32, device=DEV)
+        kv.resize(self.c, i32(extra), status=st)
+        want = self.m.resize(extra)
+        if check:
+            self.tables()
+            assert np.array_equal(host(st), want)
+        return want
+
+    def tables(self):
+        torch.cuda.synchronize()
+        c, m = self.c, self.m
+        for name, a, b in (("table", c.block_table, m.table), ("len", c.seq_len, m.len), ("held", c.seq_pages, m.held),
+                           ("refs", c.page_refs, m.refs), ("free", c.free_bits, m.free_bits())):
+            assert np.array_equal(host(a), b), name
+
+    def rand(self, B, N, dtype, loud=True):
+        x = self.rng.standard_normal((B, N, self.m.H, self.m.d))
+        if loud:
+            x *= np.exp2(self.rng.integers(-6, 7, (B, N, 1, 1)))
+        return torch.as_tensor(x, device=DEV).to(dtype)
+
+    def append(self, B, N, dtype=torch.bfloat16, count=None, k=None, v=None):
+        for layer in range(self.m.L):
+            k1 = self.rand(B, N, dtype) if k is None else k
+            v1 = self.rand(B, N, dtype) if v is None else v
+            st = torch.full((B,), -7, dtype=torch.int32, device=DEV)
+            kv.append(self.c, layer, k1, v1, count=None if count is None else i32(count), status=st)
+            assert np.array_equal(host(st), self.m.append(layer, host(k1), host(v1), count))
+
+    def grow(self, lens):
+        """Committed tokens: room, rows, lengths."""
+        ex = [-2] * self.m.S
+        ex[:len(lens)] = lens
+        assert (self.resize(ex, check=False)[:len(lens)] == 0).all()
+        self.append(len(lens), max(max(lens), 1), count=lens)
+        path = [n - 1 for n in lens]
+        kv.commit(self.c, None, i32(path))
+        self.m.len[:len(lens)], st = self.m.commit(None, path)
+        assert (st == 0).all()
+
+    def stored(self):
+        """Bytes of every written slot agree; the model keeps zeros where nothing was written."""
+        got = host(self.c.pages)
+        d, nb = self.m.d, self.m.page // 16
+        a = got.reshape(*got.shape[:3], nb, 18 * d)
+        b = self.m.pool().reshape(a.shape)
+        for b_ in range(self.m.S):
+            upto = self.m.len[b_]
+            for pos in range(upto):
+                p, s = self.m.at(b_, pos)
+                for lo, w in ((0, d // 2), (8 * d, d // 2), (16 * d, d // 16), (17 * d, d // 16)):
+                    x = a[:, p, :, s // 16, lo + (s % 16) * w:lo + (s % 16 + 1) * w]
+                    y = b[:, p, :, s // 16, lo + (s % 16) * w:lo + (s % 16 + 1) * w]
+                    assert np.array_equal(x, y), (b_, pos, lo)
+
+
+def trees(rng, B, N, absent=0.0):
+    p = np.full((B, N), -1, np.int32)
+    for i in range(1, N):
+        p[:, i] = (rng.uniform(0, 1, B) ** 1.5 * i).astype(np.int32)
+        p[rng.uniform(0, 1, B) < absent, i] = -1
+    return p
+
+
+def check_attention(pr, q, parent=None, count=None, scale=None, layer=0, out=None, workspace=None):
+    B, N, Hq, d = q.shape
+    out = torch.full((B, N, Hq, d), 7.25, dtype=q.dtype, device=DEV) if out is None else out
+    before = host(out).copy()
+    st = torch.full((B,), -7, dtype=torch.int32, device=DEV)
+    kv.tree_attention(q, pr.c, layer, None if parent is None else i32(parent), count=None if count is None else i32(count),
+                      scale=scale, out=out, status=st, workspace=workspace)
+    torch.cuda.synchronize()
+    want, live, status, mag, tot, amp = ko.attention(pr.m, layer, host(q).astype(np.float64), parent, count, scale)
+    assert np.array_equal(host(st), status)
+    got = host(out).astype(np.float64)
+    assert np.array_equal(got[~live], before[~live].astype(np.float64))       # rows without a result stay
+    # Roundings, relative to the probability-weighted |V| (mag):
+    #   P to fp16: 2^-11 each while it is a normal number; P is 2^7 or more at the row's largest score, so a
+    #   smaller one is off by at most 2^-25, that is 2^-32 of the largest probability, hence of 1: 2^-32 of
+    #   the plain sum of |V| (tot).  A score is a sum of d products with fp32 accumulation, off by at most
+    #   d * 2^-23 of sum |q||k| (amp, times log2 e in the kernel's units, back by ln 2), four more roundings
+    #   (scale, maximum, exponential) at 2^-23 of its size; a shift of a score moves a probability by that
+    #   fraction, and the sum below it too: twice.  q to fp16 after scaling: below 2^-25 of the row's largest
+    #   element, covered by one more 2^-23 of amp per element.  Sums over keys: keys * 2^-23.
+    # then half a step of the output type.
+    keys = int(pr.m.len.max()) + N
+    rel = 2.0 ** -11 + 2 * (2 * d + 8) * 2.0 ** -23 * amp[..., None] + 2 * (keys + 64) * 2.0 ** -23
+    half = torch.finfo(q.dtype).eps / 2
+    tol = mag * rel + tot * 2.0 ** -32
+    tol = tol + half * (np.abs(want) + tol) + 2.0 ** -24
+    err = np.abs(got - want)
+    bad = (err > tol) & live[..., None, None]
+    assert not bad.any(), (np.argwhere(bad)[:3], err[bad][:3], tol[bad][:3], want[bad][:3])
+    assert not np.isnan(got[live]).any()
+    return out
+
+
+# ------------------------------------------------------------------------------------- append, gather
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_append_stores_what_the_model_stores(d, page):
+    pr = Pair(layers=2, pages=40, heads=3, d=d, page=page, seqs=3, width=9, seed=d + page)
+    pr.grow([35, 0, 17])
+    pr.stored()
+    pr.resize([20, 3, 0])
+    pr.append(3, 20, torch.float16, count=[20, 3, 40])       # the last one has no room
+    pr.m.len[:] = [35 + 20, 3, 17]
+    pr.stored()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("scales", ["pow2", "any"])
+def test_append_types_scales_and_special_values(dtype, scales):
+    pr = Pair(heads=2, d=64, page=32, seqs=2, width=4, seed=5, scales=scales)
+    pr.resize([64, 64])
+    k, v = pr.rand(2, 64, dtype), pr.rand(2, 64, dtype)
+    k[0, 0, 0, :5] = torch.tensor([float("nan"), float("inf"), -float("inf"), -0.0, 0.0], device=DEV).to(dtype)
+    k[0, 1] = 0
+    v[0, 2] = torch.finfo(dtype).max
+    v[1, 3] = torch.finfo(dtype).smallest_normal
+    v[1, 4, :, :16] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0] * 2, device=DEV).to(dtype)   # borders
+    pr.append(2, 64, dtype, k=k, v=v)
+    pr.m.len[:] = 64
+    pr.stored()
+
+
+def test_append_of_strided_slices_and_gather_back():
+    pr = Pair(heads=2, d=128, page=64, seqs=3, width=4, seed=6)
+    pr.resize([30, 30, 30])
+    qkv = torch.randn((3, 30, 4 + 2 + 2, 128), device=DEV).to(torch.bfloat16)
+    k, v = qkv[:, :, 4:6], qkv[:, :, 6:]
+    pr.append(3, 30, k=k, v=v)
+    pr.m.len[:] = 30
+    pr.stored()
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        ko_, vo_ = kv.gather(pr.c, 0, 1, i32([3, 0, 90]), i32([27, 11, 9]), rows=27, dtype=dtype)
+        for b, (s, n) in enumerate(((3, 27), (0, 11), (90, 0))):
+            want = pr.m.rows(0, b, s, n) if n else [np.zeros((0, 2, 128))] * 2
+            for got, w in zip((ko_, vo_), want):
+                w = torch.as_tensor(w).float().to(dtype).float().numpy()      # 6 bits times a power of two: exact
+                assert np.array_equal(host(got)[0, b, :n], w)
+                assert (host(got)[0, b, n:] == 0).all()
+
+
+def test_fp32_rows_of_one_token_and_odd_counts():
+    pr = Pair(layers=3, pages=10, heads=1, d=64, page=16, seqs=5, width=3, seed=8)
+    pr.resize([1, 2, 16, 17, 0])
+    pr.append(5, 17, torch.float32, count=[1, 2, 16, 17, -4])
+    pr.m.len[:] = [1, 2, 16, 17, 0]
+    pr.stored()
+
+
+# ------------------------------------------------------------------------------------- tables
+
+def test_resize_grows_trims_releases_and_runs_out():
+    pr = Pair(pages=70, heads=1, d=64, page=16, seqs=40, width=6, seed=9)
+    rng = np.random.default_rng(10)
+    seen = set()
+    for step in range(12):
+        ex = rng.integers(-2, 60, 40)
+        ex[rng.integers(0, 40, 4)] = 2000                     # wider than the table
+        seen |= set(pr.resize(ex).tolist())
+        ln = [int(rng.integers(0, h * 16 + 1)) for h in pr.m.held]
+        pr.m.len[:] = ln
+        pr.c.seq_len.copy_(i32(ln))
+        if step % 3 == 2:
+            pr.resize([-1] * 20 + [0] * 20)
+    assert seen == {0, ko.NO_ROOM, ko.OUT_OF_PAGES}
+    pr.resize([-1] * 40)
+    assert (pr.m.refs == 0).all()
+
+
+@pytest.mark.parametrize("pages,seqs", [(1, 1), (31, 3), (33, 2), (40000, 1500), (140001, 8192)])
+def test_resize_of_small_and_large_pools(pages, seqs):
+    pr = Pair(pages=pages, heads=1, d=64, page=16, seqs=seqs, width=40, seed=pages)
+    rng = np.random.default_rng(seqs)
+    for _ in range(2):
+        pr.resize(rng.integers(-2, 500, seqs))
+    pr.resize(np.where(rng.uniform(0, 1, seqs) < 0.5, -1, 0))
+
+
+def test_fork_shares_pages_and_copies_the_ragged_one():
+    pr = Pair(layers=2, pages=60, heads=2, d=128, page=32, seqs=10, width=6, seed=11)
+    pr.grow([70, 64, 5, 0, 33])
+    src = [0, 0, 1, 2, 3, 9, 4, 4, 0, -1, 2, 5]
+    dst = [5, 6, 7, 8, 9, 3, 4, 8, 1, 2, 77, 9]     # empty source, self, taken twice, not empty, out of range
+    st = kv.fork(pr.c, i32(src), i32(dst))
+    want = pr.m.fork(src, dst)
+    assert np.array_equal(host(st), want)
+    assert want.tolist() == [0, 0, 0, 0, 0, 0, 9, 9, 9, 9, 9, 9]
+    pr.tables()
+    pr.stored()
+    # both go on by themselves
+    pr.resize([40] * 9 + [-2])
+    pr.append(9, 40)
+    pr.m.len[:9] += 40
+    pr.c.seq_len.copy_(i32(pr.m.len))
+    pr.stored()
+    pr.resize([-1, -1, -2, -2, -2, -2, -2, 0, 0, 0])
+    pr.tables()
+    pr.stored()
+
+
+def test_fork_out_of_pages():
+    pr = Pair(pages=8, heads=1, d=64, page=16, seqs=9, width=4, seed=12)
+    pr.grow([20, 16, 40])                                     # 2 + 1 + 3 of 8 pages
+    src, dst = [0, 1, 2, 0, 1], [3, 4, 5, 6, 7]
+    st = kv.fork(pr.c, i32(src), i32(dst))
+    want = pr.m.fork(src, dst)
+    assert np.array_equal(host(st), want) and want.tolist() == [0, 0, 0, 7, 0]
+    pr.tables()
+    pr.stored()
+
+
+# ------------------------------------------------------------------------------------- commit
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_commit_moves_the_path(d, page, in_place):
+    pr = Pair(layers=3, pages=64, heads=2, d=d, page=page, seqs=7, width=10, seed=13)
+    pr.grow([11, 30, 0, 16, 5, 7, 9])
+    pr.resize([50] * 7)
+    pr.append(7, 50)
+    path = np.full((7, 30), -1, np.int32)
+    acc = np.zeros(7, np.int32)
+    for b, nodes in enumerate(([0, 1, 2, 3], [0, 7, 9, 30, 31, 49], [0], list(range(0, 50, 2)), [0, 3, 3], [0, 4, 90],
+                               [])):
+        path[b, :len(nodes)] = nodes
+        acc[b] = len(nodes) - 1
+    path[3, 25:] = 7
+    new = None if in_place else torch.full((7,), -5, dtype=torch.int32, device=DEV)
+    st = torch.full((7,), -7, dtype=torch.int32, device=DEV)
+    got = kv.commit(pr.c, i32(path), i32(acc), new_len=new, status=st)
+    want, status = pr.m.commit(path, acc)
+    assert np.array_equal(host(st), status) and status.tolist() == [0, 0, 0, 0, 8, 8, 0]
+    assert np.array_equal(host(got), want)
+    assert np.array_equal(host(pr.c.seq_len), want if in_place else pr.m.len)
+    pr.m.len[:] = want
+    pr.stored()
+
+
+def test_commit_of_long_paths_and_bad_lengths():
+    pr = Pair(layers=1, pages=200, heads=1, d=128, page=16, seqs=5, width=40, seed=14)
+    pr.grow([3, 3, 3, 3, 3])
+    pr.resize([200] * 5)
+    pr.append(5, 200)
+    path = np.tile(np.arange(0, 200, 3, dtype=np.int32), (5, 1))       # 67 nodes, several batches of a warp
+    acc = np.array([66, 67, -2, 40, -1], np.int32)
+    st = torch.zeros((5,), dtype=torch.int32, device=DEV)
+    kv.commit(pr.c, i32(path), i32(acc), status=st)
+    want, status = pr.m.commit(path, acc)
+    assert np.array_equal(host(st), status) and status.tolist() == [0, 8, 8, 0, 0]
+    pr.m.len[:] = want
+    pr.tables()
+    pr.stored()
+
+
+# ------------------------------------------------------------------------------------- attention
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,group", [(2, 1), (1, 4), (2, 5), (1, 16), (1, 24)])
+def test_attention_of_single_tokens(dtype, d, heads, group):
+    lens = [0, 1, 15, 16, 17, 63, 64, 65, 200, 331]
+    pr = Pair(pages=120, heads=heads, d=d, page=16, seqs=10, width=22, seed=group + d)
+    pr.grow(lens)
+    pr.resize([1] * 10)
+    pr.append(10, 1, dtype)
+    q = torch.randn((10, 1, heads * group, d), device=DEV).to(dtype)
+    check_attention(pr, q)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("N", [2, 6, 33, 60, 65])
+def test_attention_of_trees(dtype, d, page, N):
+    rng = np.random.default_rng(N)
+    lens = [0, 1, 100, 64, 130]
+    pr = Pair(pages=60, heads=2, d=d, page=page, seqs=5, width=10, seed=N)
+    pr.grow(lens)
+    pr.resize([N] * 5)
+    pr.append(5, N, dtype)
+    q = torch.randn((5, N, 4, d), device=DEV).to(dtype)
+    check_attention(pr, q, parent=trees(rng, 5, N))
+    count = np.array([N, N // 2, 0, 1, N + 9], np.int32)
+    check_attention(pr, q, parent=trees(rng, 5, N, absent=0.15), count=count)
+    check_attention(pr, q, parent=trees(rng, 1, N)[0], count=count)
+
+
+@pytest.mark.parametrize("d,group", [(64, 1), (128, 3), (128, 8), (64, 32)])
+@pytest.mark.parametrize("N", [3, 8, 77, 150])
+def test_attention_of_chains(d, group, N):
+    lens = [0, 50, 7, 129]
+    pr = Pair(pages=140, heads=1, d=d, page=16, seqs=4, width=20, seed=N + d)
+    pr.grow(lens)
+    pr.resize([N] * 4)
+    pr.append(4, N)
+    q = torch.randn((4, N, group, d), device=DEV).to(torch.float16)
+    check_attention(pr, q)
+    check_attention(pr, q, count=[N, N - 1, 1, 0], scale=0.31)
+
+
+def test_attention_of_a_large_tree():
+    N = 1024
+    pr = Pair(pages=80, heads=1, d=64, page=32, seqs=2, width=40, seed=3)
+    pr.grow([33, 2])
+    pr.resize([N, N])
+    pr.append(2, N)
+    q = torch.randn((2, N, 2, 64), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, parent=trees(np.random.default_rng(4), 2, N), count=[N, 700])
+
+
+def test_attention_statuses_and_untouched_rows():
+    pr = Pair(pages=60, heads=2, d=64, page=16, seqs=6, width=8, seed=21)
+    pr.grow([20, 30, 40, 5, 6, 0])
+    pr.resize([6, 2, 6, 6, 6, 6])                 # sequence 1 has room for 34 tokens, not 36... its page holds 32
+    pr.append(6, 6)
+    parent = trees(np.random.default_rng(1), 6, 6)
+    parent[2, 3] = 4                              # no tree
+    parent[3, 0] = 0
+    parent[4, 5] = -2
+    pr.m.len[5] = -3                              # nonsense length
+    pr.c.seq_len.copy_(i32(pr.m.len))
+    q = torch.randn((6, 6, 4, 64), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, parent=parent, count=[6, 6, 6, 6, 6, 6])
+
+
+def test_attention_large_scores_and_special_rows_of_q():
+    pr = Pair(pages=40, heads=1, d=128, page=16, seqs=3, width=12, seed=22)
+    pr.grow([90, 17, 3])
+    pr.resize([4] * 3)
+    pr.append(3, 4)
+    q = torch.randn((3, 4, 2, 128), device=DEV)
+    q[0, 0] *= 1e-30                              # scores of nothing: the mean of V
+    q[0, 1] = 0
+    q[1, 2] *= 3e-3
+    q[2, 0, :, ::2] *= 1e-4
+    check_attention(pr, q.to(torch.bfloat16))
+    # scores of thousands (one-hot rows): the bound on a probability grows with them, the row stays finite
+    big = (q * 500).to(torch.bfloat16)
+    out = kv.tree_attention(big, pr.c, 0)
+    assert torch.isfinite(out).all()
+    nan = q.to(torch.bfloat16)
+    nan[0, 0, 0, 3] = float("nan")
+    out = kv.tree_attention(nan, pr.c, 0)
+    assert out[0, 0, 0].isnan().all() and torch.isfinite(out[0, 0, 1]).all() and torch.isfinite(out[1:]).all()
+
+
+def test_attention_of_strided_q_and_out_in_a_second_layer():
+    pr = Pair(layers=2, pages=40, heads=2, d=128, page=16, seqs=3, width=12, seed=23)
+    pr.grow([90, 17, 3])
+    pr.resize([5] * 3)
+    pr.append(3, 5)
+    qkv = torch.randn((3, 5, 4 + 2 + 2, 128), device=DEV).to(torch.bfloat16)
+    wide = torch.full((3, 5, 6, 128), 7.25, dtype=torch.bfloat16, device=DEV)
+    check_attention(pr, qkv[:, :, :4], layer=1, out=wide[:, :, 1:5])
+    assert (wide[:, :, 0] == 7.25).all() and (wide[:, :, 5] == 7.25).all()
+
+
+def test_page_ids_outside_the_pool_are_not_followed():
+    """A damaged table entry (no call writes one) is read as NaN for its sequence alone."""
+    pr = Pair(pages=40, heads=2, d=64, page=16, seqs=3, width=12, seed=24)
+    pr.grow([90, 50, 20])
+    pr.resize([2] * 3)
+    pr.append(3, 2)
+    q = torch.randn((3, 2, 4, 64), device=DEV).to(torch.bfloat16)
+    good = kv.tree_attention(q, pr.c, 0)
+    for bad in (-1, 40, 1 << 30, -(1 << 31)):
+        pr.c.block_table[1, 1] = bad
+        out = kv.tree_attention(q, pr.c, 0)
+        assert out[1].isnan().all() and torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+
+
+def test_attention_repeats_itself_and_splits_evenly():
+    """One long sequence over the whole grid, ragged neighbours, one workspace for many calls."""
+    pr = Pair(pages=700, heads=2, d=64, page=128, seqs=4, width=400, seed=25)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    lens = [40000, 130, 0, 9000]
+    pr.resize([n + 3 for n in lens])
+    k = torch.randn((4, 40003, 2, 64), generator=g, device=DEV).to(torch.bfloat16)
+    v = torch.randn((4, 40003, 2, 64), generator=g, device=DEV).to(torch.bfloat16)
+    kv.append(pr.c, 0, k, v, count=i32([n + 3 for n in lens]))
+    pr.c.seq_len.copy_(i32(lens))
+    q = torch.randn((4, 3, 8, 64), generator=g, device=DEV).to(torch.bfloat16)
+    ws = kv.attention_workspace(q, pr.c)
+    out = [kv.tree_attention(q, pr.c, 0, workspace=ws).clone() for _ in range(3)] + [kv.tree_attention(q, pr.c, 0)]
+    for o in out[1:]:
+        assert torch.equal(o, out[0])
+    kd, vd = kv.gather(pr.c, 0, 1, None, i32([n + 3 for n in lens]), rows=40003, dtype=torch.float32)
+    for b, n in enumerate(lens):
+        for i in range(3):
+            kk, vv = kd[0, b, :n + i + 1].double(), vd[0, b, :n + i + 1].double()
+            z = torch.einsum("thd,hgd->hgt", kk, q[b, i].double().view(2, 4, 64)) / 8
+            w = torch.softmax(z, -1)
+            o = torch.einsum("hgt,thd->hgd", w, vv).reshape(8, 64)
+            mag = torch.einsum("hgt,thd->hgd", w, vv.abs()).reshape(8, 64)
+            tol = mag * (2.0 ** -11 + 2.0 ** -13 + 40000 * 2.0 ** -24) + 2.0 ** -8 * o.abs()
+            assert ((out[0][b, i].double() - o).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------------------------- together
+
+def test_one_decode_cycle_of_the_library():
+    """Room, append, attention, LM head with verification, commit, trim: twice, as a program runs them."""
+    B, N, H, G, d, V = 3, 12, 2, 4, 64, 2000
+    pr = Pair(layers=2, pages=60, heads=H, d=d, page=16, seqs=B, width=12, seed=31)
+    pr.grow([40, 9, 77])
+    g = torch.Generator(device=DEV)
+    g.manual_seed(7)
+    wo = (torch.randn((V, H * G * d), generator=g, device=DEV) * 0.2).to(torch.bfloat16)
+    ws = None
+    for cycle in range(2):
+        pr.resize([N] * B)
+        parent = trees(np.random.default_rng(cycle), B, N)
+        k, v = pr.rand(B, N, torch.bfloat16, loud=False), pr.rand(B, N, torch.bfloat16, loud=False)
+        pr.append(B, N, k=k, v=v)
+        q = torch.randn((B, N, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+        ws = kv.attention_workspace(q, pr.c) if ws is None else ws
+        o = torch.full(q.shape, 7.25, dtype=q.dtype, device=DEV)
+        check_attention(pr, q, parent=parent, layer=1, out=o, workspace=ws)
+        hidden = o.view(B * N, H * G * d)
+        top = torch.topk(hidden.float() @ wo.float().T, 2).indices.cpu().numpy().reshape(B, N, 2)
+        tok = np.zeros((B, N), np.int32)
+        for i in range(1, N):
+            tok[:, i] = top[np.arange(B), parent[:, i], 0]
+        out = mars.lmhead_verify(hidden, wo, None, tok, parent, 0.9)
+        path, acc = host(out["path_nodes"]), host(out["accept_len"])
+        assert (acc > 0).any()
+        kv.commit(pr.c, out["path_nodes"], out["accept_len"])
+        pr.m.len[:], st = pr.m.commit(path, acc)
+        assert (st == 0).all()
+        pr.resize([0] * B)
+        pr.stored()
+
+
+def test_cycle_in_a_captured_graph():
+    """append, attention and commit captured once and replayed on new contents."""
+    B, N, H, d = 2, 6, 2, 128
+    pr = Pair(pages=40, heads=H, d=d, page=16, seqs=B, width=12, seed=33)
+    pr.grow([21, 50])
+    pr.resize([40] * B)
+    parent = trees(np.random.default_rng(5), B, N)
+    k, v, q = (torch.zeros((B, N, h, d), dtype=torch.bfloat16, device=DEV) for h in (H, H, 2 * H))
+    par, path, acc = i32(parent), i32(np.zeros((B, 4))), i32([0] * B)
+    o = torch.zeros((B, N, 2 * H, d), dtype=torch.bfloat16, device=DEV)
+    ws = kv.attention_workspace(q, pr.c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        kv.append(pr.c, 0, k, v)
+        kv.tree_attention(q, pr.c, 0, par, out=o, workspace=ws)
+        kv.commit(pr.c, path, acc)
+    for step in range(3):
+        k.copy_(pr.rand(B, N, torch.bfloat16, loud=False))
+        v.copy_(pr.rand(B, N, torch.bfloat16, loud=False))
+        q.copy_(torch.randn(q.shape, device=DEV))
+        path.copy_(i32([[0, 2, 5, -1], [0, 1, 3, 4]]))
+        acc.copy_(i32([2, 3]))
+        graph.replay()
+        torch.cuda.synchronize()
+        pr.m.append(0, host(k), host(v))
+        want, live, _, mag, _, _ = ko.attention(pr.m, 0, host(q).astype(np.float64), parent)
+        assert (np.abs(host(o) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag + 1e-6).all()
+        pr.m.len[:], _ = pr.m.commit(host(path), host(acc))
+        pr.tables()
+        pr.stored()
