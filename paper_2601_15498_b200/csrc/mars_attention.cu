@@ -26,13 +26,13 @@
 
 namespace mars {
 
-constexpr int kRowsM = 16;            // query rows per tile
+constexpr int kRowsM = RowsShape::M;  // query rows per tile
+constexpr int kUnit = RowsShape::unit_keys(kRowsM);
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = 32 * kRowsWarps;
 constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
 constexpr int kRowsOcc = 3;           // blocks per SM
-constexpr int kTunedSms = 148;
-constexpr int kRowsGrid = kTunedSms * kRowsOcc;
+constexpr int kRowsGrid = kAttnSms * kRowsOcc;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
@@ -49,23 +49,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int DT>
-__device__ __forceinline__ float2 widen2(uint32_t w)
-{
-    if constexpr (DT == MARS_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-    else return f16x2_to_float2(w);
-}
-
-// Power of two that brings a row whose largest magnitude is m into [1, 2), and its inverse.
-__device__ __forceinline__ void row_scale(float m, float *down, float *up)
-{
-    const uint32_t e = (__float_as_uint(m) >> 23) & 0xffu;
-    if (e == 0u || e >= 254u) { *down = e == 0u ? 1.0f : 0.0078125f; *up = e == 0u ? 1.0f : 128.0f; }
-    else { *down = __uint_as_float((254u - e) << 23); *up = __uint_as_float(e << 23); }
-    // e == 0: zero or subnormal rows count as they are (their products vanish next to any other term);
-    // e >= 254: the row's fp16 form would need 2^-127; 2^-7 leaves infinities to the conversion
-}
-
 template <int D>
 __host__ __device__ constexpr int rows_slot_floats() { return kRowsM * (D + 2); }
 
@@ -75,16 +58,6 @@ constexpr size_t rows_smem_bytes()
     return (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D) > (size_t)kRowsWarps * kRowsM * (D + 4) * 4
                ? (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D)
                : (size_t)kRowsWarps * kRowsM * (D + 4) * 4;
-}
-
-template <int DT>
-__device__ __forceinline__ void store_out(unsigned char *out, int64_t at, const float *x, int n)
-{
-    // n (8) consecutive values, 16-byte aligned
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = DT == MARS_BF16 ? bf16x2_from(x[2 * i], x[2 * i + 1]) : f16x2_from(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<uint4 *>(out + at * 2) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int D, int DT>
@@ -108,9 +81,9 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
     unsigned char *ring = s_ring + warp * kRowsStages * kBlk;
     const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
 
-    AttnRange r = attn_split<kRowsM, kRowsThreads>(p);
+    AttnRange r = attn_split<RowsShape, kRowsThreads>(p);
     for (int64_t u = r.begin; u < r.end;) {
-        const AttnSegment sg = attn_segment<kRowsM>(p, r, u);
+        const AttnSegment sg = attn_segment<RowsShape>(p, r, u);
         const bool whole = sg.unit0 == 0 && sg.unit1 == sg.units;
         const int rows = min(kRowsM, sg.n * p.group - sg.tile * kRowsM);
         const int row0 = sg.tile * kRowsM;               // first row of the tile: node row0/group
@@ -407,7 +380,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
                 for (int k = 0; k < kPer; ++k) acc[k] *= f;
                 const int64_t at = ((int64_t)sg.b * p.N + nd) * p.out_row + (int64_t)(sg.head * p.group + row % p.group) * p.out_head + od;
 #pragma unroll
-                for (int k = 0; k < kPer; k += 8) store_out<DT>(p.out, at + k, acc + k, 8);
+                for (int k = 0; k < kPer; k += 8) store_out8<DT>(p.out, at + k, acc + k);
             }
         }
         __syncthreads();                                  // masks, ring and sums free for the next segment
@@ -424,7 +397,6 @@ static mars_status_t rows_launch(const AttnParams &p, cudaStream_t st)
     return MARS_OK;
 }
 
-constexpr size_t kAttnCounterBytes = 4096;
 static_assert(kRowsGrid * sizeof(unsigned) <= kAttnCounterBytes, "one counter per block");
 
 static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
@@ -433,9 +405,15 @@ static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
            q_heads % kv_heads == 0 && (d == 64 || d == 128) && (int64_t)N * (q_heads / kv_heads) <= (1 << 30);
 }
 
-static size_t attn_workspace(int d)
+// The kernel for tiles of query rows takes over where a KV head has more of them than two tiles of the
+// other hold.
+static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > 2 * kRowsM && !(tree && N > kTileMaxTree); }
+
+static size_t attn_workspace(int N, int group, int d)
 {
-    return kAttnCounterBytes + sizeof(float) * 2 * kRowsGrid * (size_t)(d == 128 ? rows_slot_floats<128>() : rows_slot_floats<64>());
+    const size_t rows = sizeof(float) * 2 * kRowsGrid * (size_t)(d == 128 ? rows_slot_floats<128>() : rows_slot_floats<64>());
+    const size_t tile = attn_use_tiles(N, group, false) ? attn_tile_partial_bytes(d) : 0;
+    return kAttnCounterBytes + (rows > tile ? rows : tile);
 }
 
 }  // namespace mars
@@ -446,7 +424,7 @@ extern "C" {
 
 size_t mars_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_heads, int head_dim)
 {
-    return attn_sizes_ok(B, N, q_heads, kv_heads, head_dim) ? attn_workspace(head_dim) : 0;
+    return attn_sizes_ok(B, N, q_heads, kv_heads, head_dim) ? attn_workspace(N, q_heads / kv_heads, head_dim) : 0;
 }
 
 mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const void *q, int64_t q_row, int64_t q_head,
@@ -466,7 +444,7 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     if (((uintptr_t)q & 15) || ((uintptr_t)out & 15) || (q_row & 7) || (q_head & 7) || (out_row & 7) || (out_head & 7) ||
         ((int64_t)B * N > 1 && out_row == 0) || (q_heads > 1 && out_head == 0))
         return MARS_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < attn_workspace(cache->head_dim)) return MARS_ERR_WORKSPACE;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < attn_workspace(N, q_heads / cache->kv_heads, cache->head_dim)) return MARS_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kAttnCounterBytes, st) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -484,6 +462,7 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     p.scale_log2 = scale * 1.4426950408889634f;
     p.counters = (unsigned *)workspace;
     p.partial = (float *)((unsigned char *)workspace + kAttnCounterBytes);
+    if (attn_use_tiles(N, p.group, parent != nullptr)) return attn_tile_launch(p, cache->head_dim, dt, st);
     if (cache->head_dim == 128)
         return dt == MARS_BF16 ? rows_launch<128, MARS_BF16>(p, st) : rows_launch<128, MARS_FP16>(p, st);
     return dt == MARS_BF16 ? rows_launch<64, MARS_BF16>(p, st) : rows_launch<64, MARS_FP16>(p, st);

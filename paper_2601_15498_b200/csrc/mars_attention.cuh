@@ -2,8 +2,9 @@
 // over the thread blocks, the draft tree's ancestor masks, partial results and their merge.
 //
 // Work is cut along the keys, evenly over the grid.  An item is (sequence, KV head, tile of query
-// rows); its keys come in units of `kUnit`; the units of all items, laid end to end, are dealt to the
-// blocks in equal contiguous ranges.  Lengths live on the device, so every block works the split out
+// rows); its keys come in units of a kernel-specific number of keys, chosen so that every unit costs
+// about the same; the units of all items, laid end to end, are dealt to the blocks in equal contiguous
+// ranges.  Lengths live on the device, so every block works the split out
 // by itself (one pass over seq_len).  A block's range begins and ends anywhere, so the first and the
 // last item of it may be shared with neighbours: such a block leaves a partial result (unnormalised
 // output, maximum, sum) in the workspace, and the last one to arrive merges them in block order.
@@ -19,7 +20,16 @@
 
 namespace mars {
 
-constexpr int kUnit = 64;            // keys per unit of the split
+// Tile shapes: query rows per tile and keys per unit of the split.
+struct RowsShape {
+    static constexpr int M = 16;
+    static __host__ __device__ constexpr int unit_keys(int) { return 64; }
+};
+struct TileShape {
+    static constexpr int M = 256;
+    // tiles of up to 128 rows fill one of the kernel's two accumulators, which then share the keys
+    static __host__ __device__ constexpr int unit_keys(int rows) { return rows > 128 ? 128 : 256; }
+};
 
 struct AttnParams {
     KvView kv;
@@ -56,28 +66,37 @@ __device__ __forceinline__ int attn_nodes(const AttnParams &p, int b, int *len, 
     return n;
 }
 
+template <class S>
+__device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + S::M - 1) / S::M; }
+
+template <class S>
+__device__ __forceinline__ int attn_tile_rows(const AttnParams &p, int n, int mt) { return min(S::M, n * p.group - mt * S::M); }
+
 // Keys that the rows of tile mt (rows mt*M .. of n*group) may see: all nodes of a tree, the nodes up
 // to the tile's last one of a chain.
-template <int M>
+template <class S>
 __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, int mt)
 {
     if (p.parent) return len + n;
-    return len + min(n, ((mt + 1) * M - 1) / p.group + 1);
+    return len + min(n, ((mt + 1) * S::M - 1) / p.group + 1);
 }
 
-__device__ __forceinline__ int attn_units(int keys) { return (keys + kUnit - 1) / kUnit; }
-
-template <int M>
-__device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + M - 1) / M; }
+template <class S>
+__device__ __forceinline__ int attn_units(const AttnParams &p, int len, int n, int mt)
+{
+    const int uk = S::unit_keys(attn_tile_rows<S>(p, n, mt));
+    return (attn_keys<S>(p, len, n, mt) + uk - 1) / uk;
+}
 
 // Units of one KV head of a sequence.
-template <int M>
+template <class S>
 __device__ __forceinline__ int64_t attn_head_units(const AttnParams &p, int len, int n)
 {
-    const int tiles = attn_tiles<M>(p, n);
-    if (p.parent || tiles <= 1) return (int64_t)tiles * (n ? attn_units(attn_keys<M>(p, len, n, 0)) : 0);
+    if (n == 0) return 0;
+    const int tiles = attn_tiles<S>(p, n);
+    if (p.parent) return (int64_t)(tiles - 1) * attn_units<S>(p, len, n, 0) + attn_units<S>(p, len, n, tiles - 1);
     int64_t u = 0;
-    for (int mt = 0; mt < tiles; ++mt) u += attn_units(attn_keys<M>(p, len, n, mt));
+    for (int mt = 0; mt < tiles; ++mt) u += attn_units<S>(p, len, n, mt);
     return u;
 }
 
@@ -90,7 +109,7 @@ struct AttnRange {
 
 // The block's share of the batch (all threads call; kThreads = blockDim.x).  Block 0 also reports the
 // status of sequences that have no work.
-template <int M, int kThreads>
+template <class S, int kThreads>
 __device__ AttnRange attn_split(const AttnParams &p)
 {
     __shared__ int64_t s_sum[kThreads / 32 + 1];
@@ -103,7 +122,7 @@ __device__ AttnRange attn_split(const AttnParams &p)
     for (int b = lo; b < hi; ++b) {
         int len, st;
         const int n = attn_nodes(p, b, &len, &st);
-        sum += attn_head_units<M>(p, len, n) * p.kv.kv_heads;
+        sum += attn_head_units<S>(p, len, n) * p.kv.kv_heads;
         if (n == 0 && p.status && blockIdx.x == 0) p.status[b] = st;
     }
     int64_t inc = sum;
@@ -129,7 +148,7 @@ __device__ AttnRange attn_split(const AttnParams &p)
         for (int b = lo; b < hi; ++b) {
             int len, st;
             const int n = attn_nodes(p, b, &len, &st);
-            const int64_t u = attn_head_units<M>(p, len, n) * p.kv.kv_heads;
+            const int64_t u = attn_head_units<S>(p, len, n) * p.kv.kv_heads;
             if (r.begin < at + u) { s_b = b; s_at = at; break; }
             at += u;
         }
@@ -150,7 +169,7 @@ struct AttnSegment {
 };
 
 // Decodes the segment that begins at unit u (block-uniform); moves r.b / r.at on as sequences end.
-template <int M>
+template <class S>
 __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRange &r, int64_t u)
 {
     AttnSegment s;
@@ -158,7 +177,7 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRan
     int64_t hu;
     for (;;) {
         s.n = attn_nodes(p, r.b, &s.len, &st);
-        hu = attn_head_units<M>(p, s.len, s.n);
+        hu = attn_head_units<S>(p, s.len, s.n);
         if (u < r.at + hu * p.kv.kv_heads) break;
         r.at += hu * p.kv.kv_heads;
         ++r.b;
@@ -169,25 +188,60 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRan
     int64_t rest = in_seq - s.head * hu;
     s.item = r.at + s.head * hu;
     s.tile = 0;
-    s.keys = attn_keys<M>(p, s.len, s.n, 0);
-    s.units = attn_units(s.keys);
+    s.units = attn_units<S>(p, s.len, s.n, 0);
     if (p.parent) {
-        s.tile = (int)(rest / s.units);
+        const int last = attn_tiles<S>(p, s.n) - 1;
+        s.tile = (int)min(rest / s.units, (int64_t)last);
         rest -= (int64_t)s.tile * s.units;
         s.item += (int64_t)s.tile * s.units;
+        if (s.tile == last) s.units = attn_units<S>(p, s.len, s.n, last);
     } else {
         while (rest >= s.units) {
             rest -= s.units;
             s.item += s.units;
-            ++s.tile;
-            s.keys = attn_keys<M>(p, s.len, s.n, s.tile);
-            s.units = attn_units(s.keys);
+            s.units = attn_units<S>(p, s.len, s.n, ++s.tile);
         }
     }
+    s.keys = attn_keys<S>(p, s.len, s.n, s.tile);
     s.unit0 = (int)rest;
     s.unit1 = (int)min((int64_t)s.units, rest + (r.end - u));
     return s;
 }
+
+template <int DT>
+__device__ __forceinline__ float2 widen2(uint32_t w)
+{
+    if constexpr (DT == MARS_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    else return f16x2_to_float2(w);
+}
+
+// Power of two that brings a row whose largest magnitude is m into [1, 2), and its inverse.
+__device__ __forceinline__ void row_scale(float m, float *down, float *up)
+{
+    const uint32_t e = (__float_as_uint(m) >> 23) & 0xffu;
+    if (e == 0u || e >= 254u) { *down = e == 0u ? 1.0f : 0.0078125f; *up = e == 0u ? 1.0f : 128.0f; }
+    else { *down = __uint_as_float((254u - e) << 23); *up = __uint_as_float(e << 23); }
+    // e == 0: zero or subnormal rows count as they are (their products vanish next to any other term);
+    // e >= 254: the row's fp16 form would need 2^-127; 2^-7 leaves infinities to the conversion
+}
+
+// 8 consecutive output values at element `at` (16-byte aligned).
+template <int DT>
+__device__ __forceinline__ void store_out8(unsigned char *out, int64_t at, const float *x)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = DT == MARS_BF16 ? bf16x2_from(x[2 * i], x[2 * i + 1]) : f16x2_from(x[2 * i], x[2 * i + 1]);
+    *reinterpret_cast<uint4 *>(out + at * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+constexpr int kAttnSms = 148;                   // SM count that the grids are sized for
+constexpr size_t kAttnCounterBytes = 4096;      // one counter per block, at the head of the workspace
+
+// Kernel for many query rows per KV head (mars_attention_tile.cu).
+constexpr int kTileMaxTree = 512;               // its mask store holds trees of up to this many nodes
+size_t attn_tile_partial_bytes(int d);
+mars_status_t attn_tile_launch(const AttnParams &p, int d, int dt, cudaStream_t st);
 
 // Ancestor-or-self masks of the nodes that a tile's rows belong to, and which of them are computed.
 //   mask   [nodes of the tile][words]  bit m of node i: m is i or an ancestor of i (trees only)
