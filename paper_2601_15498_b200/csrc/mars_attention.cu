@@ -87,10 +87,12 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
         const bool whole = sg.unit0 == 0 && sg.unit1 == sg.units;
         const int rows = min(kRowsM, sg.n * p.group - sg.tile * kRowsM);
         const int row0 = sg.tile * kRowsM;               // first row of the tile: node row0/group
-        const int node0 = row0 / p.group;
-        const int nodes = (row0 + rows - 1) / p.group - node0 + 1;
-        const int words = p.parent ? (sg.n + 31) >> 5 : 0;
-        const int st = attn_tree_masks(p, sg.b, sg.n, node0, nodes, s_par, s_mask, words, s_live);
+        const int node0 = attn_node(p, row0);
+        const int nodes = attn_node(p, row0 + rows - 1) - node0 + 1;
+        const int words = (sg.n + 31) >> 5;
+        const int st = p.parent ? attn_tree_masks(p, sg.b, sg.n, node0, nodes, s_par, s_mask, words, s_live, &s_last, tid,
+                                                  kRowsThreads, [] { __syncthreads(); })
+                                : MARS_SEQ_OK;
         if (tid == 0 && p.status && sg.head == 0 && sg.tile == 0 && sg.unit0 == 0) p.status[sg.b] = st;
 
         // ---- Q fragments: rows g and g + 8, d = t*kCode + 4*s .. of k-step s
@@ -101,12 +103,13 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
         for (int half = 0; half < 2; ++half) {
             const int row = row0 + g + 8 * half;
             const bool in = g + 8 * half < rows;
-            node[half] = in ? row / p.group - node0 : -1;
+            const int nd = attn_node(p, row);
+            node[half] = in ? nd - node0 : -1;
             uint4 w[kCode / 8];
             float m = 0.0f;
             if (in) {
-                const int64_t at = ((int64_t)sg.b * p.N + row / p.group) * p.q_row +
-                                   (int64_t)(sg.head * p.group + row % p.group) * p.q_head + t * kCode;
+                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.q_row +
+                                   (int64_t)(sg.head * p.group + row - nd * p.group) * p.q_head + t * kCode;
 #pragma unroll
                 for (int i = 0; i < kCode / 8; ++i) {
                     w[i] = reinterpret_cast<const uint4 *>(p.q + at * 2)[i];
@@ -373,12 +376,12 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
             }
         }
         if (write && orow < rows) {
-            const int row = row0 + orow, nd = row / p.group;
-            if (s_live[nd - node0]) {
+            const int row = row0 + orow, nd = attn_node(p, row);
+            if (!p.parent || s_live[nd - node0]) {
                 const float f = p.scales[p.kv.kv_heads + sg.head] / sum;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) acc[k] *= f;
-                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.out_row + (int64_t)(sg.head * p.group + row % p.group) * p.out_head + od;
+                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.out_row + (int64_t)(sg.head * p.group + row - nd * p.group) * p.out_head + od;
 #pragma unroll
                 for (int k = 0; k < kPer; k += 8) store_out8<DT>(p.out, at + k, acc + k);
             }
@@ -459,6 +462,7 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     p.parent = parent; p.count = count; p.status = seq_status;
     p.shared_parent = (flags & MARS_SHARED_PARENT) != 0;
     p.B = B; p.N = N; p.group = q_heads / cache->kv_heads;
+    p.group_inv = p.group > 1 ? ~0ull / (unsigned)p.group + 1 : 0;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.counters = (unsigned *)workspace;
     p.partial = (float *)((unsigned char *)workspace + kAttnCounterBytes);

@@ -43,6 +43,7 @@ struct AttnParams {
     int32_t *status;                 // or null
     int shared_parent;
     int B, N, group;
+    uint64_t group_inv;              // floor(2^64 / group) + 1 (unused for 1)
     float scale_log2;                // softmax scale * log2(e)
     unsigned *counters;              // [grid]
     float *partial;                  // [2 * grid] slots of rows * (d + 2) floats
@@ -66,6 +67,12 @@ __device__ __forceinline__ int attn_nodes(const AttnParams &p, int b, int *len, 
     return n;
 }
 
+// Node of a query row (rows of a KV head are node-major): row / group.
+__device__ __forceinline__ int attn_node(const AttnParams &p, int row)
+{
+    return p.group == 1 ? row : (int)__umul64hi((uint64_t)(uint32_t)row, p.group_inv);
+}
+
 template <class S>
 __device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + S::M - 1) / S::M; }
 
@@ -78,7 +85,7 @@ template <class S>
 __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, int mt)
 {
     if (p.parent) return len + n;
-    return len + min(n, ((mt + 1) * S::M - 1) / p.group + 1);
+    return len + min(n, attn_node(p, (mt + 1) * S::M - 1) + 1);
 }
 
 template <class S>
@@ -88,15 +95,18 @@ __device__ __forceinline__ int attn_units(const AttnParams &p, int len, int n, i
     return (attn_keys<S>(p, len, n, mt) + uk - 1) / uk;
 }
 
-// Units of one KV head of a sequence.
+// Units of one KV head of a sequence; whole warps call (lanes share the tiles of a long chain).
 template <class S>
 __device__ __forceinline__ int64_t attn_head_units(const AttnParams &p, int len, int n)
 {
     if (n == 0) return 0;
     const int tiles = attn_tiles<S>(p, n);
-    if (p.parent) return (int64_t)(tiles - 1) * attn_units<S>(p, len, n, 0) + attn_units<S>(p, len, n, tiles - 1);
+    if (p.parent || tiles == 1)
+        return (int64_t)(tiles - 1) * attn_units<S>(p, len, n, 0) + attn_units<S>(p, len, n, tiles - 1);
     int64_t u = 0;
-    for (int mt = 0; mt < tiles; ++mt) u += attn_units<S>(p, len, n, mt);
+    for (int mt = threadIdx.x & 31; mt < tiles; mt += 32) u += attn_units<S>(p, len, n, mt);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
     return u;
 }
 
@@ -116,8 +126,11 @@ __device__ AttnRange attn_split(const AttnParams &p)
     __shared__ int64_t s_at;
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int chunk = (p.B + kThreads - 1) / kThreads;
-    const int lo = min(tid * chunk, p.B), hi = min(lo + chunk, p.B);
+    // sequences go to threads in contiguous chunks; where a sequence has many tiles, to warps
+    const bool by_warp = !p.parent && (int64_t)p.N * p.group > S::M;
+    const int who = by_warp ? warp : tid, of = by_warp ? kThreads / 32 : kThreads;
+    const int chunk = (p.B + of - 1) / of;
+    const int lo = min(who * chunk, p.B), hi = min(lo + chunk, p.B);
     int64_t sum = 0;
     for (int b = lo; b < hi; ++b) {
         int len, st;
@@ -125,6 +138,8 @@ __device__ AttnRange attn_split(const AttnParams &p)
         sum += attn_head_units<S>(p, len, n) * p.kv.kv_heads;
         if (n == 0 && p.status && blockIdx.x == 0) p.status[b] = st;
     }
+    const int64_t chunk_sum = sum;
+    if (by_warp && lane) sum = 0;
     int64_t inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -144,7 +159,8 @@ __device__ AttnRange attn_split(const AttnParams &p)
     r.begin = min(r.per * blockIdx.x, total);
     r.end = min(r.begin + r.per, total);
     int64_t at = before + inc - sum;
-    if (r.begin < r.end && at <= r.begin && r.begin < at + sum) {
+    if (by_warp) at = __shfl_sync(0xffffffffu, at, 0);
+    if (r.begin < r.end && at <= r.begin && r.begin < at + chunk_sum) {
         for (int b = lo; b < hi; ++b) {
             int len, st;
             const int n = attn_nodes(p, b, &len, &st);
@@ -168,7 +184,7 @@ struct AttnSegment {
     int64_t item;            // first unit of the item in the whole batch
 };
 
-// Decodes the segment that begins at unit u (block-uniform); moves r.b / r.at on as sequences end.
+// Decodes the segment that begins at unit u (whole warps, uniform); moves r.b / r.at on as sequences end.
 template <class S>
 __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRange &r, int64_t u)
 {
@@ -196,10 +212,31 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRan
         s.item += (int64_t)s.tile * s.units;
         if (s.tile == last) s.units = attn_units<S>(p, s.len, s.n, last);
     } else {
-        while (rest >= s.units) {
-            rest -= s.units;
-            s.item += s.units;
-            s.units = attn_units<S>(p, s.len, s.n, ++s.tile);
+        // lanes look at 32 tiles at a time for the one that holds unit `rest`
+        const int tiles = attn_tiles<S>(p, s.n), lane = threadIdx.x & 31;
+        if (tiles > 1) {
+            for (int mt0 = 0;; mt0 += 32) {
+                const int64_t mine = mt0 + lane < tiles ? attn_units<S>(p, s.len, s.n, mt0 + lane) : 0;
+                int64_t inc = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
+                    if (lane >= o) inc += t;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, rest < inc);
+                if (hit || mt0 + 32 >= tiles) {
+                    const int l = hit ? __ffs((int)hit) - 1 : 0;
+                    s.tile = mt0 + l;
+                    s.units = (int)__shfl_sync(0xffffffffu, mine, l);
+                    const int64_t skip = __shfl_sync(0xffffffffu, inc - mine, l);
+                    rest -= skip;
+                    s.item += skip;
+                    break;
+                }
+                const int64_t all = __shfl_sync(0xffffffffu, inc, 31);
+                rest -= all;
+                s.item += all;
+            }
         }
     }
     s.keys = attn_keys<S>(p, s.len, s.n, s.tile);
@@ -239,52 +276,51 @@ constexpr int kAttnSms = 148;                   // SM count that the grids are s
 constexpr size_t kAttnCounterBytes = 4096;      // one counter per block, at the head of the workspace
 
 // Kernel for many query rows per KV head (mars_attention_tile.cu).
-constexpr int kTileMaxTree = 512;               // its mask store holds trees of up to this many nodes
+constexpr int kTileMaxTree = 128;               // its mask store holds trees of up to this many nodes
 size_t attn_tile_partial_bytes(int d);
 mars_status_t attn_tile_launch(const AttnParams &p, int d, int dt, cudaStream_t st);
 
 // Ancestor-or-self masks of the nodes that a tile's rows belong to, and which of them are computed.
-//   mask   [nodes of the tile][words]  bit m of node i: m is i or an ancestor of i (trees only)
+//   mask   [nodes of the tile][words]  bit m of node i: m is i or an ancestor of i
 //   live   [nodes of the tile]         1: node takes part; absent nodes (no way to the root) do not
-// Every thread of the block calls; par is scratch for N ints.  Returns MARS_SEQ_BAD_TREE if the
-// parents are no tree (then only the root is live).
+// Trees only; the nthr threads that share `sync` call.  par is scratch for n ints, *s_bad one int.
+// Returns MARS_SEQ_BAD_TREE if the parents are no tree (then only the root is live).
+template <class Sync>
 __device__ __forceinline__ int attn_tree_masks(const AttnParams &p, int b, int n, int first, int nodes, int *par,
-                                               uint32_t *mask, int words, unsigned char *live)
+                                               uint32_t *mask, int words, unsigned char *live, int *s_bad, int tid,
+                                               int nthr, Sync sync)
 {
-    const int tid = threadIdx.x, nthr = blockDim.x;
-    int bad = 0;
-    if (p.parent) {
-        const int32_t *g = p.shared_parent ? p.parent : p.parent + (int64_t)b * p.N;
-        for (int i = tid; i < n; i += nthr) {
-            const int x = g[i];
-            if (i == 0 ? x != -1 : (x >= i || x < -1)) bad = 1;
-            par[i] = x;
-        }
+    const int32_t *g = p.shared_parent ? p.parent : p.parent + (int64_t)b * p.N;
+    if (tid == 0) *s_bad = 0;
+    sync();
+    for (int i = tid; i < n; i += nthr) {
+        const int x = g[i];
+        if (i == 0 ? x != -1 : (x >= i || x < -1)) *s_bad = 1;
+        par[i] = x;
     }
-    bad = __syncthreads_or(bad);
+    sync();
+    const bool bad = *s_bad != 0;
     for (int i = tid; i < nodes; i += nthr) {
         const int node = first + i;
         bool ok = node < n;
-        if (p.parent) {
-            uint32_t *m = mask + i * words;
-            for (int w = 0; w < words; ++w) m[w] = 0u;
-            if (bad) {
-                ok = node == 0;
-                if (ok) m[0] = 1u;
-            } else if (ok) {
-                int x = node;
-                for (;;) {                      // parents fall strictly: at most n steps
-                    m[x >> 5] |= 1u << (x & 31);
-                    if (x <= 0) break;
-                    const int up = par[x];
-                    if (up < 0) { ok = false; break; }
-                    x = up;
-                }
+        uint32_t *m = mask + i * words;
+        for (int w = 0; w < words; ++w) m[w] = 0u;
+        if (bad) {
+            ok = node == 0;
+            if (ok) m[0] = 1u;
+        } else if (ok) {
+            int x = node;
+            for (;;) {                      // parents fall strictly: at most n steps
+                m[x >> 5] |= 1u << (x & 31);
+                if (x <= 0) break;
+                const int up = par[x];
+                if (up < 0) { ok = false; break; }
+                x = up;
             }
         }
         live[i] = ok;
     }
-    __syncthreads();
+    sync();
     return bad ? MARS_SEQ_BAD_TREE : MARS_SEQ_OK;
 }
 
