@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
     __shared__ unsigned char s_live[kRowsM];
     __shared__ float s_m[kRowsWarps][kRowsM], s_l[kRowsWarps][kRowsM];
     __shared__ int s_last;
+    __shared__ AttnSeqs s_seqs;
     constexpr int kBlk = kv_block_bytes(D);
     constexpr int kChunks = kBlk / 16;
     constexpr int kCode = D / 4;              // elements of d per lane of a quad
@@ -81,9 +82,9 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
     unsigned char *ring = s_ring + warp * kRowsStages * kBlk;
     const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
 
-    AttnRange r = attn_split<RowsShape, kRowsThreads>(p);
+    AttnRange r = attn_split<RowsShape, kRowsThreads>(p, &s_seqs);
     for (int64_t u = r.begin; u < r.end;) {
-        const AttnSegment sg = attn_segment<RowsShape>(p, r, u);
+        const AttnSegment sg = attn_segment<RowsShape>(p, &s_seqs, r, u);
         const bool whole = sg.unit0 == 0 && sg.unit1 == sg.units;
         const int rows = min(kRowsM, sg.n * p.group - sg.tile * kRowsM);
         const int row0 = sg.tile * kRowsM;               // first row of the tile: node row0/group

@@ -26,9 +26,8 @@ struct RowsShape {
     static __host__ __device__ constexpr int unit_keys(int) { return 64; }
 };
 struct TileShape {
-    static constexpr int M = 256;
-    // tiles of up to 128 rows fill one of the kernel's two accumulators, which then share the keys
-    static __host__ __device__ constexpr int unit_keys(int rows) { return rows > 128 ? 128 : 256; }
+    static constexpr int M = 128;
+    static __host__ __device__ constexpr int unit_keys(int) { return 128; }
 };
 
 struct AttnParams {
@@ -59,12 +58,12 @@ __device__ __forceinline__ float ex2(float x)
 // Nodes of sequence b that take part, and whether its pages hold them; len < 0 counts as no room.
 __device__ __forceinline__ int attn_nodes(const AttnParams &p, int b, int *len, int *status)
 {
-    const int n = p.count ? min(max(p.count[b], 0), p.N) : p.N;
-    *len = p.kv.seq_len[b];
-    *status = MARS_SEQ_OK;
-    if (n == 0) return 0;
-    if (*len < 0 || (int64_t)*len + n > kv_capacity(p.kv, b)) { *status = MARS_SEQ_NO_ROOM; return 0; }
-    return n;
+    const int count = p.count ? p.count[b] : p.N, l = p.kv.seq_len[b], cap = kv_capacity(p.kv, b);
+    const int n = min(max(count, 0), p.N);
+    const bool room = n == 0 || (l >= 0 && (int64_t)l + n <= cap);
+    *len = l;
+    *status = room ? MARS_SEQ_OK : MARS_SEQ_NO_ROOM;
+    return room ? n : 0;
 }
 
 // Node of a query row (rows of a KV head are node-major): row / group.
@@ -110,17 +109,24 @@ __device__ __forceinline__ int64_t attn_head_units(const AttnParams &p, int len,
     return u;
 }
 
+// What the block's first sequences come to, in shared memory: segments are decoded from here.
+constexpr int kSeqCache = 32;
+struct AttnSeqs {
+    int64_t units[kSeqCache];     // per KV head
+    int len[kSeqCache], n[kSeqCache];
+};
+
 struct AttnRange {
     int64_t begin, end;     // this block's units
     int64_t per;            // units per block
     int64_t at;             // first unit of sequence b
-    int b;                  // sequence of unit `begin`
+    int b, b0;              // sequence of the unit reached, of unit `begin`
 };
 
 // The block's share of the batch (all threads call; kThreads = blockDim.x).  Block 0 also reports the
 // status of sequences that have no work.
 template <class S, int kThreads>
-__device__ AttnRange attn_split(const AttnParams &p)
+__device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
 {
     __shared__ int64_t s_sum[kThreads / 32 + 1];
     __shared__ int64_t s_at;
@@ -172,6 +178,17 @@ __device__ AttnRange attn_split(const AttnParams &p)
     __syncthreads();
     r.b = s_b;
     r.at = s_at;
+    r.b0 = s_b;
+    if (r.begin < r.end) {
+        // whole warps where lanes share a sequence's tiles, else a lane per sequence
+        for (int i = by_warp ? warp : tid; i < kSeqCache && r.b0 + i < p.B; i += by_warp ? kThreads / 32 : kThreads) {
+            int len, st;
+            const int n = attn_nodes(p, r.b0 + i, &len, &st);
+            const int64_t u = attn_head_units<S>(p, len, n);
+            seqs->units[i] = u; seqs->len[i] = len; seqs->n[i] = n;
+        }
+    }
+    __syncthreads();
     return r;
 }
 
@@ -186,14 +203,19 @@ struct AttnSegment {
 
 // Decodes the segment that begins at unit u (whole warps, uniform); moves r.b / r.at on as sequences end.
 template <class S>
-__device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, AttnRange &r, int64_t u)
+__device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, const AttnSeqs *seqs, AttnRange &r, int64_t u)
 {
     AttnSegment s;
     int st;
     int64_t hu;
     for (;;) {
-        s.n = attn_nodes(p, r.b, &s.len, &st);
-        hu = attn_head_units<S>(p, s.len, s.n);
+        const int i = r.b - r.b0;
+        if (i < kSeqCache) {
+            s.n = seqs->n[i]; s.len = seqs->len[i]; hu = seqs->units[i];
+        } else {
+            s.n = attn_nodes(p, r.b, &s.len, &st);
+            hu = attn_head_units<S>(p, s.len, s.n);
+        }
         if (u < r.at + hu * p.kv.kv_heads) break;
         r.at += hu * p.kv.kv_heads;
         ++r.b;
@@ -280,9 +302,9 @@ constexpr int kTileMaxTree = 128;               // its mask store holds trees of
 size_t attn_tile_partial_bytes(int d);
 mars_status_t attn_tile_launch(const AttnParams &p, int d, int dt, cudaStream_t st);
 
-// Ancestor-or-self masks of the nodes that a tile's rows belong to, and which of them are computed.
-//   mask   [nodes of the tile][words]  bit m of node i: m is i or an ancestor of i
-//   live   [nodes of the tile]         1: node takes part; absent nodes (no way to the root) do not
+// Ancestor-or-self masks of nodes first .. first + nodes - 1, and which of them are computed.
+//   mask   [nodes][words]  bit m of node i: m is i or an ancestor of i
+//   live   [nodes]         1: node takes part; absent nodes (no way to the root) do not
 // Trees only; the nthr threads that share `sync` call.  par is scratch for n ints, *s_bad one int.
 // Returns MARS_SEQ_BAD_TREE if the parents are no tree (then only the root is live).
 template <class Sync>
