@@ -7,16 +7,21 @@
 // bits down to 2^-14 of the row's largest and an error below 2^-25 of it beyond.  The heads' fp32
 // scales are factored out of both sums.
 //
-// Kernel for few query rows per KV head (`attn_rows_kernel`, tiles of 16 rows): bound by reading the
-// cache.  The page bytes go through a small shared-memory ring straight into the register fragments of
-// mma.sync -- no unpacked copy of K or V exists anywhere:
-//   S (16 rows x 8 keys) += Q (16 x 16) K^T (16 x 8): a lane's B fragment is 4 consecutive values of
-//     one key; since the order of the d sum is free, lane t of a quad takes d = t*d/4 .. of its key,
-//     one aligned vector of codes and its own scale bytes.
-//   O (16 x 8) += P (16 x 16) V (16 x 8): the fragment needs pairs of KEYS at one d.  Codes of two
-//     keys are interleaved nibble by nibble (two logic operations for 8 values each) before the
-//     conversion, so the conversion itself delivers (key, key') pairs.  Output column g of n-tile j is
-//     d = g*d/8 + j: the lane's codes are one vector, all of one scale.
+// Kernel for few query rows per KV head (`attn_rows_kernel`, tiles of 8, 16 or 32 rows): bound by
+// reading the cache.  The page bytes go through a small shared-memory ring straight into the register
+// fragments of mma.sync -- no unpacked copy of K or V exists anywhere.  Keys and values are the 16-row
+// operand, the query rows the 8-column one, so a token of four heads to a KV head wastes half of a
+// tile, not three quarters, and every unpacked fragment serves all query rows of the tile:
+//   S^T (16 keys x 8 rows) += K (16 x 16) Q^T (16 x 8): a lane's K fragment is 4 consecutive values of
+//     two keys; since the order of the d sum is free, lane t of a quad takes d = t*d/4 .. of its keys,
+//     one aligned vector of codes and its own scale bytes each.
+//   O^T (16 d x 8 rows) += V^T (16 x 16 keys) P^T (16 x 8): P^T is S^T's fragment transposed by
+//     movmatrix; the V fragment needs pairs of KEYS at one d.  Codes of two keys are interleaved nibble
+//     by nibble (two logic operations for 8 values each) before the conversion, so the conversion itself
+//     delivers (key, key') pairs.  Row g of m-tile j is d = g*d/8 + 2j (g + 8: the next): the lane's codes
+//     are one vector, all of one scale.
+// The running maximum needs no reduction per block: a vote finds whether any score exceeds the row's
+// reference by 2^8; only then (rarely after the first blocks) is it recomputed and O rescaled.
 #include "mars_attention.cuh"
 #include "mars_hooks.cuh"
 
@@ -26,13 +31,13 @@
 
 namespace mars {
 
-constexpr int kRowsM = RowsShape::M;  // query rows per tile
-constexpr int kUnit = RowsShape::unit_keys(kRowsM);
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = 32 * kRowsWarps;
 constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
-constexpr int kRowsOcc = 3;           // blocks per SM
-constexpr int kRowsGrid = kAttnSms * kRowsOcc;
+constexpr int kRowsMax = 32;          // largest tile
+constexpr int rows_occ(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }   // blocks per SM (registers)
+constexpr int rows_grid(int rows) { return kAttnSms * rows_occ(rows); }
+constexpr int kUnit = 64;             // RowsShape::unit_keys
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
@@ -49,98 +54,57 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D>
-__host__ __device__ constexpr int rows_slot_floats() { return kRowsM * (D + 2); }
-
-template <int D>
-constexpr size_t rows_smem_bytes()
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
 {
-    return (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D) > (size_t)kRowsWarps * kRowsM * (D + 4) * 4
-               ? (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D)
-               : (size_t)kRowsWarps * kRowsM * (D + 4) * 4;
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+    return r;
 }
 
-template <int D, int DT>
-__global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const AttnParams p)
+template <int D>
+__host__ __device__ constexpr int rows_slot_floats(int rows) { return rows * (D + 2); }
+
+template <int D>
+constexpr size_t rows_smem_bytes(int rows)
+{
+    const size_t ring = (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D), sums = (size_t)kRowsWarps * rows * (D + 4) * 4;
+    return (rows == kRowsMax ? (size_t)rows * D * 2 : 0) + (ring > sums ? ring : sums);
+}
+
+template <int D, int DT, int kRows>
+__global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kernel(const AttnParams p)
 {
     pdl_launch_dependents();
     pdl_wait();
-    extern __shared__ __align__(16) unsigned char s_ring[];
+    using Shape = RowsShape<kRows>;
+    constexpr int kNT = kRows / 8;            // n-tiles of query rows
+    constexpr bool kQShared = kRows == kRowsMax;   // Q fragments in shared memory (64 registers less)
+    extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_par[MARS_MAX_NODES];
-    __shared__ uint32_t s_mask[kRowsM * (MARS_MAX_NODES / 32)];
-    __shared__ unsigned char s_live[kRowsM];
-    __shared__ float s_m[kRowsWarps][kRowsM], s_l[kRowsWarps][kRowsM];
+    __shared__ uint32_t s_mask[kRows * (MARS_MAX_NODES / 32)];
+    __shared__ unsigned char s_live[kRows];
+    __shared__ float s_m[kRowsWarps][kRows], s_l[kRowsWarps][kRows];
     __shared__ int s_last;
     __shared__ AttnSeqs s_seqs;
     constexpr int kBlk = kv_block_bytes(D);
     constexpr int kChunks = kBlk / 16;
     constexpr int kCode = D / 4;              // elements of d per lane of a quad
-    constexpr int kTiles = D / 8;             // n-tiles of the output
+    constexpr int kSteps = D / 16;            // k-steps of S = m-tiles of O
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;
+    uint2 *s_q = reinterpret_cast<uint2 *>(s_dyn);                        // [k-step][n-tile][lane]
+    unsigned char *s_ring = s_dyn + (kQShared ? kRows * D * 2 : 0);
     unsigned char *ring = s_ring + warp * kRowsStages * kBlk;
     const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
 
-    AttnRange r = attn_split<RowsShape, kRowsThreads>(p, &s_seqs);
+    AttnRange r = attn_split<Shape, kRowsThreads>(p, &s_seqs);
     for (int64_t u = r.begin; u < r.end;) {
-        const AttnSegment sg = attn_segment<RowsShape>(p, &s_seqs, r, u);
+        const AttnSegment sg = attn_segment<Shape>(p, &s_seqs, r, u);
         const bool whole = sg.unit0 == 0 && sg.unit1 == sg.units;
-        const int rows = min(kRowsM, sg.n * p.group - sg.tile * kRowsM);
-        const int row0 = sg.tile * kRowsM;               // first row of the tile: node row0/group
+        const int rows = min(kRows, sg.n * p.group - sg.tile * kRows);
+        const int row0 = sg.tile * kRows;                // first row of the tile: node row0/group
         const int node0 = attn_node(p, row0);
-        const int nodes = attn_node(p, row0 + rows - 1) - node0 + 1;
-        const int words = (sg.n + 31) >> 5;
-        const int st = p.parent ? attn_tree_masks(p, sg.b, sg.n, node0, nodes, s_par, s_mask, words, s_live, &s_last, tid,
-                                                  kRowsThreads, [] { __syncthreads(); })
-                                : MARS_SEQ_OK;
-        if (tid == 0 && p.status && sg.head == 0 && sg.tile == 0 && sg.unit0 == 0) p.status[sg.b] = st;
-
-        // ---- Q fragments: rows g and g + 8, d = t*kCode + 4*s .. of k-step s
-        uint32_t qa[D / 16][4];
-        float rs[2];                                     // score scale of the two rows, in log2 units
-        int node[2];                                     // tile-local node of the row, -1 behind the rows
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int row = row0 + g + 8 * half;
-            const bool in = g + 8 * half < rows;
-            const int nd = attn_node(p, row);
-            node[half] = in ? nd - node0 : -1;
-            uint4 w[kCode / 8];
-            float m = 0.0f;
-            if (in) {
-                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.q_row +
-                                   (int64_t)(sg.head * p.group + row - nd * p.group) * p.q_head + t * kCode;
-#pragma unroll
-                for (int i = 0; i < kCode / 8; ++i) {
-                    w[i] = reinterpret_cast<const uint4 *>(p.q + at * 2)[i];
-                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = widen2<DT>(x[j]);
-                        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kCode / 8; ++i) w[i] = make_uint4(0u, 0u, 0u, 0u);
-            }
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            float down, up;
-            row_scale(m, &down, &up);
-            rs[half] = p.scale_log2 * p.scales[sg.head] * up;
-#pragma unroll
-            for (int i = 0; i < kCode / 8; ++i) {
-                const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = widen2<DT>(x[j]);
-                    // word 4*i + j holds d = t*kCode + 8*i + 2*j, +1: k-step 2*i + j/2, register j&1
-                    qa[2 * i + (j >> 1)][half + 2 * (j & 1)] = f16x2_from(f.x * down, f.y * down);
-                }
-            }
-        }
 
         // ---- this warp's 16-key blocks of the segment
         const int first = sg.unit0 * (kUnit / 16) + warp;
@@ -159,11 +123,11 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
                 if (i >= ids_at + 32) fetch_ids(i);
                 const int id = __shfl_sync(0xffffffffu, ids, i - ids_at);
                 if (id >= 0) {
-                    const unsigned char *src = kv_block<D>(p.kv, p.layer, id, sg.head, (first + i * kRowsWarps) * 16);
-                    const uint32_t dst = ring_u32 + (i % kRowsStages) * kBlk;
+                    const unsigned char *src = kv_block<D>(p.kv, p.layer, id, sg.head, (first + i * kRowsWarps) * 16) + lane * 16;
+                    const uint32_t dst = ring_u32 + (i % kRowsStages) * kBlk + lane * 16;
 #pragma unroll
                     for (int c = 0; c < (kChunks + 31) / 32; ++c)
-                        if (c * 32 + lane < kChunks) cp_async16(dst + (c * 32 + lane) * 16, src + (c * 32 + lane) * 16);
+                        if (c * 32 + lane < kChunks) cp_async16(dst + c * 512, src + c * 512);
                 } else {
                     poisoned = true;                     // no such page: the rows become NaN
                 }
@@ -173,98 +137,132 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
 #pragma unroll
         for (int i = 0; i < kRowsStages - 1; ++i) issue(i);
 
-        float o[kTiles][4];
+        const int nodes = attn_node(p, row0 + rows - 1) - node0 + 1;
+        const int words = (sg.n + 31) >> 5;
+        const int st = p.parent ? attn_tree_masks(p, sg.b, sg.n, node0, nodes, s_par, s_mask, words, s_live, &s_last, tid,
+                                                  kRowsThreads, [] { __syncthreads(); })
+                                : MARS_SEQ_OK;
+        if (tid == 0 && p.status && sg.head == 0 && sg.tile == 0 && sg.unit0 == 0) p.status[sg.b] = st;
+
+        // ---- Q^T fragments: row 8n + g, d = t*kCode + 4*s .. of k-step s
+        uint2 q[kQShared ? 1 : kSteps][kQShared ? 1 : kNT];
+        float rs[kNT][2];                                // score scale of rows 8n + 2t, + 1 in log2 units
+        int node[kNT][2];                                // tile-local node of those rows, -1 behind the rows
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j)
+        for (int n = 0; n < kNT; ++n) {
+            const int row = row0 + 8 * n + g;
+            const bool in = 8 * n + g < rows;
+            const int nd = attn_node(p, row);
+            uint4 w[kCode / 8];
+            float m = 0.0f;
+            if (in) {
+                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.q_row + (int64_t)(sg.head * p.group + row - nd * p.group) * p.q_head + t * kCode;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[j][k] = 0.0f;
-        float mref[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+                for (int i = 0; i < kCode / 8; ++i) {
+                    w[i] = reinterpret_cast<const uint4 *>(p.q + at * 2)[i];
+                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 f = widen2<DT>(x[j]);
+                        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kCode / 8; ++i) w[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            float down, up;
+            row_scale(m, &down, &up);
+            const float scale = p.scale_log2 * p.scales[sg.head] * up;
+            const int local = in ? nd - node0 : -1;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                rs[n][e] = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + e));
+                node[n][e] = __shfl_sync(0xffffffffu, local, 4 * (2 * t + e));
+            }
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {           // words 2s, 2s + 1 of this lane's values
+                const uint4 v = w[s >> 1];
+                const float2 a = widen2<DT>(s & 1 ? v.z : v.x), b = widen2<DT>(s & 1 ? v.w : v.y);
+                const uint2 f = make_uint2(f16x2_from(a.x * down, a.y * down), f16x2_from(b.x * down, b.y * down));
+                if constexpr (kQShared) {
+                    if (warp == 0) s_q[(s * kNT + n) * 32 + lane] = f;
+                } else {
+                    q[s][n] = f;
+                }
+            }
+        }
+        if constexpr (kQShared) __syncthreads();
+
+        float o[kSteps][kNT][4];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[j][n][k] = 0.0f;
+        float mref[kNT][2], l[kNT][2];
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) { mref[n][0] = mref[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.0f; }
+        // rows and columns of the 16-key tile are permuted inside pairs so that neither the K rows nor the
+        // V rows that a quarter warp reads together fall on the same banks
+        const int key = (g & 6) + ((g ^ (g >> 1)) & 1);
+        const int k0 = 2 * t + (t & 1), k1 = 2 * t + ((t & 1) ^ 1);
 
         for (int i = 0; i < mine; ++i) {
             cp_async_wait<kRowsStages - 2>();
             __syncwarp();
             const unsigned char *blk = ring + (i % kRowsStages) * kBlk;
             const int pos0 = (first + i * kRowsWarps) * 16;
-            // ---- S = Q K^T for 16 keys: n-tile w, column c is key 8w + 2*(c/2) + ((c&1) ^ (c/2 & 1))
-            float s[2][4];
+            // ---- S^T = K Q^T for 16 keys
+            float s[kNT][4];
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[n][k] = 0.0f;
+            uint32_t code[2][kCode / 8], scale[2][2];
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[w][k] = 0.0f;
-                const int key = 8 * w + (g & 6) + ((g ^ (g >> 1)) & 1);
-                uint32_t code[kCode / 8], sc2;
+                uint32_t sc2;
                 if constexpr (D == 128) {
-                    const uint4 c = *reinterpret_cast<const uint4 *>(blk + key * 64 + t * 16);
-                    code[0] = c.x; code[1] = c.y; code[2] = c.z; code[3] = c.w;
-                    sc2 = *reinterpret_cast<const unsigned short *>(blk + 16 * D + key * 8 + t * 2);
+                    const uint4 c = *reinterpret_cast<const uint4 *>(blk + (8 * w + key) * 64 + t * 16);
+                    code[w][0] = c.x; code[w][1] = c.y; code[w][2] = c.z; code[w][3] = c.w;
+                    sc2 = *reinterpret_cast<const unsigned short *>(blk + 16 * D + (8 * w + key) * 8 + t * 2);
                 } else {
-                    const uint2 c = *reinterpret_cast<const uint2 *>(blk + key * 32 + t * 8);
-                    code[0] = c.x; code[1] = c.y;
-                    sc2 = blk[16 * D + key * 4 + t];
+                    const uint2 c = *reinterpret_cast<const uint2 *>(blk + (8 * w + key) * 32 + t * 8);
+                    code[w][0] = c.x; code[w][1] = c.y;
+                    sc2 = blk[16 * D + (8 * w + key) * 4 + t];
                 }
                 const uint32_t sh = e4m3x2_to_f16x2(sc2);
-                const uint32_t scale[2] = {__byte_perm(sh, sh, 0x1010), __byte_perm(sh, sh, 0x3232)};
-#pragma unroll
-                for (int v = 0; v < kCode / 8; ++v) {
-                    uint32_t h[4];
-                    e2m1x8_to_f16x2(code[v], h);
-                    const uint32_t f = scale[v >> 1];
-                    mma_f16(s[w], qa[2 * v], hmul2(h[0], f), hmul2(h[1], f));
-                    mma_f16(s[w], qa[2 * v + 1], hmul2(h[2], f), hmul2(h[3], f));
-                }
+                scale[w][0] = __byte_perm(sh, sh, 0x1010);
+                scale[w][1] = __byte_perm(sh, sh, 0x3232);
             }
-            // ---- scores in log2 units; behind the committed tokens only ancestors count
-            const bool edge = pos0 + 16 > sg.len;
 #pragma unroll
-            for (int w = 0; w < 2; ++w)
+            for (int v = 0; v < kCode / 8; ++v) {
+                uint32_t h[2][4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float x = s[w][k] * rs[k >> 1];
-                    if (edge) {
-                        const int m = pos0 + 8 * w + 2 * t + ((k ^ t) & 1) - sg.len;    // draft node of the key
-                        bool see = m < 0;
-                        if (m >= 0 && pos0 + 8 * w + 2 * t + ((k ^ t) & 1) < sg.keys && node[k >> 1] >= 0)
-                            see = p.parent ? (s_mask[node[k >> 1] * words + (m >> 5)] >> (m & 31)) & 1u
-                                           : m <= node0 + node[k >> 1];
-                        if (!see) x = -INFINITY;
+                for (int w = 0; w < 2; ++w) {
+                    e2m1x8_to_f16x2(code[w][v], h[w]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) h[w][k] = hmul2(h[w][k], scale[w][v >> 1]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t a[4] = {h[0][2 * e], h[1][2 * e], h[0][2 * e + 1], h[1][2 * e + 1]};
+#pragma unroll
+                    for (int n = 0; n < kNT; ++n) {
+                        uint2 b;
+                        if constexpr (kQShared) b = s_q[((2 * v + e) * kNT + n) * 32 + lane];
+                        else b = q[2 * v + e][n];
+                        mma_f16(s[n], a, b.x, b.y);
                     }
-                    s[w][k] = x;
-                }
-            // ---- running maximum, moved only when it grows by more than 2^8
-            float mx[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-                mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-                mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-            }
-            if (__any_sync(0xffffffffu, mx[0] > mref[0] + 8.0f || mx[1] > mref[1] + 8.0f)) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float to = fmaxf(mref[h], mx[h]);
-                    const float f = to == -INFINITY ? 1.0f : ex2(mref[h] - to);
-                    mref[h] = to;
-                    l[h] *= f;
-#pragma unroll
-                    for (int j = 0; j < kTiles; ++j) { o[j][2 * h] *= f; o[j][2 * h + 1] *= f; }
                 }
             }
-            // P = 2^(s - mref + 7) <= 2^15: with the row's largest at 2^7 or more, fp16 keeps 11 bits of
-            // every probability above 2^-21 of it and an error of 2^-32 of it below
-            const float base[2] = {mref[0] == -INFINITY ? 0.0f : mref[0] - 7.0f,
-                                   mref[1] == -INFINITY ? 0.0f : mref[1] - 7.0f};
-            uint32_t pa[4];
-#pragma unroll
-            for (int w = 0; w < 2; ++w)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(s[w][2 * h] - base[h]), p1 = ex2(s[w][2 * h + 1] - base[h]);
-                    l[h] += p0 + p1;
-                    pa[2 * w + h] = f16x2_from(p0, p1);
-                }
-            // ---- O += P V: this lane's keys are k0, k1 (n-tile 0) and k0 + 8, k1 + 8 (n-tile 1)
-            const int k0 = 2 * t + (t & 1), k1 = 2 * t + ((t & 1) ^ 1);
-            uint32_t vs[2], vc[4][kTiles / 8];
+            // ---- V's codes and scales early: their latency hides behind the scores
+            uint32_t vs[2], vc[4][kSteps / 4];
+            const bool edge = pos0 + 16 > sg.len;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const unsigned char *sp = blk + 17 * D;
@@ -286,8 +284,61 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
                     }
                 }
             }
+            // ---- scores in log2 units (element k: key g or g + 8, row 2t + (k & 1)); behind the committed
+            // tokens only ancestors count
+            bool grow = false;
 #pragma unroll
-            for (int v = 0; v < kTiles / 8; ++v) {
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float x = s[n][k] * rs[n][k & 1];
+                    if (edge) {
+                        const int pos = pos0 + 8 * (k >> 1) + key, m = pos - sg.len, nd = node[n][k & 1];
+                        bool see = m < 0;
+                        if (m >= 0 && pos < sg.keys && nd >= 0)
+                            see = p.parent ? (s_mask[nd * words + (m >> 5)] >> (m & 31)) & 1u : m <= node0 + nd;
+                        if (!see) x = -INFINITY;
+                    }
+                    s[n][k] = x;
+                    grow |= x > mref[n][k & 1] + 8.0f;
+                }
+            // ---- the reference maximum moves only when a score exceeds it by more than 2^8
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(s[n][e], s[n][2 + e]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+                        if (mx > mref[n][e] + 8.0f) {
+                            const float f = ex2(mref[n][e] - mx);
+                            mref[n][e] = mx;
+                            l[n][e] *= f;
+#pragma unroll
+                            for (int j = 0; j < kSteps; ++j) { o[j][n][e] *= f; o[j][n][2 + e] *= f; }
+                        }
+                    }
+            }
+            // P = 2^(s - mref + 7) <= 2^15: with the row's largest at 2^7 or more, fp16 keeps 11 bits of
+            // every probability above 2^-21 of it and an error of 2^-32 of it below
+            uint32_t pb[kNT][2];
+#pragma unroll
+            for (int n = 0; n < kNT; ++n) {
+                float x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float ref = mref[n][k & 1];
+                    x[k] = ex2(s[n][k] - (ref == -INFINITY ? 0.0f : ref - 7.0f));
+                }
+                l[n][0] += x[0] + x[2];
+                l[n][1] += x[1] + x[3];
+                pb[n][0] = transpose8x8(f16x2_from(x[0], x[1]));
+                pb[n][1] = transpose8x8(f16x2_from(x[2], x[3]));
+            }
+            // ---- O^T += V^T P^T: this lane's keys are k0, k1 (first eight) and k0 + 8, k1 + 8
+#pragma unroll
+            for (int v = 0; v < kSteps / 4; ++v) {
                 uint32_t even[2][4], odd[2][4];
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
@@ -297,94 +348,108 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    mma_f16(o[8 * v + 2 * j], pa, hmul2(even[0][j], vs[0]), hmul2(even[1][j], vs[1]));
-                    mma_f16(o[8 * v + 2 * j + 1], pa, hmul2(odd[0][j], vs[0]), hmul2(odd[1][j], vs[1]));
+                    const uint32_t a[4] = {hmul2(even[0][j], vs[0]), hmul2(odd[0][j], vs[0]), hmul2(even[1][j], vs[1]),
+                                           hmul2(odd[1][j], vs[1])};
+#pragma unroll
+                    for (int n = 0; n < kNT; ++n) mma_f16(o[4 * v + j][n], a, pb[n][0], pb[n][1]);
                 }
             }
             __syncwarp();
             issue(i + kRowsStages - 1);
         }
         cp_async_wait<0>();
-        if (__any_sync(0xffffffffu, poisoned)) { l[0] = l[1] = NAN; if (mref[0] == -INFINITY) mref[0] = 0.0f; if (mref[1] == -INFINITY) mref[1] = 0.0f; }
+        if (__any_sync(0xffffffffu, poisoned)) {
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { l[n][e] = NAN; if (mref[n][e] == -INFINITY) mref[n][e] = 0.0f; }
+        }
 
         // ---- the four warps' sums, then the block's result
         __syncthreads();                                  // ring free
-        float *s_o = reinterpret_cast<float *>(s_ring);   // [warp][16][D + 4]
+        float *s_o = reinterpret_cast<float *>(s_ring);   // [warp][row][D + 4]
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            if (t == 0) { s_m[warp][g + 8 * h] = mref[h]; s_l[warp][g + 8 * h] = l[h]; }
-            float *to = s_o + (warp * kRowsM + g + 8 * h) * (D + 4) + 2 * t * kTiles;
+        for (int n = 0; n < kNT; ++n)
 #pragma unroll
-            for (int j = 0; j < kTiles; ++j) {
-                to[j] = o[j][2 * h];
-                to[kTiles + j] = o[j][2 * h + 1];
+            for (int e = 0; e < 2; ++e) {
+                float x = l[n][e];
+#pragma unroll
+                for (int k = 4; k < 32; k <<= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
+                const int row = 8 * n + 2 * t + e;
+                if (g == 0) { s_m[warp][row] = mref[n][e]; s_l[warp][row] = x; }
+                float *to = s_o + (warp * kRows + row) * (D + 4) + g * (D / 8);
+#pragma unroll
+                for (int j = 0; j < kSteps; j += 2)
+                    *reinterpret_cast<float4 *>(to + 2 * j) = make_float4(o[j][n][e], o[j][n][2 + e], o[j + 1][n][e], o[j + 1][n][2 + e]);
+            }
+        __syncthreads();
+        // each thread: kPer values of d of a row, kPass rows of the tile one after the other
+        constexpr int kPer = 8, kAcross = D / kPer, kAtOnce = kRowsThreads / kAcross;
+        bool write = whole;
+        const int c0 = (int)(sg.item / r.per), c1 = (int)((sg.item + sg.units - 1) / r.per);
+        auto slot_of = [&](int c) { return p.partial + (int64_t)(2 * c + (r.per * c >= sg.item ? 0 : 1)) * rows_slot_floats<D>(kRows); };
+        const int od = (tid % kAcross) * kPer;
+        auto emit = [&](int orow, float (&acc)[kPer], float sum) {
+            if (orow >= rows) return;
+            const int row = row0 + orow, nd = attn_node(p, row);
+            if (p.parent && !s_live[nd - node0]) return;
+            const float f = p.scales[p.kv.kv_heads + sg.head] / sum;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) acc[k] *= f;
+            const int64_t at = ((int64_t)sg.b * p.N + nd) * p.out_row + (int64_t)(sg.head * p.group + row - nd * p.group) * p.out_head + od;
+            store_out8<DT>(p.out, at, acc);
+        };
+        for (int orow = tid / kAcross; orow < rows; orow += kAtOnce) {
+            const float m = fmaxf(fmaxf(s_m[0][orow], s_m[1][orow]), fmaxf(s_m[2][orow], s_m[3][orow]));
+            float acc[kPer], sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kRowsWarps; ++w) {
+                const float f = s_m[w][orow] == -INFINITY ? 0.0f : ex2(s_m[w][orow] - m);
+                sum += s_l[w][orow] * f;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) acc[k] += s_o[(w * kRows + orow) * (D + 4) + od + k] * f;
+            }
+            if (whole) {
+                emit(orow, acc, sum);
+            } else {
+                // partial result: slot 0 of the block for the item its range begins with, 1 for the other
+                float *dst = p.partial + (int64_t)(2 * blockIdx.x + (u == r.begin ? 0 : 1)) * rows_slot_floats<D>(kRows);
+#pragma unroll
+                for (int k = 0; k < kPer; k += 4)
+                    *reinterpret_cast<float4 *>(dst + orow * D + od + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
+                if (od == 0) { dst[kRows * D + orow] = m; dst[kRows * D + kRows + orow] = sum; }
             }
         }
-        __syncthreads();
-        constexpr int kPer = D / 8;                       // output values per thread: row tid/8
-        const int orow = tid >> 3, od = (tid & 7) * kPer;
-        float m = fmaxf(fmaxf(s_m[0][orow], s_m[1][orow]), fmaxf(s_m[2][orow], s_m[3][orow]));
-        float acc[kPer], sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kRowsWarps; ++w) {
-            const float f = s_m[w][orow] == -INFINITY ? 0.0f : ex2(s_m[w][orow] - m);
-            sum += s_l[w][orow] * f;
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) acc[k] += s_o[(w * kRowsM + orow) * (D + 4) + od + k] * f;
-        }
-        bool write = whole;
         if (!whole) {
-            // partial result: slot 0 of the block for the item its range begins with, 1 for the other
-            const int slot = 2 * blockIdx.x + (u == r.begin ? 0 : 1);
-            float *dst = p.partial + (int64_t)slot * rows_slot_floats<D>();
-#pragma unroll
-            for (int k = 0; k < kPer; k += 4)
-                *reinterpret_cast<float4 *>(dst + orow * D + od + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
-            if ((tid & 7) == 0) { dst[kRowsM * D + orow] = m; dst[kRowsM * D + kRowsM + orow] = sum; }
-            const int c0 = (int)(sg.item / r.per), c1 = (int)((sg.item + sg.units - 1) / r.per);
             __threadfence();
             __syncthreads();
             if (tid == 0) s_last = atomicAdd(p.counters + c0, 1u) == (unsigned)(c1 - c0);
             __syncthreads();
-            if (s_last) {
+            write = s_last != 0;
+            if (write) {
                 __threadfence();
-                m = -INFINITY;
-                for (int c = c0; c <= c1; ++c) {
-                    const int sl = 2 * c + (r.per * c >= sg.item ? 0 : 1);
-                    m = fmaxf(m, __ldcg(p.partial + (int64_t)sl * rows_slot_floats<D>() + kRowsM * D + orow));
-                }
-                sum = 0.0f;
+                for (int orow = tid / kAcross; orow < rows; orow += kAtOnce) {
+                    float m = -INFINITY, sum = 0.0f, acc[kPer];
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
-                for (int c = c0; c <= c1; ++c) {
-                    const int sl = 2 * c + (r.per * c >= sg.item ? 0 : 1);
-                    const float *src = p.partial + (int64_t)sl * rows_slot_floats<D>();
-                    const float pm = __ldcg(src + kRowsM * D + orow);
-                    const float f = pm == -INFINITY ? 0.0f : ex2(pm - m);
-                    sum += __ldcg(src + kRowsM * D + kRowsM + orow) * f;
-#pragma unroll
-                    for (int k = 0; k < kPer; k += 4) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od + k));
-                        acc[k] += x.x * f; acc[k + 1] += x.y * f; acc[k + 2] += x.z * f; acc[k + 3] += x.w * f;
+                    for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) {
+                        const float *src = slot_of(c);
+                        const float pm = __ldcg(src + kRows * D + orow), pl = __ldcg(src + kRows * D + kRows + orow);
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od));
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od + 4));
+                        const float mm = fmaxf(m, pm);
+                        const float a = m == -INFINITY ? 0.0f : ex2(m - mm), b = pm == -INFINITY ? 0.0f : ex2(pm - mm);
+                        m = mm;
+                        sum = sum * a + pl * b;
+                        acc[0] = acc[0] * a + x.x * b; acc[1] = acc[1] * a + x.y * b; acc[2] = acc[2] * a + x.z * b; acc[3] = acc[3] * a + x.w * b;
+                        acc[4] = acc[4] * a + y.x * b; acc[5] = acc[5] * a + y.y * b; acc[6] = acc[6] * a + y.z * b; acc[7] = acc[7] * a + y.w * b;
                     }
+                    emit(orow, acc, sum);
                 }
                 if (tid == 0) p.counters[c0] = 0u;
-                write = true;
-            }
-        }
-        if (write && orow < rows) {
-            const int row = row0 + orow, nd = attn_node(p, row);
-            if (!p.parent || s_live[nd - node0]) {
-                const float f = p.scales[p.kv.kv_heads + sg.head] / sum;
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) acc[k] *= f;
-                const int64_t at = ((int64_t)sg.b * p.N + nd) * p.out_row + (int64_t)(sg.head * p.group + row - nd * p.group) * p.out_head + od;
-#pragma unroll
-                for (int k = 0; k < kPer; k += 8) store_out8<DT>(p.out, at + k, acc + k);
             }
         }
         __syncthreads();                                  // masks, ring and sums free for the next segment
@@ -392,16 +457,26 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsOcc) attn_rows_kernel(const
     }
 }
 
-template <int D, int DT>
+template <int D, int DT, int kRows>
 static mars_status_t rows_launch(const AttnParams &p, cudaStream_t st)
 {
-    const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, attn_rows_kernel<D, DT>, dim3(kRowsGrid), dim3(kRowsThreads),
-                                     rows_smem_bytes<D>(), st, p);
+    cudaError_t e = cudaSuccess;
+    if (rows_smem_bytes<D>(kRows) > 40 * 1024)
+        e = cudaFuncSetAttribute(attn_rows_kernel<D, DT, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<D>(kRows));
+    if (e == cudaSuccess)
+        e = launch_pdl(hook(kHookNoOverlap) == 0, attn_rows_kernel<D, DT, kRows>, dim3(rows_grid(kRows)), dim3(kRowsThreads),
+                       rows_smem_bytes<D>(kRows), st, p);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     return MARS_OK;
 }
 
-static_assert(kRowsGrid * sizeof(unsigned) <= kAttnCounterBytes, "one counter per block");
+template <int D, int DT>
+static mars_status_t rows_launch(const AttnParams &p, int rows, cudaStream_t st)
+{
+    return rows == 8 ? rows_launch<D, DT, 8>(p, st) : rows == 16 ? rows_launch<D, DT, 16>(p, st) : rows_launch<D, DT, 32>(p, st);
+}
+
+static_assert(rows_grid(8) * sizeof(unsigned) <= kAttnCounterBytes, "one counter per block");
 
 static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
 {
@@ -409,13 +484,15 @@ static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
            q_heads % kv_heads == 0 && (d == 64 || d == 128) && (int64_t)N * (q_heads / kv_heads) <= (1 << 30);
 }
 
-// The kernel for tiles of query rows takes over where a KV head has more of them than two tiles of the
-// other hold.
-static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > 2 * kRowsM && !(tree && N > kTileMaxTree); }
+// The kernel for tiles of query rows takes over where a KV head has more of them than the largest
+// tile of the other holds.
+static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > kRowsMax && !(tree && N > kTileMaxTree); }
+static int attn_rows(int N, int group) { return (int64_t)N * group <= 8 ? 8 : (int64_t)N * group <= 16 ? 16 : 32; }
 
 static size_t attn_workspace(int N, int group, int d)
 {
-    const size_t rows = sizeof(float) * 2 * kRowsGrid * (size_t)(d == 128 ? rows_slot_floats<128>() : rows_slot_floats<64>());
+    const int n = attn_rows(N, group);
+    const size_t rows = sizeof(float) * 2 * rows_grid(n) * (size_t)(d == 128 ? rows_slot_floats<128>(n) : rows_slot_floats<64>(n));
     const size_t tile = attn_use_tiles(N, group, false) ? attn_tile_partial_bytes(d) : 0;
     return kAttnCounterBytes + (rows > tile ? rows : tile);
 }
@@ -468,9 +545,10 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     p.counters = (unsigned *)workspace;
     p.partial = (float *)((unsigned char *)workspace + kAttnCounterBytes);
     if (attn_use_tiles(N, p.group, parent != nullptr)) return attn_tile_launch(p, cache->head_dim, dt, st);
+    const int rows = attn_rows(N, p.group);
     if (cache->head_dim == 128)
-        return dt == MARS_BF16 ? rows_launch<128, MARS_BF16>(p, st) : rows_launch<128, MARS_FP16>(p, st);
-    return dt == MARS_BF16 ? rows_launch<64, MARS_BF16>(p, st) : rows_launch<64, MARS_FP16>(p, st);
+        return dt == MARS_BF16 ? rows_launch<128, MARS_BF16>(p, rows, st) : rows_launch<128, MARS_FP16>(p, rows, st);
+    return dt == MARS_BF16 ? rows_launch<64, MARS_BF16>(p, rows, st) : rows_launch<64, MARS_FP16>(p, rows, st);
 }
 
 }  // extern "C"

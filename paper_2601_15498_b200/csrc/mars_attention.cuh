@@ -21,8 +21,9 @@
 namespace mars {
 
 // Tile shapes: query rows per tile and keys per unit of the split.
+template <int kRows>
 struct RowsShape {
-    static constexpr int M = 16;
+    static constexpr int M = kRows;
     static __host__ __device__ constexpr int unit_keys(int) { return 64; }
 };
 struct TileShape {
