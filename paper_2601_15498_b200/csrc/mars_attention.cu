@@ -38,6 +38,7 @@ constexpr int kRowsMax = 32;          // largest tile
 constexpr int rows_occ(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }   // blocks per SM (registers)
 constexpr int rows_grid(int rows) { return kAttnSms * rows_occ(rows); }
 constexpr int kUnit = 64;             // RowsShape::unit_keys
+constexpr float kNone = 1e30f;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
@@ -110,20 +111,22 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
         const int first = sg.unit0 * (kUnit / 16) + warp;
         const int last = min((sg.keys + 15) >> 4, sg.unit1 * (kUnit / 16));      // exclusive
         const int mine = first < last ? (last - first + kRowsWarps - 1) / kRowsWarps : 0;
-        int ids = -1, ids_at = 0;                        // lane i: page of block ids_at + i
-        auto fetch_ids = [&](int i0) {
-            ids_at = i0;
-            const int i = i0 + lane;
-            ids = i < mine ? kv_page_id(p.kv, sg.b, (first + i * kRowsWarps) * 16) : -1;
+        uint64_t from = 0;                               // lane i: address of block from_at + i, 0: no such page
+        int from_at = 0;
+        auto locate = [&](int i0) {
+            from_at = i0;
+            const int i = i0 + lane, pos = (first + i * kRowsWarps) * 16;
+            const int id = i < mine ? kv_page_id(p.kv, sg.b, pos) : -1;
+            from = id >= 0 ? (uint64_t)kv_block<D>(p.kv, p.layer, id, sg.head, pos) : 0;
         };
-        fetch_ids(0);
+        locate(0);
         bool poisoned = false;
         auto issue = [&](int i) {                        // 16-key block i of this warp into its ring slot
             if (i < mine) {
-                if (i >= ids_at + 32) fetch_ids(i);
-                const int id = __shfl_sync(0xffffffffu, ids, i - ids_at);
-                if (id >= 0) {
-                    const unsigned char *src = kv_block<D>(p.kv, p.layer, id, sg.head, (first + i * kRowsWarps) * 16) + lane * 16;
+                if (i >= from_at + 32) locate(i);
+                const uint64_t at = __shfl_sync(0xffffffffu, from, i - from_at);
+                if (at) {
+                    const unsigned char *src = (const unsigned char *)at + lane * 16;
                     const uint32_t dst = ring_u32 + (i % kRowsStages) * kBlk + lane * 16;
 #pragma unroll
                     for (int c = 0; c < (kChunks + 31) / 32; ++c)
@@ -175,7 +178,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
             float down, up;
             row_scale(m, &down, &up);
-            const float scale = p.scale_log2 * p.scales[sg.head] * up;
+            const float scale = fmaxf(p.scale_log2 * p.scales[sg.head] * up, 1.17549435e-38f);
             const int local = in ? nd - node0 : -1;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -203,9 +206,11 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
             for (int n = 0; n < kNT; ++n)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[j][n][k] = 0.0f;
-        float mref[kNT][2], l[kNT][2];
+        // base = 7 - reference maximum; kNone stands for "no key yet" and needs no case of its own: every
+        // score exceeds it, and ex2 of anything minus it is 0
+        float base[kNT][2], l[kNT][2];
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) { mref[n][0] = mref[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.0f; }
+        for (int n = 0; n < kNT; ++n) { base[n][0] = base[n][1] = kNone; l[n][0] = l[n][1] = 0.0f; }
         // rows and columns of the 16-key tile are permuted inside pairs so that neither the K rows nor the
         // V rows that a quarter warp reads together fall on the same banks
         const int key = (g & 6) + ((g ^ (g >> 1)) & 1);
@@ -272,7 +277,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
                     if (pos0 + 8 * w + k0 >= sg.len + sg.n) a = 0u;
                     if (pos0 + 8 * w + k1 >= sg.len + sg.n) c = 0u;
                 }
-                vs[w] = e4m3x2_to_f16x2(a | (c << 8));
+                vs[w] = e4m3x2_to_f16x2(__byte_perm(a, c, 0x0040));
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const unsigned char *cp = blk + 8 * D + (8 * w + (e ? k1 : k0)) * (D / 2) + g * (D / 16);
@@ -284,57 +289,58 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
                     }
                 }
             }
-            // ---- scores in log2 units (element k: key g or g + 8, row 2t + (k & 1)); behind the committed
-            // tokens only ancestors count
-            bool grow = false;
+            // ---- behind the committed tokens only ancestors count (element k: key g or g + 8, row 2t + (k & 1))
+            if (edge) {
 #pragma unroll
-            for (int n = 0; n < kNT; ++n)
+                for (int n = 0; n < kNT; ++n)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float x = s[n][k] * rs[n][k & 1];
-                    if (edge) {
+                    for (int k = 0; k < 4; ++k) {
                         const int pos = pos0 + 8 * (k >> 1) + key, m = pos - sg.len, nd = node[n][k & 1];
                         bool see = m < 0;
                         if (m >= 0 && pos < sg.keys && nd >= 0)
                             see = p.parent ? (s_mask[nd * words + (m >> 5)] >> (m & 31)) & 1u : m <= node0 + nd;
-                        if (!see) x = -INFINITY;
+                        if (!see) s[n][k] = -INFINITY;
                     }
-                    s[n][k] = x;
-                    grow |= x > mref[n][k & 1] + 8.0f;
+            }
+            // ---- P = 2^(s - maximum + 7), the maximum as it was; it moves only when a score exceeds it by
+            // more than 2^8.  So P <= 2^15, and with the row's largest at 2^7 or more fp16 keeps 11 bits of
+            // every probability above 2^-21 of it and an error of 2^-32 of it below
+            float x[kNT][4], top = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[n][k] = fmaf(s[n][k], rs[n][k & 1], base[n][k & 1]);
+                    top = fmaxf(top, x[n][k]);
                 }
-            // ---- the reference maximum moves only when a score exceeds it by more than 2^8
-            if (__any_sync(0xffffffffu, grow)) {
+            if (__any_sync(0xffffffffu, top > 15.0f)) {
 #pragma unroll
                 for (int n = 0; n < kNT; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[n][e], s[n][2 + e]);
+                        float mx = fmaxf(s[n][e], s[n][2 + e]) * rs[n][e];
 #pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-                        if (mx > mref[n][e] + 8.0f) {
-                            const float f = ex2(mref[n][e] - mx);
-                            mref[n][e] = mx;
+                        for (int k = 4; k < 32; k <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+                        if (mx + base[n][e] > 15.0f) {
+                            const float f = ex2(7.0f - mx - base[n][e]);
+                            base[n][e] = 7.0f - mx;
                             l[n][e] *= f;
 #pragma unroll
                             for (int j = 0; j < kSteps; ++j) { o[j][n][e] *= f; o[j][n][2 + e] *= f; }
+                            x[n][e] = fmaf(s[n][e], rs[n][e], base[n][e]);
+                            x[n][2 + e] = fmaf(s[n][2 + e], rs[n][e], base[n][e]);
                         }
                     }
             }
-            // P = 2^(s - mref + 7) <= 2^15: with the row's largest at 2^7 or more, fp16 keeps 11 bits of
-            // every probability above 2^-21 of it and an error of 2^-32 of it below
             uint32_t pb[kNT][2];
 #pragma unroll
             for (int n = 0; n < kNT; ++n) {
-                float x[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float ref = mref[n][k & 1];
-                    x[k] = ex2(s[n][k] - (ref == -INFINITY ? 0.0f : ref - 7.0f));
-                }
-                l[n][0] += x[0] + x[2];
-                l[n][1] += x[1] + x[3];
-                pb[n][0] = transpose8x8(f16x2_from(x[0], x[1]));
-                pb[n][1] = transpose8x8(f16x2_from(x[2], x[3]));
+                for (int k = 0; k < 4; ++k) x[n][k] = ex2(x[n][k]);
+                l[n][0] += x[n][0] + x[n][2];
+                l[n][1] += x[n][1] + x[n][3];
+                pb[n][0] = transpose8x8(f16x2_from(x[n][0], x[n][1]));
+                pb[n][1] = transpose8x8(f16x2_from(x[n][2], x[n][3]));
             }
             // ---- O^T += V^T P^T: this lane's keys are k0, k1 (first eight) and k0 + 8, k1 + 8
 #pragma unroll
@@ -362,7 +368,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
 #pragma unroll
             for (int n = 0; n < kNT; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) { l[n][e] = NAN; if (mref[n][e] == -INFINITY) mref[n][e] = 0.0f; }
+                for (int e = 0; e < 2; ++e) l[n][e] = NAN;
         }
 
         // ---- the four warps' sums, then the block's result
@@ -376,7 +382,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
 #pragma unroll
                 for (int k = 4; k < 32; k <<= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
                 const int row = 8 * n + 2 * t + e;
-                if (g == 0) { s_m[warp][row] = mref[n][e]; s_l[warp][row] = x; }
+                if (g == 0) { s_m[warp][row] = 7.0f - base[n][e]; s_l[warp][row] = x; }
                 float *to = s_o + (warp * kRows + row) * (D + 4) + g * (D / 8);
 #pragma unroll
                 for (int j = 0; j < kSteps; j += 2)
@@ -406,7 +412,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
             for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
 #pragma unroll
             for (int w = 0; w < kRowsWarps; ++w) {
-                const float f = s_m[w][orow] == -INFINITY ? 0.0f : ex2(s_m[w][orow] - m);
+                const float f = ex2(s_m[w][orow] - m);
                 sum += s_l[w][orow] * f;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) acc[k] += s_o[(w * kRows + orow) * (D + 4) + od + k] * f;
@@ -431,7 +437,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
             if (write) {
                 __threadfence();
                 for (int orow = tid / kAcross; orow < rows; orow += kAtOnce) {
-                    float m = -INFINITY, sum = 0.0f, acc[kPer];
+                    float m = -kNone, sum = 0.0f, acc[kPer];
 #pragma unroll
                     for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
 #pragma unroll 4
@@ -441,7 +447,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
                         const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od));
                         const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od + 4));
                         const float mm = fmaxf(m, pm);
-                        const float a = m == -INFINITY ? 0.0f : ex2(m - mm), b = pm == -INFINITY ? 0.0f : ex2(pm - mm);
+                        const float a = ex2(m - mm), b = ex2(pm - mm);
                         m = mm;
                         sum = sum * a + pl * b;
                         acc[0] = acc[0] * a + x.x * b; acc[1] = acc[1] * a + x.y * b; acc[2] = acc[2] * a + x.z * b; acc[3] = acc[3] * a + x.w * b;

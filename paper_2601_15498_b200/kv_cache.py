@@ -19,7 +19,7 @@ import ctypes
 import torch
 
 from . import mars
-from .mars import MarsError, _check, _stream, lib
+from .mars import MarsError, _check, lib
 
 FP16 = 2
 MAX_SEQS = 8192
@@ -69,6 +69,7 @@ class KVCache:
                                     seq_pages.data_ptr(), page_refs.data_ptr(), free_bits.data_ptr(), layers, num_pages,
                                     kv_heads, head_dim, page_size, seqs, width)
         self._ref = ctypes.byref(self._struct)
+        self._index = pages.get_device()
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, kv_heads: int, head_dim: int, page_size: int, seqs: int,
@@ -89,67 +90,65 @@ class KVCache:
                    page_size)
 
 
-class _on:
-    """The cache's device as the current one, at no cost where it already is."""
-    __slots__ = ("guard",)
+# The calls below run a few times per layer and decode step, so their host time counts: attributes are
+# read once, devices compared by index, the stream taken as a raw handle.
 
-    def __init__(self, dev):
-        self.guard = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+def _call(fn, cache: KVCache, *args) -> None:
+    """fn(descriptor, *args, stream) with the cache's device current; raises on a refusal."""
+    idx = cache._index
+    stream = torch._C._cuda_getCurrentRawStream(idx)
+    if torch._C._cuda_getDevice() == idx:
+        code = fn(cache._ref, *args, stream)
+    else:
+        with torch.cuda.device(idx):
+            code = fn(cache._ref, *args, stream)
+    if code:
+        _check(code, fn.__name__)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
 
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
-
-
-def _i32(t, n: int, dev, name: str):
-    """Device pointer of an int32 [n] tensor, None for None."""
+def _i32(t, n: int, index: int, name: str):
+    """Device pointer of an int32 tensor of n entries, None for None."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.device != dev or not t.is_contiguous() or t.numel() != n:
-        raise MarsError(f"{name} must be a contiguous int32 tensor of {n} entries on {dev}")
+    if t.dtype is not torch.int32 or t.get_device() != index or t.numel() != n or not t.is_contiguous():
+        raise MarsError(f"{name} must be a contiguous int32 tensor of {n} entries on the cache's device")
     return t.data_ptr()
 
 
-def _rows(t, heads: int, d: int, dev, name: str):
+def _rows(t, heads: int, d: int, index: int, name: str):
     """[B, N, heads, d] with unit inner stride and rows b*N + i at one stride: (pointer, row, head)."""
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != d or t.device != dev or t.dtype not in _DTYPES:
-        raise MarsError(f"{name} must be [B, N, {heads}, {d}] of bfloat16, float16 or float32 on {dev}")
-    B, N = t.shape[:2]
+    shape = t.shape
+    if len(shape) != 4 or shape[2] != heads or shape[3] != d or t.get_device() != index or t.dtype not in _DTYPES:
+        raise MarsError(f"{name} must be [B, N, {heads}, {d}] of bfloat16, float16 or float32 on the cache's device")
     sb, sn, sh, sd = t.stride()
-    if sd != 1 or (B > 1 and N > 1 and sb != N * sn):
+    if shape[1] == 1:
+        sn = sb if shape[0] > 1 else heads * d
+    elif shape[0] > 1 and sb != shape[1] * sn:
+        sd = 0
+    if sd != 1:
         raise MarsError(f"{name}: rows b*N + i must lie at one stride, with unit inner stride")
-    row = sn if N > 1 else sb if B > 1 else heads * d
-    return t.data_ptr(), row, sh if heads > 1 else d
+    return t.data_ptr(), sn, sh if heads > 1 else d
 
 
 def resize(cache: KVCache, extra: torch.Tensor, status: torch.Tensor | None = None) -> torch.Tensor | None:
     """mars_kv_resize: pages for seq_len[b] + extra[b] tokens of every sequence (0 trims, -1 releases,
     below: leave).  Returns `status` (int32 [seqs]) as it was given."""
-    dev = cache.device
-    with _on(dev):
-        code = lib().mars_kv_resize(cache._ref, _i32(extra, cache.seqs, dev, "extra"),
-                                    _i32(status, cache.seqs, dev, "status"), _stream())
-    _check(code, "mars_kv_resize")
+    dev = cache._index
+    _call(lib().mars_kv_resize, cache, _i32(extra, cache.seqs, dev, "extra"), _i32(status, cache.seqs, dev, "status"))
     return status
 
 
 def append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, count: torch.Tensor | None = None,
            status: torch.Tensor | None = None) -> None:
     """mars_kv_append: rows k, v [B, N, kv_heads, head_dim] to positions seq_len[b] + i."""
-    dev = cache.device
+    dev = cache._index
     kp, kr, kh = _rows(k, cache.kv_heads, cache.head_dim, dev, "k")
     vp, vr, vh = _rows(v, cache.kv_heads, cache.head_dim, dev, "v")
-    if k.shape != v.shape or k.dtype != v.dtype:
+    if k.shape != v.shape or k.dtype is not v.dtype:
         raise MarsError("k and v must have the same shape and dtype")
     B, N = k.shape[:2]
-    with _on(dev):
-        code = lib().mars_kv_append(cache._ref, layer, kp, kr, kh, vp, vr, vh, _DTYPES[k.dtype], B, N,
-                                    _i32(count, B, dev, "count"), _i32(status, B, dev, "status"), _stream())
-    _check(code, "mars_kv_append")
+    _call(lib().mars_kv_append, cache, layer, kp, kr, kh, vp, vr, vh, _DTYPES[k.dtype], B, N,
+          _i32(count, B, dev, "count"), _i32(status, B, dev, "status"))
 
 
 def attention_workspace_bytes(B: int, N: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -171,37 +170,33 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, parent: torch.Te
     """mars_tree_attention: q [B, N, q_heads, head_dim] over the cache; parent int32 [B, N], [N] or None
     (chains).  `workspace` comes from ``attention_workspace`` and is used by these calls only; without
     one, a call allocates its own.  Rows without a result keep what `out` holds."""
-    dev = cache.device
-    if q.dim() != 4 or q.shape[2] % cache.kv_heads:
+    dev, H = cache._index, cache.kv_heads
+    if q.dim() != 4 or q.shape[2] % H:
         raise MarsError("q must be [B, N, q_heads, head_dim] with q_heads a multiple of kv_heads")
     B, N, Hq, d = q.shape
     qp, qr, qh = _rows(q, Hq, cache.head_dim, dev, "q")
     if out is None:
-        out = torch.empty((B, N, Hq, d), dtype=q.dtype, device=dev)
+        out = torch.empty((B, N, Hq, d), dtype=q.dtype, device=cache.device)
     op, orow, oh = _rows(out, Hq, cache.head_dim, dev, "out")
-    if out.shape != q.shape or out.dtype != q.dtype:
+    if out.dtype is not q.dtype or out.shape != q.shape:
         raise MarsError("out must have the shape and dtype of q")
-    flags = 0
-    pp = None
+    flags, pp = 0, None
     if parent is not None:
-        if parent.dim() == 1:
-            flags |= mars.SHARED_PARENT
-        pp = _i32(parent, N if parent.dim() == 1 else B * N, dev, "parent")
+        shared = parent.dim() == 1
+        flags = mars.SHARED_PARENT if shared else 0
+        pp = _i32(parent, N if shared else B * N, dev, "parent")
     if workspace is None:
-        need = attention_workspace_bytes(B, N, Hq, cache.kv_heads, d)
+        need = attention_workspace_bytes(B, N, Hq, H, d)
         if need == 0:
             raise MarsError("unsupported sizes")
-        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=cache.device)
     else:
-        if workspace.device != dev or not workspace.is_contiguous():
+        if workspace.get_device() != dev or not workspace.is_contiguous():
             raise MarsError("workspace must be a contiguous tensor on the cache's device")
         flags |= mars.COUNTERS_ZERO
-    with _on(dev):
-        code = lib().mars_tree_attention(cache._ref, layer, qp, qr, qh, _DTYPES[q.dtype], Hq, B, N, pp,
-                                         _i32(count, B, dev, "count"), d ** -0.5 if scale is None else float(scale),
-                                         flags, op, orow, oh, _i32(status, B, dev, "status"), workspace.data_ptr(),
-                                         workspace.numel() * workspace.element_size(), _stream())
-    _check(code, "mars_tree_attention")
+    _call(lib().mars_tree_attention, cache, layer, qp, qr, qh, _DTYPES[q.dtype], Hq, B, N, pp,
+          _i32(count, B, dev, "count"), d ** -0.5 if scale is None else scale, flags, op, orow, oh,
+          _i32(status, B, dev, "status"), workspace.data_ptr(), workspace.nbytes)
     return out
 
 
@@ -209,34 +204,30 @@ def commit(cache: KVCache, path_nodes: torch.Tensor | None, accept_len: torch.Te
            new_len: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
     """mars_kv_commit with the path_nodes [B, W] and accept_len [B] of a verification (path_nodes None:
     chains).  `new_len` int32 [B] receives the lengths, by default cache.seq_len itself."""
-    dev = cache.device
+    dev = cache._index
     B = accept_len.numel()
-    new_len = cache.seq_len if new_len is None else new_len
     W = 0
     if path_nodes is not None:
         if path_nodes.dim() != 2 or path_nodes.shape[0] != B:
             raise MarsError("path_nodes must be [B, W]")
         W = path_nodes.shape[1]
-    if new_len is not cache.seq_len:
-        _i32(new_len, B, dev, "new_len")
-    with _on(dev):
-        code = lib().mars_kv_commit(cache._ref, _i32(path_nodes, B * W, dev, "path_nodes"), W,
-                                    _i32(accept_len, B, dev, "accept_len"), B, new_len.data_ptr(),
-                                    _i32(status, B, dev, "status"), _stream())
-    _check(code, "mars_kv_commit")
+    if new_len is None or new_len is cache.seq_len:
+        new_len = cache.seq_len
+        lp = new_len.data_ptr()
+    else:
+        lp = _i32(new_len, B, dev, "new_len")
+    _call(lib().mars_kv_commit, cache, _i32(path_nodes, B * W, dev, "path_nodes"), W,
+          _i32(accept_len, B, dev, "accept_len"), B, lp, _i32(status, B, dev, "status"))
     return new_len
 
 
 def fork(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, status: torch.Tensor | None = None) -> torch.Tensor:
     """mars_kv_fork: sequence dst[p] becomes a copy of src[p]; returns the pairs' status."""
-    dev = cache.device
+    dev = cache._index
     n = src.numel()
     if status is None:
-        status = torch.empty((n,), dtype=torch.int32, device=dev)
-    with _on(dev):
-        code = lib().mars_kv_fork(cache._ref, _i32(src, n, dev, "src"), _i32(dst, n, dev, "dst"), n,
-                                  _i32(status, n, dev, "status"), _stream())
-    _check(code, "mars_kv_fork")
+        status = torch.empty((n,), dtype=torch.int32, device=cache.device)
+    _call(lib().mars_kv_fork, cache, _i32(src, n, dev, "src"), _i32(dst, n, dev, "dst"), n, _i32(status, n, dev, "status"))
     return status
 
 
@@ -244,20 +235,17 @@ def gather(cache: KVCache, layer0: int, layers: int, start: torch.Tensor | None,
            rows: int | None = None, dtype=torch.bfloat16, out=None):
     """mars_kv_gather: (k, v), each [layers, B, rows, kv_heads, head_dim], of positions start[b] ..
     start[b] + count[b] - 1; `out` = such a pair to write into (its dtype is used)."""
-    dev = cache.device
+    dev = cache._index
     B = start.numel() if start is not None else count.numel() if count is not None else cache.seqs
     if out is None:
         shape = (layers, B, int(rows), cache.kv_heads, cache.head_dim)
-        out = (torch.zeros(shape, dtype=dtype, device=dev), torch.zeros(shape, dtype=dtype, device=dev))
+        out = (torch.zeros(shape, dtype=dtype, device=cache.device), torch.zeros(shape, dtype=dtype, device=cache.device))
     k, v = out
-    rows = k.shape[2] if k.dim() == 5 else 0
-    for t in (k, v):
-        if tuple(t.shape) != (layers, B, rows, cache.kv_heads, cache.head_dim) or not t.is_contiguous() \
-                or t.device != dev or t.dtype not in _DTYPES or t.dtype != k.dtype:
-            raise MarsError("out must be two contiguous [layers, B, rows, kv_heads, head_dim] tensors of one dtype")
-    with _on(dev):
-        code = lib().mars_kv_gather(cache._ref, layer0, layers, B, _i32(start, B, dev, "start"),
-                                    _i32(count, B, dev, "count"), rows, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype],
-                                    _stream())
-    _check(code, "mars_kv_gather")
+    shape = k.shape
+    if len(shape) != 5 or shape != v.shape or shape[0] != layers or shape[1] != B or shape[3] != cache.kv_heads \
+            or shape[4] != cache.head_dim or k.dtype is not v.dtype or k.dtype not in _DTYPES \
+            or not (k.is_contiguous() and v.is_contiguous()) or k.get_device() != dev or v.get_device() != dev:
+        raise MarsError("out must be two contiguous [layers, B, rows, kv_heads, head_dim] tensors of one dtype")
+    _call(lib().mars_kv_gather, cache, layer0, layers, B, _i32(start, B, dev, "start"), _i32(count, B, dev, "count"),
+          shape[2], k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype])
     return k, v

@@ -36,6 +36,8 @@ class _DebugOut(ctypes.Structure):
 def lib() -> ctypes.CDLL:
     """Open libmars.so (built in-tree by ``build.build()``); raises if it is missing."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = _build.LIB

@@ -139,9 +139,9 @@ def test_binding_checks_tensors():
         with pytest.raises(mars.MarsError, match="contiguous"):
             kv_cache.KVCache(**{**good, k: bad})
     with pytest.raises(mars.MarsError, match="one stride"):
-        kv_cache._rows(t(3, 4, 2, 64, dt=torch.float32)[:, :3], 2, 64, torch.device("cpu"), "k")
+        kv_cache._rows(t(3, 4, 2, 64, dt=torch.float32)[:, :3], 2, 64, -1, "k")
     with pytest.raises(mars.MarsError, match="must be"):
-        kv_cache._rows(t(3, 4, 2, 64), 2, 64, torch.device("cpu"), "k")
+        kv_cache._rows(t(3, 4, 2, 64), 2, 64, -1, "k")
     with pytest.raises(mars.MarsError, match="int32"):
-        kv_cache._i32(t(4), 3, torch.device("cpu"), "count")
-    assert kv_cache._rows(t(3, 4, 9, 64, dt=torch.float32)[:, :, 2:4], 2, 64, torch.device("cpu"), "k")[1:] == (576, 64)
+        kv_cache._i32(t(4), 3, -1, "count")
+    assert kv_cache._rows(t(3, 4, 9, 64, dt=torch.float32)[:, :, 2:4], 2, 64, -1, "k")[1:] == (576, 64)
