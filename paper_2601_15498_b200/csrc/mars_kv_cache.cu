@@ -30,38 +30,63 @@ struct AppendParams {
     const int32_t *count;
     int32_t *status;
     int N;
+    bool wide;                 // every group of 16 values on a 32-byte boundary
 };
 
-// 16 values of `DT` at p (16-byte aligned), widened exactly.
-template <int DT>
-__device__ __forceinline__ void load16(const unsigned char *p, float (&x)[16])
+// 32 bytes at p; `wide`: p is 32-byte aligned and one load does (two 16-byte loads of a warp would each
+// touch half of every 32-byte sector).
+__device__ __forceinline__ void load32(const unsigned char *p, bool wide, uint32_t (&w)[8])
 {
-    const uint4 *q = reinterpret_cast<const uint4 *>(p);
-    if constexpr (DT == MARS_FP32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 u = ld_stream(q + i);
-            x[4 * i] = __uint_as_float(u.x); x[4 * i + 1] = __uint_as_float(u.y);
-            x[4 * i + 2] = __uint_as_float(u.z); x[4 * i + 3] = __uint_as_float(u.w);
-        }
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
     } else {
-        const uint4 u[2] = {ld_stream(q), ld_stream(q + 1)};
+        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store32(unsigned char *p, bool wide, const uint32_t (&w)[8])
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+            ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// 16 values of `DT`, widened exactly.
+template <int DT>
+__device__ __forceinline__ void load16(const unsigned char *p, bool wide, float (&x)[16])
+{
+    uint32_t w[8];
+    load32(p, wide, w);
+    if constexpr (DT == MARS_FP32) {
+        uint32_t v[8];
+        load32(p + 32, wide, v);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+        for (int i = 0; i < 8; ++i) { x[i] = __uint_as_float(w[i]); x[8 + i] = __uint_as_float(v[i]); }
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (DT == MARS_BF16) {
-                    x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-                    x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-                } else {
-                    const float2 f = f16x2_to_float2(w[j]);
-                    x[8 * i + 2 * j] = f.x;
-                    x[8 * i + 2 * j + 1] = f.y;
-                }
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (DT == MARS_BF16) {
+                x[2 * j] = __uint_as_float(w[j] << 16);
+                x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            } else {
+                const float2 f = f16x2_to_float2(w[j]);
+                x[2 * j] = f.x;
+                x[2 * j + 1] = f.y;
             }
         }
     }
+}
+
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t e4m3_from(float x)   // nearest even, saturating; x >= 0, not NaN
@@ -86,9 +111,33 @@ __device__ __forceinline__ uint32_t e2m1x8_from(const float *t)
     return r;
 }
 
-// One thread per 16 values: grid.y = sequence, x over (row, head, K or V, group of 16).
-// The quotient x / (s*g) is an IEEE division on purpose: with 8-bit significands and a power of two
-// as g many quotients lie exactly on the border of two codes, where a reciprocal's last bit decides.
+// Sixteen values against their scale: IEEE quotients x / sg, as the definition has it, in place.  With
+// 8-bit significands and a power of two as g many quotients lie exactly on the border of two codes,
+// where a reciprocal's last bit would decide.  Fast form: x * r and one residual correction
+// (Markstein 1990: with r the rounded reciprocal, fma(fma(-q, sg, x), r, q) is the rounded quotient
+// while nothing over- or underflows); |x / sg| <= 6.4 there, since the scale did not saturate.
+__device__ __forceinline__ void quotients16(float (&x)[16], float sg, bool plain)
+{
+    if (plain) {
+        const float r = __frcp_rn(sg);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float q = __fmul_rn(x[i], r);
+            x[i] = __fmaf_rn(__fmaf_rn(-q, sg, x[i]), r, q);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = sg > 0.0f ? __fdiv_rn(x[i], sg) : 0.0f;
+    }
+}
+
+constexpr int kRowIters = 4;     // rows that a thread of append / gather goes through
+
+// Rows a block of 256 threads covers at once when a row takes per_row threads.
+__host__ __device__ inline int rows_at_once(int per_row) { return per_row >= 256 ? 1 : 256 / per_row; }
+
+// A thread per 16 values and row (kRowIters rows one after the other): grid.y = sequence.
+// Bound by memory from a few thousand rows on; below that by its latency.
 template <int D, int DT>
 __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
 {
@@ -96,43 +145,46 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
     pdl_wait();
     constexpr int kG = D / 16;   // groups of a row
     const int b = blockIdx.y;
-    const int n = p.count ? min(max(p.count[b], 0), p.N) : p.N;
-    const int len = p.kv.seq_len[b];
-    const bool room = n == 0 || (len >= 0 && (int64_t)len + n <= kv_capacity(p.kv, b));
-    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (idx == 0 && p.status) p.status[b] = room ? MARS_SEQ_OK : MARS_SEQ_NO_ROOM;
+    const int count = p.count ? p.count[b] : p.N, len = p.kv.seq_len[b], cap = kv_capacity(p.kv, b);
+    const int n = min(max(count, 0), p.N);
+    const bool room = n == 0 || (len >= 0 && (int64_t)len + n <= cap);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) p.status[b] = room ? MARS_SEQ_OK : MARS_SEQ_NO_ROOM;
     if (!room) return;
-    const int per_row = p.kv.kv_heads * 2 * kG;
-    const int64_t row = idx / per_row;
-    if (row >= n) return;
-    const int in_row = (int)(idx - row * per_row);
-    const int h = in_row / (2 * kG), kv = (in_row / kG) & 1, grp = in_row % kG;
-    const int pos = len + (int)row;
-    const int id = kv_page_id(p.kv, b, pos);
-    if (id < 0) return;
-
-    float x[16];
-    load16<DT>(p.src[kv] + (((int64_t)b * p.N + row) * p.row[kv] + h * p.head[kv] + grp * 16) * elem_bytes(DT), x);
-    float a = 0.0f;
+    const int per_row = p.kv.kv_heads * 2 * kG, at_once = rows_at_once(per_row);
+    const int lane_row = per_row >= 256 ? 0 : (int)threadIdx.x / per_row;
+    if (lane_row >= at_once) return;
+    int row = blockIdx.x * at_once * kRowIters + lane_row;
+#pragma unroll 1
+    for (int it = 0; it < kRowIters && row < n; ++it, row += at_once) {
+        const int pos = len + row, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+#pragma unroll 1
+        for (int c = per_row >= 256 ? threadIdx.x : (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
+            if (id < 0) break;
+            const int h = c / (2 * kG), kv = (c / kG) & 1, grp = c % kG;
+            const unsigned char *src = (kv ? p.src[1] : p.src[0]) +
+                                       (((int64_t)b * p.N + row) * (kv ? p.row[1] : p.row[0]) + h * (kv ? p.head[1] : p.head[0]) + grp * 16) * elem_bytes(DT);
+            float x[16];
+            load16<DT>(src, p.wide, x);
+            float a = fabsf(x[0]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        x[i] = x[i] == x[i] ? x[i] : 0.0f;
-        a = fmaxf(a, fabsf(x[i]));
-    }
-    const float g = p.scales[kv * p.kv.kv_heads + h];
-    const uint32_t s8 = e4m3_from(__fdiv_rn(__fdiv_rn(a, 6.0f), g));
-    const float sg = __fmul_rn(f16x2_to_float2(e4m3x2_to_f16x2(s8)).x, g);
-    uint2 codes = make_uint2(0u, 0u);
-    if (sg > 0.0f) {
+            for (int i = 1; i < 16; ++i) a = max_nan(a, fabsf(x[i]));
+            if (a != a) {                    // NaN counts as 0
+                a = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], sg);
-        codes.x = e2m1x8_from(x);
-        codes.y = e2m1x8_from(x + 8);
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = x[i] == x[i] ? x[i] : 0.0f;
+                    a = fmaxf(a, fabsf(x[i]));
+                }
+            }
+            const float g = p.scales[kv * p.kv.kv_heads + h];
+            const uint32_t s8 = e4m3_from(__fdiv_rn(__fdiv_rn(a, 6.0f), g));
+            const float sg = __fmul_rn(f16x2_to_float2(e4m3x2_to_f16x2(s8)).x, g);
+            quotients16(x, sg, s8 != 0x7eu && sg > 1e-30f && sg < 1e30f);
+            unsigned char *blk = kv_block<D>(p.kv, p.layer, id, h, pos);
+            *reinterpret_cast<uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8) = make_uint2(e2m1x8_from(x), e2m1x8_from(x + 8));
+            blk[16 * D + D * kv + slot * kG + grp] = (unsigned char)s8;
+        }
     }
-    unsigned char *blk = kv_block<D>(p.kv, p.layer, id, h, pos);
-    const int slot = pos & 15;
-    *reinterpret_cast<uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8) = codes;
-    blk[16 * D + D * kv + slot * kG + grp] = (unsigned char)s8;
 }
 
 // --------------------------------------------------------------------------------- gather
@@ -143,61 +195,68 @@ struct GatherParams {
     const int32_t *start, *count;
     unsigned char *dst[2];
     int B, rows;
+    bool wide;                 // outputs on 32-byte boundaries
 };
 
-// One thread per 16 values: grid.y = sequence, grid.z = layer.
+// A thread per 16 values and row, as in append: grid.y = sequence, grid.z = layer.
 template <int D, int DT>
 __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams p)
 {
     pdl_launch_dependents();
     pdl_wait();
     constexpr int kG = D / 16;
-    const int b = blockIdx.y, lay = blockIdx.z;
-    const int n = p.count ? min(max(p.count[b], 0), p.rows) : p.rows;
-    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const int per_row = p.kv.kv_heads * 2 * kG;
-    const int64_t row = idx / per_row;
-    if (row >= n) return;
-    const int in_row = (int)(idx - row * per_row);
-    const int kv = in_row / (p.kv.kv_heads * kG), h = (in_row / kG) % p.kv.kv_heads, grp = in_row % kG;
-    const int64_t pos64 = (int64_t)(p.start ? p.start[b] : 0) + row;
-    if (pos64 < 0 || pos64 >= kv_capacity(p.kv, b)) return;
-    const int pos = (int)pos64;
-    const int id = kv_page_id(p.kv, b, pos);
-    if (id < 0) return;
+    const int b = blockIdx.y, lay = blockIdx.z, H = p.kv.kv_heads;
+    const int count = p.count ? p.count[b] : p.rows, start = p.start ? p.start[b] : 0, cap = kv_capacity(p.kv, b);
+    const int n = min(max(count, 0), p.rows);
+    const int per_row = H * 2 * kG, at_once = rows_at_once(per_row);
+    const int lane_row = per_row >= 256 ? 0 : (int)threadIdx.x / per_row;
+    if (lane_row >= at_once) return;
     unsigned char *layer = p.kv.pages + (int64_t)(p.layer0 + lay) * p.kv.layer_bytes;
-    const unsigned char *blk = kv_block<D>(p.kv, layer, id, h, pos);
-    const int slot = pos & 15;
-    const uint2 codes = *reinterpret_cast<const uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8);
-    const float s = f16x2_to_float2(e4m3x2_to_f16x2(blk[16 * D + D * kv + slot * kG + grp])).x;
-    // code * scale has at most 6 significant bits, so the product with g is the only rounding
-    const float g = p.kv.scales[((int64_t)(p.layer0 + lay) * 2 + kv) * p.kv.kv_heads + h];
-    float x[16];
-    uint32_t hh[4];
+    const float *scales = p.kv.scales + (int64_t)(p.layer0 + lay) * 2 * H;
+    int row = blockIdx.x * at_once * kRowIters + lane_row;
+#pragma unroll 1
+    for (int it = 0; it < kRowIters && row < n; ++it, row += at_once) {
+        const int64_t pos64 = (int64_t)start + row;
+        if (pos64 < 0 || pos64 >= cap) continue;
+        const int pos = (int)pos64, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+#pragma unroll 1
+        for (int c = per_row >= 256 ? threadIdx.x : (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
+            if (id < 0) break;
+            const int kv = c >= H * kG, h = (c / kG) - kv * H, grp = c % kG;
+            const unsigned char *blk = kv_block<D>(p.kv, layer, id, h, pos);
+            const uint2 codes = *reinterpret_cast<const uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8);
+            const uint32_t s = e4m3x2_to_f16x2(blk[16 * D + D * kv + slot * kG + grp] * 0x101u);
+            // code * scale is exact in fp16, so the product with g is the only rounding before the output's
+            const float g = scales[kv * H + h];
+            float x[16];
+            uint32_t hh[4];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        e2m1x8_to_f16x2(w ? codes.y : codes.x, hh);
+            for (int w = 0; w < 2; ++w) {
+                e2m1x8_to_f16x2(w ? codes.y : codes.x, hh);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 f = f16x2_to_float2(hh[j]);
-            x[8 * w + 2 * j] = f.x * s * g;
-            x[8 * w + 2 * j + 1] = f.y * s * g;
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = f16x2_to_float2(hmul2(hh[j], s));
+                    x[8 * w + 2 * j] = f.x * g;
+                    x[8 * w + 2 * j + 1] = f.y * g;
+                }
+            }
+            const int64_t at = ((((int64_t)lay * p.B + b) * p.rows + row) * H + h) * D + grp * 16;
+            unsigned char *o = (kv ? p.dst[1] : p.dst[0]) + at * elem_bytes(DT);
+            uint32_t w[8];
+            if constexpr (DT == MARS_FP32) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(x[8 * half + i]);
+                    store32(o + 32 * half, p.wide, w);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[i] = DT == MARS_BF16 ? bf16x2_from(x[2 * i], x[2 * i + 1]) : f16x2_from(x[2 * i], x[2 * i + 1]);
+                store32(o, p.wide, w);
+            }
         }
-    }
-    const int64_t at = ((((int64_t)lay * p.B + b) * p.rows + row) * p.kv.kv_heads + h) * D + grp * 16;
-    uint4 *o = reinterpret_cast<uint4 *>((kv ? p.dst[1] : p.dst[0]) + at * elem_bytes(DT));
-    if constexpr (DT == MARS_FP32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
-                              __float_as_uint(x[4 * i + 3]));
-    } else {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w[i] = DT == MARS_BF16 ? bf16x2_from(x[2 * i], x[2 * i + 1]) : f16x2_from(x[2 * i], x[2 * i + 1]);
-        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        o[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
 }
 
@@ -216,9 +275,9 @@ struct CommitParams {
 __device__ bool commit_path_ok(const CommitParams &p, int b, int lane, int *a_out)
 {
     const int a = p.accept_len[b], len = p.kv.seq_len[b];
+    const int64_t cap = kv_capacity(p.kv, b);
     *a_out = a;
     if (a == -1) return true;
-    const int64_t cap = kv_capacity(p.kv, b);
     bool ok = a >= 0 && len >= 0 && (p.path ? a < p.path_width : (int64_t)len + a < cap);
     if (ok && p.path) {
         const int32_t *path = p.path + (int64_t)b * p.path_width;
@@ -258,34 +317,42 @@ __global__ void __launch_bounds__(128) kv_commit_kernel(const CommitParams p)
     constexpr int kCode = D / 16, kPieces = kCode + 2, kPer = 4;
     constexpr int kRows = 32 * kPer / kPieces;   // rows per batch
     for (int j0 = 1; j0 <= a; j0 += kRows) {
+        const int rows = min(kRows, a + 1 - j0);
+        // lane r: block of row j0 + r's source and destination and its slots there, 0 where nothing moves
+        uint64_t from = 0, into = 0;
+        int slots = 0;
+        if (lane < rows) {
+            const int src = len + path[j0 + lane], dst = len + j0 + lane;
+            const int ids = kv_page_id(p.kv, b, src), idd = kv_page_id(p.kv, b, dst);
+            if (src != dst && ids >= 0 && idd >= 0) {
+                from = (uint64_t)kv_block<D>(p.kv, layer, ids, h, src);
+                into = (uint64_t)kv_block<D>(p.kv, layer, idd, h, dst);
+                slots = (src & 15) | (dst & 15) << 4;
+            }
+        }
         uint4 v[kPer];
         unsigned char *to[kPer];
-        const int rows = min(kRows, a + 1 - j0);
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             const int i = u * 32 + lane, r = i / kPieces, c = i - r * kPieces;
+            const unsigned char *sb = (const unsigned char *)__shfl_sync(0xffffffffu, from, r & 31);
+            unsigned char *db = (unsigned char *)__shfl_sync(0xffffffffu, into, r & 31);
+            const int sl = __shfl_sync(0xffffffffu, slots, r & 31), ss = sl & 15, ds = sl >> 4;
             to[u] = nullptr;
-            if (r < rows) {
-                const int j = j0 + r, src = len + path[j], dst = len + j;
-                const int ids = kv_page_id(p.kv, b, src), idd = kv_page_id(p.kv, b, dst);
-                if (src != dst && ids >= 0 && idd >= 0) {
-                    const unsigned char *sb = kv_block<D>(p.kv, layer, ids, h, src);
-                    unsigned char *db = kv_block<D>(p.kv, layer, idd, h, dst);
-                    const int ss = src & 15, ds = dst & 15;
-                    if (c < kCode) {
-                        const int half = c / (kCode / 2), in = c % (kCode / 2);
-                        v[u] = *reinterpret_cast<const uint4 *>(sb + 8 * D * half + ss * (D / 2) + in * 16);
-                        to[u] = db + 8 * D * half + ds * (D / 2) + in * 16;
+            if (r < rows && sb) {
+                if (c < kCode) {
+                    const int off = 8 * D * (c / (kCode / 2)), in = (c % (kCode / 2)) * 16;
+                    v[u] = *reinterpret_cast<const uint4 *>(sb + off + ss * (D / 2) + in);
+                    to[u] = db + off + ds * (D / 2) + in;
+                } else {
+                    const int off = 16 * D + D * (c - kCode);
+                    if constexpr (D == 128) {
+                        const uint2 t = *reinterpret_cast<const uint2 *>(sb + off + ss * 8);
+                        v[u].x = t.x; v[u].y = t.y;
                     } else {
-                        const int off = 16 * D + D * (c - kCode);
-                        if constexpr (D == 128) {
-                            const uint2 t = *reinterpret_cast<const uint2 *>(sb + off + ss * 8);
-                            v[u].x = t.x; v[u].y = t.y;
-                        } else {
-                            v[u].x = *reinterpret_cast<const uint32_t *>(sb + off + ss * 4);
-                        }
-                        to[u] = db + off + ds * (D / 16);
+                        v[u].x = *reinterpret_cast<const uint32_t *>(sb + off + ss * 4);
                     }
+                    to[u] = db + off + ds * (D / 16);
                 }
             }
         }
@@ -379,10 +446,29 @@ __device__ int count_free(const uint32_t *bits, int words, int enough, int *s_wa
     return have;
 }
 
+// The k-th (from 0) set bit of w, which has more than k.
+__device__ __forceinline__ int nth_bit(uint32_t w, int k)
+{
+    int at = 0;
+#pragma unroll
+    for (int half = 16; half; half >>= 1) {
+        const int c = __popc((w >> at) & ((1u << half) - 1u));
+        if (k >= c) { k -= c; at += half; }
+    }
+    return at;
+}
+
+struct FreeTile {                // 1024 words of the free set: exclusive prefix counts and the words
+    int first[kPoolThreads];
+    uint32_t word[kPoolThreads];
+    int warp[32];
+};
+
 // The lowest free pages 0, 1, ... of the set go, in order, to `give(rank, page)` for rank < total, and
-// leave the set (one thread block; each word belongs to one thread).
+// leave the set (one thread block).  Ranks, not words, are spread over the threads: free pages tend to
+// lie together, and a word's 32 pages would otherwise be given by one thread.
 template <class Give>
-__device__ void take_free(uint32_t *bits, int words, int total, int *s_warp, Give give)
+__device__ void take_free(uint32_t *bits, int words, int total, FreeTile *f, Give give)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int base = 0;
@@ -396,28 +482,33 @@ __device__ void take_free(uint32_t *bits, int words, int total, int *s_warp, Giv
             const int t = __shfl_up_sync(0xffffffffu, inc, o);
             if (lane >= o) inc += t;
         }
-        if (lane == 31) s_warp[warp] = inc;
+        if (lane == 31) f->warp[warp] = inc;
         __syncthreads();
-        if (warp == 0) {
-            int x = s_warp[lane];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int t = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += t;
+        const int sums = f->warp[lane];
+        const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums : 0);
+        const int all = __reduce_add_sync(0xffffffffu, sums);
+        const int first = before + inc - c;
+        f->first[tid] = first;
+        f->word[tid] = word;
+        __syncthreads();
+        const int here = min(all, total - base);
+        for (int r = tid; r < here; r += kPoolThreads) {
+            int lo = 0, hi = kPoolThreads;           // last word with first <= r
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (f->first[mid] <= r) lo = mid;
+                else hi = mid;
             }
-            s_warp[lane] = x;
+            give(base + r, (w0 + lo) * 32 + nth_bit(f->word[lo], r - f->first[lo]));
         }
-        __syncthreads();
-        int rank = base + inc - c + (warp ? s_warp[warp - 1] : 0);
-        base += s_warp[31];
-        uint32_t left = word;
-        while (left && rank < total) {
-            const int bit = __ffs((int)left) - 1;
-            left &= left - 1;
-            give(rank, w * 32 + bit);
-            ++rank;
+        // what stays of this thread's word
+        if (c && first < here) {
+            int gone = min(c, here - first);
+            if (gone == c) word = 0u;
+            for (; word && gone; --gone) word &= word - 1;
+            bits[w] = word;
         }
-        if (left != word) bits[w] = left;
+        base += all;
         __syncthreads();
     }
 }
@@ -449,18 +540,16 @@ __device__ __forceinline__ void cluster_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Pages that sequence b shall hold; -1: the request does not fit its table row; `leave`: no request.
-__device__ __forceinline__ int resize_want(const PoolParams &p, int b, int held, bool *leave)
+// Pages that a sequence with `held` pages shall hold; -1: the request does not fit its table row.
+__device__ __forceinline__ int resize_want(const PoolParams &p, int extra, int len, int held)
 {
-    const int ex = p.extra[b];
-    *leave = ex < -1;
-    if (ex < -1) return held;
-    if (ex == -1) return 0;
-    const int64_t pages = ((int64_t)max(p.seq_len[b], 0) + ex + p.page_size - 1) >> p.page_log2;
+    if (extra < -1) return held;
+    if (extra == -1) return 0;
+    const int64_t pages = ((int64_t)max(len, 0) + extra + p.page_size - 1) >> p.page_log2;
     return pages > p.table_width ? -1 : (int)pages;
 }
 
-// One cluster of eight blocks.  First all of it gives pages back (a warp per sequence; counts and free
+// One cluster of eight blocks.  First all of it gives pages back (counts and free
 // bits are changed by commutative integer atomics, so the order is immaterial); the cluster barrier
 // makes that visible; then its first block serves the growing requests from the lowest free pages,
 // found by a prefix sum over the bit set.  No order of threads shows in the result.
@@ -470,39 +559,44 @@ __global__ void __cluster_dims__(kPoolCluster, 1, 1) __launch_bounds__(kPoolThre
     pdl_wait();
     extern __shared__ int s_first[];   // [n]
     __shared__ int s_warp[32];
+    __shared__ FreeTile s_free;
     const int lane = threadIdx.x & 31;
-    for (int b = blockIdx.x * (kPoolThreads / 32) + (threadIdx.x >> 5); b < p.n; b += kPoolCluster * (kPoolThreads / 32)) {
-        const int held = min(max(p.seq_pages[b], 0), p.table_width);
-        bool leave;
-        const int want = resize_want(p, b, held, &leave);
-        const int ex = p.extra[b];
-        __syncwarp();
-        if (!leave && want >= 0 && want < held) {
-            int32_t *row = p.table + (int64_t)b * p.table_width;
-            for (int c = want + lane; c < held; c += 32) {
+    // a lane per sequence decides, then the warp gives back the pages of one sequence after the other
+    constexpr int kLanes = 8;           // sequences per warp and round: more warps share the rows of a round
+    const int warps = kPoolCluster * (kPoolThreads / 32), warp = blockIdx.x * (kPoolThreads / 32) + (threadIdx.x >> 5);
+    for (int b0 = warp * kLanes; b0 < p.n; b0 += warps * kLanes) {
+        const int b = b0 + lane;
+        int held = 0, want = 0;
+        bool drop = false;
+        if (lane < kLanes && b < p.n) {
+            const int ex = p.extra[b], pages = p.seq_pages[b], len = p.seq_len[b];
+            held = min(max(pages, 0), p.table_width);
+            want = resize_want(p, ex, len, held);
+            drop = want >= 0 && want < held;
+            if (drop) p.seq_pages[b] = want;
+            if (ex == -1) p.seq_len[b] = 0;
+            if (p.status && want <= held) p.status[b] = want < 0 ? MARS_SEQ_NO_ROOM : MARS_SEQ_OK;
+        }
+        for (unsigned left = __ballot_sync(0xffffffffu, drop); left; left &= left - 1) {
+            const int i = __ffs((int)left) - 1;
+            const int from = __shfl_sync(0xffffffffu, want, i), upto = __shfl_sync(0xffffffffu, held, i);
+            int32_t *row = p.table + (int64_t)(b0 + i) * p.table_width;
+#pragma unroll 8
+            for (int c = from + lane; c < upto; c += 32) {
                 const int id = row[c];
                 row[c] = -1;
                 if ((unsigned)id < (unsigned)p.num_pages && atomicSub(p.refs + id, 1) == 1)
                     atomicOr(p.bits + (id >> 5), 1u << (id & 31));
             }
-            if (lane == 0) p.seq_pages[b] = want;
         }
-        if (lane == 0 && ex == -1) p.seq_len[b] = 0;
-        if (lane == 0 && p.status && (leave || want <= held))
-            p.status[b] = want < 0 ? MARS_SEQ_NO_ROOM : MARS_SEQ_OK;
     }
     __threadfence();
     cluster_barrier();
     if (blockIdx.x != 0) return;
 
     for (int b = threadIdx.x; b < p.n; b += kPoolThreads) {
-        const int held = min(max(__ldcg(p.seq_pages + b), 0), p.table_width);
-        const int ex = p.extra[b];
-        int want = held;
-        if (ex >= 0) {
-            const int64_t pages = ((int64_t)max(__ldcg(p.seq_len + b), 0) + ex + p.page_size - 1) >> p.page_log2;
-            if (pages <= p.table_width) want = (int)pages;
-        }
+        const int ex = p.extra[b], pages = __ldcg(p.seq_pages + b), len = __ldcg(p.seq_len + b);
+        const int held = min(max(pages, 0), p.table_width), want = ex >= 0 ? resize_want(p, ex, len, held) : held;
         s_first[b] = max(want - held, 0);
     }
     __syncthreads();
@@ -518,7 +612,7 @@ __global__ void __cluster_dims__(kPoolCluster, 1, 1) __launch_bounds__(kPoolThre
         taken = s_first[i];
         // rank `have` may be the first of request i, or inside it; in both cases i is not served
     }
-    take_free(p.bits, words, taken, s_warp, [&](int rank, int page) {
+    take_free(p.bits, words, taken, &s_free, [&](int rank, int page) {
         if (page >= p.num_pages) return;
         const int i = owner_of(s_first, p.n, rank);
         const int held = min(max(__ldcg(p.seq_pages + i), 0), p.table_width);
@@ -544,6 +638,7 @@ __global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams 
     pdl_wait();
     extern __shared__ int s_first[];   // [n]
     __shared__ int s_warp[32];
+    __shared__ FreeTile s_free;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kWarps = kPoolThreads / 32;
     // 1. what is wrong with a pair taken by itself (a warp per pair); sources as they stand
@@ -552,13 +647,16 @@ __global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams 
         bool ok = (unsigned)s < (unsigned)p.seqs && (unsigned)d < (unsigned)p.seqs && s != d;
         int len = 0;
         if (ok) {
-            const int held = p.seq_pages[s];
+            const int held = p.seq_pages[s], there = p.seq_pages[d];
             len = p.seq_len[s];
             const int64_t pages = ((int64_t)len + p.page_size - 1) >> p.page_log2;
-            ok = len >= 0 && pages <= held && pages <= p.table_width && p.seq_pages[d] == 0;
-            if (ok)
+            ok = len >= 0 && pages <= held && pages <= p.table_width && there == 0;
+            if (ok) {
+                const int32_t *row = p.table + (int64_t)s * p.table_width;
+#pragma unroll 4
                 for (int c = lane; c < (int)pages; c += 32)
-                    if ((unsigned)p.table[(int64_t)s * p.table_width + c] >= (unsigned)p.num_pages) ok = false;
+                    if ((unsigned)row[c] >= (unsigned)p.num_pages) ok = false;
+            }
         }
         ok = __all_sync(0xffffffffu, ok);
         if (lane == 0) p.status[i] = !ok ? MARS_SEQ_BAD_FORK : len == 0 ? kForkEmpty : MARS_SEQ_OK;
@@ -583,7 +681,7 @@ __global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams 
     const int have = total ? count_free(p.bits, words, total, s_warp) : 0;
     auto need_of = [&](int i) { return (i + 1 < p.n ? s_first[i + 1] : total) - s_first[i]; };
     const int taken = min(have, total);    // needs are 0 or 1: every rank below `have` ends its request
-    take_free(p.bits, words, taken, s_warp, [&](int rank, int page) {
+    take_free(p.bits, words, taken, &s_free, [&](int rank, int page) {
         if (page >= p.num_pages) return;
         const int i = owner_of(s_first, p.n, rank);
         const int len = p.seq_len[p.src[i]];
@@ -609,6 +707,7 @@ __global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams 
         }
         const int len = p.seq_len[s], full = len >> p.page_log2;
         __syncwarp();
+#pragma unroll 4
         for (int c = lane; c < full; c += 32) {
             const int id = p.table[(int64_t)s * p.table_width + c];
             p.table[(int64_t)d * p.table_width + c] = id;
@@ -719,10 +818,11 @@ mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void
     p.src[0] = (const unsigned char *)k; p.src[1] = (const unsigned char *)v;
     p.row[0] = k_row; p.row[1] = v_row; p.head[0] = k_head; p.head[1] = v_head;
     p.count = count; p.status = seq_status; p.N = N;
-    const int64_t threads = (int64_t)N * cache->kv_heads * 2 * (cache->head_dim / 16);
-    const int64_t blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffff) return MARS_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks, B);
+    const int es = elem_bytes(dt);
+    p.wide = !(((uintptr_t)k | (uintptr_t)v | (uintptr_t)(k_row * es) | (uintptr_t)(k_head * es) | (uintptr_t)(v_row * es) |
+                (uintptr_t)(v_head * es)) & 31);
+    const int rows = rows_at_once(cache->kv_heads * 2 * (cache->head_dim / 16)) * kRowIters;
+    const dim3 grid((unsigned)((N + rows - 1) / rows), B);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cache->head_dim == 128)
         return dt == MARS_BF16   ? kv_launch(kv_append_kernel<128, MARS_BF16>, grid, 256, 0, st, p)
@@ -799,14 +899,14 @@ mars_status_t mars_kv_gather(const mars_kv_cache_t *cache, int layer0, int layer
     if (!k_out || !v_out || B < 1 || B > cache->seqs || rows < 1 || layer0 < 0 || layers < 1 || layers > cache->layers - layer0)
         return MARS_ERR_INVALID_ARG;
     if (((uintptr_t)k_out & 15) || ((uintptr_t)v_out & 15)) return MARS_ERR_INVALID_ARG;
-    if (!kv_dtype_ok(dt) || rows > (1 << 30)) return MARS_ERR_UNSUPPORTED;
+    if (!kv_dtype_ok(dt) || rows > (1 << 24)) return MARS_ERR_UNSUPPORTED;
     GatherParams p;
     p.kv = kv_view(cache);
     p.layer0 = layer0; p.start = start; p.count = count; p.B = B; p.rows = rows;
     p.dst[0] = (unsigned char *)k_out; p.dst[1] = (unsigned char *)v_out;
-    const int64_t threads = (int64_t)rows * cache->kv_heads * 2 * (cache->head_dim / 16), blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffff) return MARS_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks, B, layers);
+    p.wide = !(((uintptr_t)k_out | (uintptr_t)v_out) & 31);
+    const int per_block = rows_at_once(cache->kv_heads * 2 * (cache->head_dim / 16)) * kRowIters;
+    const dim3 grid((unsigned)((rows + per_block - 1) / per_block), B, layers);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cache->head_dim == 128)
         return dt == MARS_BF16   ? kv_launch(kv_gather_kernel<128, MARS_BF16>, grid, 256, 0, st, p)
