@@ -7,16 +7,12 @@
 //   warps 20-27 softmax, two groups of four that take the key tiles in turn (thread = query row): score
 //               scale, mask, maximum, P back into tensor memory.  All of them bring Q into shared
 //               memory and write the result.
-//   warps 4-11  unpack K, 12-19 V: code * scale in fp16 from a ring into two stages of tiles
+//   warps 4-11  unpack K, 12-19 V: a warp fetches its 16 keys of every tile with 16-byte asynchronous copies
+//               (three tiles in flight), and writes code * scale in fp16 into two stages of tiles
 //               [128 keys][d] (128-byte swizzle)
 //   warp 0      tensor memory, and the MMAs: S = Q K^T (both operands in shared memory), O += P V (P in
 //               tensor memory over the columns of S; V's tile read with d as its leading dimension,
 //               so that neither K nor V is ever transposed)
-//   warps 1, 2  K and V blocks into their rings (six slots of 64 keys each) with 16-byte asynchronous
-//               copies.  Warps of their own: loads by the unpacking threads would be waited for by the
-//               proxy fence that hands each tile to the tensor cores (measured: half of their time).
-//               Not bulk copies: a block's K is 1024 + 128 bytes, and eight such copies from the lanes
-//               of one warp took 1500 cycles to issue, which bounded the kernel.
 //
 // Bounds per 128 keys and SM: MMA 1024 cycles, exponentials (16 a cycle) 1024, unpacking about 700 on
 // the same pipes as the rest of the softmax.  What it takes to get near them is that no step waits for
@@ -29,7 +25,9 @@
 // The groups share the running maximum: a group loads and reduces its scores while the other one is at
 // its exponentials, and only the decision on the maximum is passed from tile to tile.
 //
-// Each role walks the block's segments by itself; loaders, unpacking and MMA run ahead into the next one.
+// Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
+// (Loading by warps of their own was tried: issuing the copies of 64 keys took such a warp 500 to 1500
+// cycles beside the others, with bulk copies as with these, and bounded the kernel.)
 //
 // Every wait is bounded.  One that gives up raises the block's abort flag; all roles fall through to
 // the common end, the sequence's status becomes MARS_SEQ_TIMEOUT, tensor memory is freed.
@@ -46,19 +44,20 @@ namespace mars {
 constexpr int kTileThreads = 896;
 constexpr int kSoftThreads = 256;
 constexpr int kTileKeys = 128;
-constexpr int kHalfKeys = 64;                          // keys of a ring slot
-constexpr int kRingSlots = 6;
+constexpr int kUnpackWarps = 8;                        // per K and V: 16 keys each
+constexpr int kRing = 3;                               // tiles in flight per warp
 constexpr int kBufs = 3;                               // S buffers
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kColO = 384;                        // S buffer i at 128 i, then O
 
 template <int D> constexpr uint32_t tile_bytes() { return 128u * D * 2; }    // 128 rows of d fp16
-template <int D> constexpr uint32_t slot_bytes() { return (kHalfKeys / kKvBlock) * 9 * D; }    // codes [4][8d], scales [4][d]
+template <int D> constexpr uint32_t slot_bytes() { return 9 * D; }           // a block's K or V: codes [16][d/2], scales [16][d/16]
+template <int D> constexpr uint32_t ring_bytes() { return 2 * kUnpackWarps * kRing * slot_bytes<D>(); }
 template <int D> constexpr int tile_slot_floats() { return TileShape::M * (D + 2); }
 
 constexpr int kMaskWords = kTileMaxTree / 32;
 
-// shared memory: Q | K (2 stages) | V (2 stages) | ring of K | ring of V | the rest
+// shared memory: Q | K (2 stages) | V (2 stages) | rings of the unpacking warps | the rest
 struct TileSmem {
     uint32_t mask[kTileMaxTree * kMaskWords];
     int par[kTileMaxTree];
@@ -66,9 +65,7 @@ struct TileSmem {
     AttnSeqs seqs;
     float xch[2][128];                                  // [group][row]: largest of q's halves; sums
     float mref[2][128];                                 // [group][row]: the maximum as its last tile left it
-    int page[2][kRingSlots][4];                         // of a slot's blocks: -1 not in the pool, -2 no key
     uint64_t kfull[2], kempty[2], vfull[2], vempty[2], sfull[kBufs], pfull[kBufs], odone[kBufs];
-    uint64_t rfull[2][kRingSlots], rempty[2][kRingSlots];
     uint64_t chain[4][2];                               // [quarter of the rows][group]: maximum decided
     uint64_t qfull, drain;
     uint32_t tmem;
@@ -78,7 +75,7 @@ struct TileSmem {
 
 template <int D> constexpr size_t tile_smem_bytes()
 {
-    const size_t need = 1024 + 5 * (size_t)tile_bytes<D>() + 2 * kRingSlots * slot_bytes<D>() + sizeof(TileSmem);
+    const size_t need = 1024 + 5 * (size_t)tile_bytes<D>() + ring_bytes<D>() + sizeof(TileSmem);
     return need > 120 * 1024 ? need : 120 * 1024;      // one block per SM: each takes all of tensor memory
 }
 static_assert(tile_smem_bytes<128>() <= 227 * 1024 - 1024, "shared memory of one SM, with room for the static part");
@@ -130,12 +127,6 @@ __device__ __forceinline__ void cp_async16_to(uint32_t dst, const void *src)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-// Arrives on the barrier (without raising its count) once this thread's copies so far have landed.
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar)
-{
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
@@ -197,81 +188,27 @@ __device__ __forceinline__ TileSegment tile_segment(const AttnParams &p, const T
     return s;
 }
 
-// ------------------------------------------------------------------------------------- warps 1, 2
-
-template <int D>
-__device__ __forceinline__ void tile_load(const AttnParams &p, AttnRange r, TileSmem *sh, uint32_t ring, int v)
-{
-    const int lane = threadIdx.x & 31;
-    volatile int *abort_flag = &sh->abort;
-    uint64_t *full = sh->rfull[v], *empty = sh->rempty[v];
-    uint32_t slot = 0, phase = 0;
-    bool ok = true;
-    constexpr int kPer = D / 64;             // instructions of 32 x 16 bytes for a block's codes
-    constexpr int kScl = D / 16;             // 16-byte pieces of a block's scales
-    for (int64_t u = r.begin; u < r.end && ok;) {
-        const TileSegment sg = tile_segment(p, sh, r, u);
-        const int halves = 2 * sg.tiles, valid = sg.len + sg.n;     // keys from `valid` on were never written
-        // lane 4h + c: page id of block c of half tile h0 + h, and from it where that block's K or V begins
-        auto ids_from = [&](int h0) {
-            const int hh = h0 + (lane >> 2), pos = sg.key0 + hh * kHalfKeys + (lane & 3) * kKvBlock;
-            return hh < halves && pos < valid ? kv_page_id(p.kv, sg.b, pos) : -2;
-        };
-        int next = ids_from(0);
-        for (int h0 = 0; h0 < halves && ok; h0 += 8) {
-            const int ids = next;
-            next = ids_from(h0 + 8);
-            uint64_t src = 0;
-            if (ids >= 0)
-                src = (uint64_t)(kv_block<D>(p.kv, p.layer, ids, sg.head, sg.key0 + (h0 + (lane >> 2)) * kHalfKeys + (lane & 3) * kKvBlock) + v * 8 * D);
-#pragma unroll 1
-            for (int h = 0; h < min(8, halves - h0); ++h) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[slot]), phase ^ 1u, abort_flag, &sh->word));
-                if (!ok) break;
-                const uint32_t dst = ring + slot * slot_bytes<D>() + lane * 16, bar = smem_u32(&full[slot]);
-                if ((lane >> 2) == h) sh->page[v][slot][lane & 3] = ids;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint64_t at = __shfl_sync(0xffffffffu, src, 4 * h + c);
-                    if (at) {
-#pragma unroll
-                        for (int i = 0; i < kPer; ++i)
-                            cp_async16_to(dst + c * 8 * D + i * 512, (const unsigned char *)at + lane * 16 + i * 512);
-                    }
-                }
-                const uint64_t at = __shfl_sync(0xffffffffu, src, 4 * h + ((lane / kScl) & 3));
-                if (at && lane < 4 * kScl)
-                    cp_async16_to(dst + 32 * D, (const unsigned char *)at + 16 * D - v * 7 * D + (lane % kScl) * 16);
-                cp_async_arrive(bar);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar);                            // the page ids are written
-                if (++slot == kRingSlots) { slot = 0; phase ^= 1u; }
-            }
-        }
-        u += sg.unit1 - sg.unit0;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");         // nothing in flight when the block ends
-}
-
 // ------------------------------------------------------------------------------------- warps 4-19
 
-// One key's codes (this thread's part of them) from a ring slot into row `key` of a tile, in = its place
-// in the slot.  Two threads per key; chunks of 32 codes, the order of a row's halves alternating with
-// the key so that both the reads (rows d/2 bytes apart) and the swizzled writes are free of bank conflicts.
+// A warp's 16 keys of K or V from its ring slot into rows key0 .. key0 + 15 of a tile: two threads per key,
+// chunks of 32 codes, the order of a row's halves alternating with the key so that both the reads
+// (rows d/2 bytes apart) and the swizzled writes are free of bank conflicts.  have: the slot holds the
+// block and the key was written; else zeros, and `scale` for its scales.
 template <int D>
-__device__ __forceinline__ void tile_unpack(const unsigned char *slot, int in, int key, int page, unsigned char *tile, int v)
+__device__ __forceinline__ void tile_unpack(const unsigned char *slot, int key0, bool have, uint32_t scale, unsigned char *tile)
 {
     constexpr int kN = D / 64;
-    const unsigned char *blk = slot + in * (D / 2), *scl = slot + 32 * D + in * (D / 16);
-    const int odd = threadIdx.x & 1, swap = D == 128 ? (in >> 1) & 1 : 0;
+    const int lane = threadIdx.x & 31, in = lane >> 1, odd = lane & 1, key = key0 + in;
+    const int swap = D == 128 ? (in >> 1) & 1 : 0;
+    const unsigned char *blk = slot + in * (D / 2), *scl = slot + 8 * D + in * (D / 16);
     uint4 c[kN];
     uint32_t s[kN];
 #pragma unroll
     for (int a = 0; a < kN; ++a) {
         const int part = ((a ^ swap) << 1) | odd;
         c[a] = make_uint4(0u, 0u, 0u, 0u);
-        s[a] = v && page == -1 ? 0x7f7fu : 0u;                   // no such page: NaN
-        if (page >= 0) {
+        s[a] = scale;
+        if (have) {
             c[a] = *reinterpret_cast<const uint4 *>(blk + part * 16);
             s[a] = *reinterpret_cast<const unsigned short *>(scl + part * 2);
         }
@@ -293,40 +230,70 @@ __device__ __forceinline__ void tile_unpack(const unsigned char *slot, int in, i
     }
 }
 
-// K (v = 0) or V (v = 1): eight warps each, four for either half of a tile.
+// K (v = 0) or V (v = 1); w: which 16 keys of a tile.  A tile's copies are one group of the warp's, in
+// order over all segments, so the ring needs no barriers.
 template <int D>
 __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange r, TileSmem *sh, unsigned char *tiles,
-                                                 const unsigned char *ring, int v)
+                                                 unsigned char *ring, int v, int w)
 {
-    const int lane = threadIdx.x & 31, key = ((threadIdx.x - 128) & 255) >> 1, in = key & 63;
-    const uint32_t half = key >> 6;
+    const int lane = threadIdx.x & 31;
     volatile int *abort_flag = &sh->abort;
     uint64_t *full = v ? sh->vfull : sh->kfull, *empty = v ? sh->vempty : sh->kempty;
-    uint32_t n = 0, slot = half, phase = 0;
+    const uint32_t ring_u32 = smem_u32(ring) + lane * 16;
+    constexpr uint64_t kNoPage = 1;          // address that stands for a page outside the pool; 0: no key
+    uint32_t n = 0, at = 0, put = 0;         // tiles unpacked; ring slots to read and to fill next
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) {
-        return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, abort_flag, &sh->word)) != 0;
-    };
     for (int64_t u = r.begin; u < r.end && ok;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
-        const int valid = sg.len + sg.n;
+        const int valid = sg.len + sg.n, first = sg.key0 + w * kKvBlock;   // keys from `valid` on were never written
+        // lane i: where the warp's block of tile i0 + i is
+        auto locate = [&](int i0) -> uint64_t {
+            const int pos = first + (i0 + lane) * kTileKeys;
+            if (i0 + lane >= sg.tiles || pos >= valid) return 0;
+            const int id = kv_page_id(p.kv, sg.b, pos);
+            return id < 0 ? kNoPage : (uint64_t)(kv_block<D>(p.kv, p.layer, id, sg.head, pos) + v * 8 * D);
+        };
+        uint64_t here = locate(0), next = sg.tiles > 32 ? locate(32) : 0;
+        auto issue = [&](int t) {            // tile t of the segment, 32 tiles of addresses from t & ~31 in `here`
+            if (t < sg.tiles) {
+                const uint64_t from = __shfl_sync(0xffffffffu, here, t & 31);
+                if (from > kNoPage) {
+                    const unsigned char *src = (const unsigned char *)from + lane * 16;
+                    const uint32_t dst = ring_u32 + put * slot_bytes<D>();
+#pragma unroll
+                    for (int i = 0; i < D / 64; ++i) cp_async16_to(dst + i * 512, src + i * 512);
+                    // the scales follow K's codes by 16d bytes, V's by 9d
+                    if (lane < D / 16) cp_async16_to(dst + 8 * D, src + 16 * D - v * 7 * D);
+                }
+                put = put == kRing - 1 ? 0u : put + 1;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        uint64_t seen = here;                // addresses of the tiles being unpacked (issue runs ahead)
+#pragma unroll
+        for (int t = 0; t < kRing - 1; ++t) issue(t);
         for (int t = 0; t < sg.tiles; ++t, ++n) {
+            if ((t & 31) == 0) seen = here;
+            const uint64_t from = __shfl_sync(0xffffffffu, seen, t & 31);
+            if (((t + kRing - 1) & 31) == 0) { here = next; next = locate(t + kRing - 1 + 32); }
+            issue(t + kRing - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            __syncwarp();
             const uint32_t st = n & 1u;
-            ok = wait(&sh->rfull[v][slot], phase) && wait(&empty[st], ((n >> 1) & 1u) ^ 1u);
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[st]), ((n >> 1) & 1u) ^ 1u, abort_flag, &sh->word)) != 0;
             if (!ok) break;
-            int page = sh->page[v][slot][in >> 4];
-            if (sg.key0 + t * kTileKeys + key >= valid) page = -2;               // slot never written
-            tile_unpack<D>(ring + slot * slot_bytes<D>(), in, key, page, tiles + st * tile_bytes<D>(), v);
+            const bool have = from > kNoPage && first + t * kTileKeys + (lane >> 1) < valid;
+            // V of a page outside the pool: NaN
+            tile_unpack<D>(ring + at * slot_bytes<D>(), w * kKvBlock, have, v && from == kNoPage ? 0x7f7fu : 0u, tiles + st * tile_bytes<D>());
+            at = at == kRing - 1 ? 0u : at + 1;
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) { mbar_arrive(smem_u32(&full[st])); mbar_arrive(smem_u32(&sh->rempty[v][slot])); }
-            slot += 2;
-            if (slot >= kRingSlots) { slot -= kRingSlots; phase ^= 1u; }
+            if (lane == 0) mbar_arrive(smem_u32(&full[st]));
         }
         u += sg.unit1 - sg.unit0;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");         // nothing in flight when the block ends
 }
-static_assert(kRingSlots % 2 == 0, "a half tile keeps to its slots");
 
 // ------------------------------------------------------------------------------------- warp 0
 
@@ -699,7 +666,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
     unsigned char *sm = smem_raw + (base - raw);
     constexpr uint32_t kT = tile_bytes<D>();
     unsigned char *ring = sm + 5 * kT;
-    TileSmem *sh = reinterpret_cast<TileSmem *>(ring + 2 * kRingSlots * slot_bytes<D>());
+    TileSmem *sh = reinterpret_cast<TileSmem *>(ring + ring_bytes<D>());
     const int tid = threadIdx.x, warp = tid >> 5;
 
     const AttnRange r = attn_split<TileShape, kTileThreads>(p, &sh->seqs);
@@ -709,10 +676,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
             mbar_init(smem_u32(&sh->vfull[i]), 8);
             mbar_init(smem_u32(&sh->kempty[i]), 1);
             mbar_init(smem_u32(&sh->vempty[i]), 1);
-            for (int k = 0; k < kRingSlots; ++k) {
-                mbar_init(smem_u32(&sh->rfull[i][k]), 33);
-                mbar_init(smem_u32(&sh->rempty[i][k]), 4);
-            }
             for (int k = 0; k < 4; ++k) mbar_init(smem_u32(&sh->chain[k][i]), 1);
         }
         for (int i = 0; i < kBufs; ++i) {
@@ -742,12 +705,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
         tile_softmax<D, DT>(p, r, sh, tmem, sm);
     } else if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        const int v = warp >= 12;
-        tile_unpack_role<D>(p, r, sh, sm + (v ? 3 : 1) * kT, ring + v * kRingSlots * slot_bytes<D>(), v);
+        const int v = warp >= 4 + kUnpackWarps;
+        tile_unpack_role<D>(p, r, sh, sm + (v ? 3 : 1) * kT, ring + (warp - 4) * kRing * slot_bytes<D>(), v, (warp - 4) & (kUnpackWarps - 1));
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) tile_mma<D>(p, r, sh, tmem, base, base + kT, base + 3 * kT);
-        else if (warp < 3) tile_load<D>(p, r, sh, smem_u32(ring) + (warp - 1) * kRingSlots * slot_bytes<D>(), warp - 1);
     }
 
     tc_fence_before();
