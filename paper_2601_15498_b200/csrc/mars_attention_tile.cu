@@ -10,7 +10,7 @@
 //   warps 4-11  unpack K, 12-19 V: a warp fetches its 16 keys of every tile with 16-byte asynchronous copies
 //               (three tiles in flight), and writes code * scale in fp16 into two stages of tiles
 //               [128 keys][d] (128-byte swizzle)
-//   warp 0      tensor memory, and the MMAs: S = Q K^T (both operands in shared memory), O += P V (P in
+//   warp 3      tensor memory, and the MMAs: S = Q K^T (both operands in shared memory), O += P V (P in
 //               tensor memory over the columns of S; V's tile read with d as its leading dimension,
 //               so that neither K nor V is ever transposed)
 //
@@ -295,7 +295,7 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
     asm volatile("cp.async.wait_all;" ::: "memory");         // nothing in flight when the block ends
 }
 
-// ------------------------------------------------------------------------------------- warp 0
+// ------------------------------------------------------------------------------------- warp 3
 
 template <int D>
 __device__ __forceinline__ void tile_mma(const AttnParams &p, AttnRange r, TileSmem *sh, uint32_t tmem_any, uint32_t q_at,
@@ -373,23 +373,20 @@ __device__ __forceinline__ float max32(const float *v)
     for (int k = 4; k < 32; k += 4) { a = max3(a, v[k], v[k + 1]); b = max3(b, v[k + 2], v[k + 3]); }
     return fmaxf(a, b);
 }
-// P of 32 scores into 16 columns; adds them to l2.
-__device__ __forceinline__ void exp32(float *v, float rs, float minus, uint32_t at, float (&l2)[2])
+// P of 64 scores into 32 columns; adds them to l4.
+__device__ __forceinline__ void exp64(float *v, float rs, float minus, uint32_t at, float (&l4)[4])
 {
+    uint32_t h[32];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t h[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            float &a = v[16 * c + 2 * k], &b = v[16 * c + 2 * k + 1];
-            fma2(a, b, rs, minus);
-            a = ex2(a);
-            b = ex2(b);
-            add2(l2[0], l2[1], a, b);
-            h[k] = f16x2_from(a, b);
-        }
-        tc_st8(at + c * 8, h);
+    for (int k = 0; k < 32; ++k) {
+        float &a = v[2 * k], &b = v[2 * k + 1];
+        fma2(a, b, rs, minus);
+        a = ex2(a);
+        b = ex2(b);
+        add2(l4[2 * (k & 1)], l4[2 * (k & 1) + 1], a, b);
+        h[k] = f16x2_from(a, b);
     }
+    tc_st32(at, h);
 }
 
 template <int D, int DT>
@@ -541,9 +538,8 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             }
             // P = 2^(s - mref + 7), see mars_attention.cu; over columns of S that were read for good
             const float minus = mref == -INFINITY ? 0.0f : 7.0f - mref;
-            float l2[2] = {0.0f, 0.0f};
-            exp32(v, rs, minus, sc, l2);
-            exp32(v + 32, rs, minus, sc + 16, l2);
+            float l4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            exp64(v, rs, minus, sc, l4);
             tc_ld32_issue(sc + 64, v);
             tc_ld32_issue(sc + 96, v + 32);
             tc_ld32_wait(v);
@@ -552,9 +548,8 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                 mask32(v, visible32(pos0 + 64, sg.len, node, tree, mask, words));
                 mask32(v + 32, visible32(pos0 + 96, sg.len, node, tree, mask, words));
             }
-            exp32(v, rs, minus, sc + 32, l2);
-            exp32(v + 32, rs, minus, sc + 48, l2);
-            l += l2[0] + l2[1];
+            exp64(v, rs, minus, sc + 32, l4);
+            l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -709,7 +704,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
         tile_unpack_role<D>(p, r, sh, sm + (v ? 3 : 1) * kT, ring + (warp - 4) * kRing * slot_bytes<D>(), v, (warp - 4) & (kUnpackWarps - 1));
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == 0) tile_mma<D>(p, r, sh, tmem, base, base + kT, base + 3 * kT);
+        if (warp == 3) tile_mma<D>(p, r, sh, tmem, base, base + kT, base + 3 * kT);
     }
 
     tc_fence_before();
