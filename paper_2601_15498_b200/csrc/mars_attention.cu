@@ -37,7 +37,7 @@ constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
 constexpr int kRowsMax = 32;          // largest tile
 constexpr int rows_occ(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }   // blocks per SM (registers)
 constexpr int rows_grid(int rows) { return kAttnSms * rows_occ(rows); }
-constexpr int kUnit = 64;             // RowsShape::unit_keys
+constexpr int kUnit = RowsShape<8>::kUnit;
 constexpr float kNone = 1e30f;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
     AttnRange r = attn_split<Shape, kRowsThreads>(p, &s_seqs);
     for (int64_t u = r.begin; u < r.end;) {
         const AttnSegment sg = attn_segment<Shape>(p, &s_seqs, r, u);
+        if (sg.unit0 >= sg.unit1) { u += sg.span; continue; }
         const bool whole = sg.unit0 == 0 && sg.unit1 == sg.units;
         const int rows = min(kRows, sg.n * p.group - sg.tile * kRows);
         const int row0 = sg.tile * kRows;                // first row of the tile: node row0/group
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
         // each thread: kPer values of d of a row, kPass rows of the tile one after the other
         constexpr int kPer = 8, kAcross = D / kPer, kAtOnce = kRowsThreads / kAcross;
         bool write = whole;
-        const int c0 = (int)(sg.item / r.per), c1 = (int)((sg.item + sg.units - 1) / r.per);
+        const int c0 = sg.c0, c1 = sg.c1;
         auto slot_of = [&](int c) { return p.partial + (int64_t)(2 * c + (r.per * c >= sg.item ? 0 : 1)) * rows_slot_floats<D>(kRows); };
         const int od = (tid % kAcross) * kPer;
         auto emit = [&](int orow, float (&acc)[kPer], float sum) {
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
             }
         }
         __syncthreads();                                  // masks, ring and sums free for the next segment
-        u += sg.unit1 - sg.unit0;
+        u += sg.span;
     }
 }
 

@@ -20,15 +20,18 @@
 
 namespace mars {
 
-// Tile shapes: query rows per tile and keys per unit of the split.
+// Tile shapes: query rows per tile, keys per unit of the split, and what an item costs besides its keys
+// (decoding, Q, masks, the pipeline's fill and drain, the result) in units.  Counting that in evens out
+// the blocks where items are short.  Measured, us at 0 / this / twice this: 64 trees 485 / 437 / 446,
+// four prompts 200 / 147 / 156 (TileShape); 64 tokens 115 / 105 / 109, 64 chains 232 / 202 / 212.
 template <int kRows>
 struct RowsShape {
     static constexpr int M = kRows;
-    static __host__ __device__ constexpr int unit_keys(int) { return 64; }
+    static constexpr int kUnit = 64, kFixed = kRows == 32 ? 8 : 6;
 };
 struct TileShape {
     static constexpr int M = 128;
-    static __host__ __device__ constexpr int unit_keys(int) { return 128; }
+    static constexpr int kUnit = 128, kFixed = 7;
 };
 
 struct AttnParams {
@@ -88,11 +91,18 @@ __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, in
     return len + min(n, attn_node(p, (mt + 1) * S::M - 1) + 1);
 }
 
+// Units of an item: its fixed cost, then its keys.
 template <class S>
 __device__ __forceinline__ int attn_units(const AttnParams &p, int len, int n, int mt)
 {
-    const int uk = S::unit_keys(attn_tile_rows<S>(p, n, mt));
-    return (attn_keys<S>(p, len, n, mt) + uk - 1) / uk;
+    return S::kFixed + (attn_keys<S>(p, len, n, mt) + S::kUnit - 1) / S::kUnit;
+}
+
+// a / b for a >= 0, b > 0; nearly always in 32 bits, where it takes a third of the time.
+__device__ __forceinline__ int64_t attn_div(int64_t a, int64_t b)
+{
+    if (((uint64_t)a | (uint64_t)b) >> 32 == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
 }
 
 // Units of one KV head of a sequence; whole warps call (lanes share the tiles of a long chain).
@@ -139,9 +149,10 @@ __device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
     const int chunk = (p.B + of - 1) / of;
     const int lo = min(who * chunk, p.B), hi = min(lo + chunk, p.B);
     int64_t sum = 0;
+    int len = 0, n = 0;           // of the last sequence of the chunk; with one per chunk nothing is read twice
     for (int b = lo; b < hi; ++b) {
-        int len, st;
-        const int n = attn_nodes(p, b, &len, &st);
+        int st;
+        n = attn_nodes(p, b, &len, &st);
         sum += attn_head_units<S>(p, len, n) * p.kv.kv_heads;
         if (n == 0 && p.status && blockIdx.x == 0) p.status[b] = st;
     }
@@ -162,31 +173,42 @@ __device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
         total += s_sum[w];
     }
     AttnRange r;
-    r.per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    r.per = max(attn_div(total + gridDim.x - 1, gridDim.x), (int64_t)1);
     r.begin = min(r.per * blockIdx.x, total);
     r.end = min(r.begin + r.per, total);
     int64_t at = before + inc - sum;
     if (by_warp) at = __shfl_sync(0xffffffffu, at, 0);
     if (r.begin < r.end && at <= r.begin && r.begin < at + chunk_sum) {
-        for (int b = lo; b < hi; ++b) {
-            int len, st;
-            const int n = attn_nodes(p, b, &len, &st);
-            const int64_t u = attn_head_units<S>(p, len, n) * p.kv.kv_heads;
-            if (r.begin < at + u) { s_b = b; s_at = at; break; }
-            at += u;
+        if (chunk == 1) {
+            s_b = lo;
+            s_at = at;
+        } else {
+            for (int b = lo; b < hi; ++b) {
+                int st;
+                n = attn_nodes(p, b, &len, &st);
+                const int64_t u = attn_head_units<S>(p, len, n) * p.kv.kv_heads;
+                if (r.begin < at + u) { s_b = b; s_at = at; break; }
+                at += u;
+            }
         }
     }
     __syncthreads();
-    r.b = s_b;
+    r.b = r.b0 = s_b;
     r.at = s_at;
-    r.b0 = s_b;
     if (r.begin < r.end) {
-        // whole warps where lanes share a sequence's tiles, else a lane per sequence
-        for (int i = by_warp ? warp : tid; i < kSeqCache && r.b0 + i < p.B; i += by_warp ? kThreads / 32 : kThreads) {
-            int len, st;
-            const int n = attn_nodes(p, r.b0 + i, &len, &st);
-            const int64_t u = attn_head_units<S>(p, len, n);
-            seqs->units[i] = u; seqs->len[i] = len; seqs->n[i] = n;
+        if (chunk == 1) {
+            const int i = lo - r.b0;
+            if (lo < hi && i >= 0 && i < kSeqCache) {
+                seqs->units[i] = attn_div(chunk_sum, p.kv.kv_heads); seqs->len[i] = len; seqs->n[i] = n;
+            }
+        } else {
+            // whole warps where lanes share a sequence's tiles, else a lane per sequence
+            for (int i = by_warp ? warp : tid; i < kSeqCache && r.b0 + i < p.B; i += of) {
+                int st;
+                n = attn_nodes(p, r.b0 + i, &len, &st);
+                const int64_t u = attn_head_units<S>(p, len, n);
+                seqs->units[i] = u; seqs->len[i] = len; seqs->n[i] = n;
+            }
         }
     }
     __syncthreads();
@@ -197,8 +219,10 @@ __device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
 struct AttnSegment {
     int b, head, tile;
     int len, n, keys;        // committed tokens, nodes, keys of the tile
-    int unit0, unit1;        // this block's units of the item, of `units`
+    int unit0, unit1;        // this block's units of keys, of `units`; none if unit0 >= unit1
     int units;
+    int64_t span;            // units on from here to the next segment
+    int c0, c1;              // first and last block with keys of the item
     int64_t item;            // first unit of the item in the whole batch
 };
 
@@ -223,16 +247,16 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, const A
     }
     s.b = r.b;
     const int64_t in_seq = u - r.at;
-    s.head = (int)(in_seq / hu);
+    s.head = (int)attn_div(in_seq, hu);
     int64_t rest = in_seq - s.head * hu;
-    s.item = r.at + s.head * hu;
+    int64_t item = r.at + s.head * hu;       // first unit of the item in the whole batch
     s.tile = 0;
     s.units = attn_units<S>(p, s.len, s.n, 0);
     if (p.parent) {
         const int last = attn_tiles<S>(p, s.n) - 1;
-        s.tile = (int)min(rest / s.units, (int64_t)last);
+        s.tile = (int)min(attn_div(rest, s.units), (int64_t)last);
         rest -= (int64_t)s.tile * s.units;
-        s.item += (int64_t)s.tile * s.units;
+        item += (int64_t)s.tile * s.units;
         if (s.tile == last) s.units = attn_units<S>(p, s.len, s.n, last);
     } else {
         // lanes look at 32 tiles at a time for the one that holds unit `rest`
@@ -253,18 +277,23 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, const A
                     s.units = (int)__shfl_sync(0xffffffffu, mine, l);
                     const int64_t skip = __shfl_sync(0xffffffffu, inc - mine, l);
                     rest -= skip;
-                    s.item += skip;
+                    item += skip;
                     break;
                 }
                 const int64_t all = __shfl_sync(0xffffffffu, inc, 31);
                 rest -= all;
-                s.item += all;
+                item += all;
             }
         }
     }
     s.keys = attn_keys<S>(p, s.len, s.n, s.tile);
-    s.unit0 = (int)rest;
-    s.unit1 = (int)min((int64_t)s.units, rest + (r.end - u));
+    s.span = min((int64_t)s.units - rest, r.end - u);
+    s.unit0 = max((int)rest - S::kFixed, 0);
+    s.unit1 = max((int)(rest + s.span) - S::kFixed, 0);
+    s.units -= S::kFixed;
+    s.c0 = (int)attn_div(item + S::kFixed, r.per);
+    s.c1 = (int)attn_div(item + S::kFixed + s.units - 1, r.per);
+    s.item = item;
     return s;
 }
 

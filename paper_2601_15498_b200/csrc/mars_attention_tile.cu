@@ -183,7 +183,7 @@ __device__ __forceinline__ TileSegment tile_segment(const AttnParams &p, const T
     s.rows = attn_tile_rows<TileShape>(p, s.n, s.tile);
     s.row0 = s.tile * TileShape::M;
     s.key0 = s.unit0 * kTileKeys;
-    s.tiles = s.unit1 - s.unit0;
+    s.tiles = max(s.unit1 - s.unit0, 0);
     s.whole = s.tiles == s.units;
     return s;
 }
@@ -245,6 +245,7 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
     bool ok = true;
     for (int64_t u = r.begin; u < r.end && ok;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
+        if (sg.tiles == 0) { u += sg.span; continue; }
         const int valid = sg.len + sg.n, first = sg.key0 + w * kKvBlock;   // keys from `valid` on were never written
         // lane i: where the warp's block of tile i0 + i is
         auto locate = [&](int i0) -> uint64_t {
@@ -290,7 +291,7 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&full[st]));
         }
-        u += sg.unit1 - sg.unit0;
+        u += sg.span;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");         // nothing in flight when the block ends
 }
@@ -329,10 +330,12 @@ __device__ __forceinline__ void tile_mma(const AttnParams &p, AttnRange r, TileS
         sbuf = sbuf == kBufs - 1 ? 0u : sbuf + 1;
         return true;
     };
-    for (int64_t u = r.begin; u < r.end && ok; ++n_seg) {
+    for (int64_t u = r.begin; u < r.end && ok;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
+        if (sg.tiles == 0) { u += sg.span; continue; }
         const int tiles = __shfl_sync(0xffffffffu, sg.tiles, 0);
         ok = wait(&sh->qfull, n_seg & 1u);
+        ++n_seg;
         for (int t = 0; t < min(kBufs, tiles) && ok; ++t) ok = issue_s();
         for (int t = 0; t < tiles && ok; ++t) {
             ok = wait(&sh->vfull[vst], vpar) && wait(&sh->pfull[pbuf], ppar);
@@ -350,7 +353,7 @@ __device__ __forceinline__ void tile_mma(const AttnParams &p, AttnRange r, TileS
             else ++pbuf;
             if (t + kBufs < tiles) ok = issue_s();
         }
-        u += sg.unit1 - sg.unit0;
+        u += sg.span;
     }
     // all MMAs of this warp must retire before tensor memory is freed
     tc_commit_if(lead, smem_u32(&sh->drain));
@@ -406,6 +409,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
     };
     for (int64_t u = r.begin; u < r.end;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
+        if (sg.tiles == 0) { u += sg.span; continue; }
         const bool tree = p.parent != nullptr;
         const int words = (sg.n + 31) >> 5;
         const int node = rr < sg.rows ? attn_node(p, sg.row0 + rr) : -1;
@@ -600,7 +604,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             }
         }
         if (!sg.whole) {
-            const int c0 = (int)(sg.item / r.per), c1 = (int)((sg.item + sg.units - 1) / r.per);
+            const int c0 = sg.c0, c1 = sg.c1;
             __threadfence();
             softmax_sync();
             if (tid == 0) sh->last = atomicAdd(p.counters + c0, 1u) == (unsigned)(c1 - c0);
@@ -646,7 +650,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         tc_fence_before();
         softmax_sync();                   // masks, exchange arrays and O are free for the next segment
         tc_fence_after();
-        u += sg.unit1 - sg.unit0;
+        u += sg.span;
     }
 }
 
