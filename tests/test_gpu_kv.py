@@ -502,3 +502,132 @@ def test_cycle_in_a_captured_graph():
         pr.m.len[:], _ = pr.m.commit(host(path), host(acc))
         pr.tables()
         pr.stored()
+
+
+# ------------------------------------------------------------------------------------- edges of the split
+
+@pytest.mark.parametrize("N,group", [(1, 8), (1, 9), (4, 4), (1, 17), (8, 4), (11, 3), (1, 64), (1, 130), (32, 4), (43, 3)])
+def test_attention_at_the_borders_of_the_row_tiles(N, group):
+    """8, 9, 16, 17, 32, 33, 64, 128, 129 and 130 query rows per KV head: every kernel and its neighbour."""
+    pr = Pair(pages=60, heads=1, d=128, page=32, seqs=3, width=16, seed=N * group)
+    pr.grow([200, 31, 0])
+    pr.resize([N] * 3)
+    pr.append(3, N)
+    q = torch.randn((3, N, group, 128), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q)
+    check_attention(pr, q, parent=trees(np.random.default_rng(N), 3, N), count=[N, N, max(N // 2, 1)])
+
+
+@pytest.mark.parametrize("N", [128, 129])
+def test_attention_of_trees_at_the_border_of_the_mask_store(N):
+    pr = Pair(pages=40, heads=1, d=128, page=64, seqs=2, width=8, seed=N)
+    pr.grow([100, 1])
+    pr.resize([N] * 2)
+    pr.append(2, N)
+    q = torch.randn((2, N, 2, 128), device=DEV).to(torch.float16)
+    check_attention(pr, q, parent=trees(np.random.default_rng(N), 2, N, absent=0.05))
+
+
+@pytest.mark.parametrize("B,N", [(300, 1), (1000, 1), (1000, 40)])
+def test_attention_of_many_sequences_most_of_them_idle(B, N):
+    """More sequences than threads that split the work, and blocks whose share spans many idle ones."""
+    rng = np.random.default_rng(B)
+    pr = Pair(pages=2 * B * (1 + N // 32), heads=1, d=64, page=16, seqs=B, width=5, seed=B)
+    lens = [int(x) for x in rng.integers(0, 20, B)]
+    pr.resize([n + N for n in lens], check=False)
+    k = pr.rand(B, 20 + N, torch.bfloat16, loud=False)
+    pr.append(B, 20 + N, count=[n + N for n in lens], k=k, v=k.flip(-1).contiguous())
+    pr.m.len[:] = lens
+    pr.c.seq_len.copy_(i32(lens))
+    count = np.where(rng.uniform(0, 1, B) < 0.04, N, 0).astype(np.int32)
+    q = torch.randn((B, N, 2, 64), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, count=count)
+    if N == 1:
+        check_attention(pr, q)
+
+
+def test_attention_of_an_idle_batch_writes_nothing():
+    pr = Pair(pages=10, heads=2, d=64, page=16, seqs=3, width=4, seed=40)
+    pr.grow([20, 3, 0])
+    for N in (1, 40):
+        q = torch.randn((3, N, 4, 64), device=DEV).to(torch.bfloat16)
+        check_attention(pr, q, count=[0, -5, 0])
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Calls of both kernels in flight at once, on streams that nothing orders."""
+    prs, qs, ws, out, streams = [], [], [], [], []
+    for s in range(2):
+        pr = Pair(pages=200, heads=2, d=128, page=64, seqs=4, width=60, seed=50 + s)
+        pr.grow([500, 20, 130, 64])
+        pr.resize([33] * 4)
+        pr.append(4, 33)
+        q = torch.randn((4, 33 if s else 2, 8, 128), device=DEV).to(torch.bfloat16)
+        prs.append(pr), qs.append(q), ws.append(kv.attention_workspace(q, pr.c)), out.append(torch.zeros_like(q))
+        streams.append(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                kv.tree_attention(qs[s], prs[s].c, 0, out=out[s], workspace=ws[s])
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert torch.equal(out[s], check_attention(prs[s], qs[s]))
+
+
+def test_one_workspace_for_calls_of_different_sizes():
+    """The largest call's workspace serves the smaller ones, in any order."""
+    pr = Pair(pages=200, heads=2, d=64, page=32, seqs=3, width=60, seed=60)
+    pr.grow([900, 20, 130])
+    pr.resize([64] * 3)
+    pr.append(3, 64)
+    qs = [torch.randn((3, N, 8, 64), device=DEV).to(torch.bfloat16) for N in (64, 1, 3, 64, 5, 1)]
+    ws = kv.attention_workspace(qs[0], pr.c)
+    need = max(kv.attention_workspace_bytes(3, q.shape[1], 8, 2, 64) for q in qs)
+    ws = torch.zeros((need,), dtype=torch.uint8, device=DEV)
+    for q in qs:
+        check_attention(pr, q, workspace=ws)
+
+
+def test_append_rows_off_the_32_byte_grid_and_wide_heads():
+    """16-byte aligned rows that are not 32-byte aligned; more values in a row than a block has threads."""
+    pr = Pair(heads=20, d=128, page=16, seqs=2, width=4, pages=12, seed=70)
+    pr.resize([10, 10])
+    flat = torch.randn((2 * 10 * 41 * 128 + 8,), device=DEV).to(torch.bfloat16)
+    both = flat[8:].view(2, 10, 41, 128)
+    assert both.data_ptr() % 32 == 16
+    k, v = both[:, :, :20], both[:, :, 20:40]
+    pr.append(2, 10, k=k, v=v)
+    pr.m.len[:] = 10
+    pr.stored()
+    out = (torch.zeros((2 * 10 * 20 * 128 + 8,), dtype=torch.bfloat16, device=DEV)[8:].view(1, 2, 10, 20, 128),
+           torch.zeros((1, 2, 10, 20, 128), dtype=torch.bfloat16, device=DEV))
+    kv.gather(pr.c, 0, 1, i32([0, 0]), i32([10, 10]), out=out)
+    for got, want in zip(out, pr.m.rows(0, 1, 0, 10)):
+        assert np.array_equal(host(got)[0, 1], torch.as_tensor(want).float().to(torch.bfloat16).float().numpy())
+
+
+def test_quotients_on_every_border():
+    """x / (s * g) exactly between two codes, for every scale of a sixteen and many g: to the even code."""
+    rng = np.random.default_rng(80)
+    g = rng.uniform(0.01, 50.0, (1, 2, 64)).astype(np.float32)
+    g[0, 0, :32] = np.exp2(rng.integers(-8, 8, 32))
+    c = kv.KVCache.empty(1, 40, 64, 64, 16, 2, 20, DEV, scales=g)
+    m = ko.Model(1, 40, 64, 64, 16, 2, 20, g)
+    kv.resize(c, i32([300, 300]))
+    m.resize([300, 300])
+    mids = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    s = ko.E4M3[rng.integers(1, 127, (2, 300, 64, 4, 1))]
+    x = np.tile(mids, 2) * s * np.where(rng.uniform(0, 1, (2, 300, 64, 4, 16)) < 0.5, -1, 1)
+    x = (x * g[0, 0][None, None, :, None, None]).reshape(2, 300, 64, 64)
+    x = np.nextafter(x.astype(np.float32), np.where(rng.uniform(0, 1, x.shape) < 0.3, np.float32(np.inf), x.astype(np.float32)))
+    k = torch.as_tensor(x, device=DEV)
+    kv.append(c, 0, k, k)
+    m.append(0, x, x)
+    for b in range(2):
+        for pos in range(0, 300, 7):
+            p, slot = m.at(b, pos)
+            raw = host(c.pages)[0, p].reshape(64, 1, 18 * 64)[:, 0]
+            code = raw[:, slot * 32:(slot + 1) * 32]
+            assert np.array_equal(code & 15, m.code[0, p, slot, :, 0, 0::2]) and np.array_equal(code >> 4, m.code[0, p, slot, :, 0, 1::2])
+            assert np.array_equal(raw[:, 16 * 64 + slot * 4:16 * 64 + slot * 4 + 4], m.scale[0, p, slot, :, 0])
