@@ -37,7 +37,7 @@ constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
 constexpr int kRowsMax = 32;          // largest tile
 constexpr int rows_occ(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }   // blocks per SM (registers)
 constexpr int rows_grid(int rows) { return kAttnSms * rows_occ(rows); }
-constexpr int kUnit = RowsShape<8>::kUnit;
+constexpr int kUnit = RowsShape<8>::unit_keys(8);
 constexpr float kNone = 1e30f;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)

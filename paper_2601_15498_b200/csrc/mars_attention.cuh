@@ -27,11 +27,14 @@ namespace mars {
 template <int kRows>
 struct RowsShape {
     static constexpr int M = kRows;
-    static constexpr int kUnit = 64, kFixed = kRows == 32 ? 8 : 6;
+    static constexpr int kFixed = kRows == 32 ? 8 : 6;
+    static __host__ __device__ constexpr int unit_keys(int) { return 64; }
 };
 struct TileShape {
-    static constexpr int M = 128;
-    static constexpr int kUnit = 128, kFixed = 7;
+    static constexpr int M = 256;
+    static constexpr int kFixed = 6;
+    // up to 128 rows fill one of the kernel's two accumulators; the two then share the keys
+    static __host__ __device__ constexpr int unit_keys(int rows) { return rows > 128 ? 128 : 256; }
 };
 
 struct AttnParams {
@@ -95,7 +98,8 @@ __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, in
 template <class S>
 __device__ __forceinline__ int attn_units(const AttnParams &p, int len, int n, int mt)
 {
-    return S::kFixed + (attn_keys<S>(p, len, n, mt) + S::kUnit - 1) / S::kUnit;
+    const int uk = S::unit_keys(attn_tile_rows<S>(p, n, mt));
+    return S::kFixed + (attn_keys<S>(p, len, n, mt) + uk - 1) / uk;
 }
 
 // a / b for a >= 0, b > 0; nearly always in 32 bits, where it takes a third of the time.

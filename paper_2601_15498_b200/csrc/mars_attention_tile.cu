@@ -1,33 +1,28 @@
 // libmars: attention of draft nodes over the paged 4-bit cache, many query rows per KV head.
 //
 // The products run on tcgen05.mma (kind::f16, 128 x 128 x 16 steps, fp32 accumulators in tensor
-// memory); see mars_attention.cu for the arithmetic.  A tile is 128 query rows of one KV head; one
-// block per SM:
+// memory); see mars_attention.cu for the arithmetic.  Up to 256 query rows of one KV head -- a whole
+// tree of 60 nodes with four heads to a KV head -- share every key that is unpacked.  One block per SM:
 //
-//   warps 20-27 softmax, two groups of four that take the key tiles in turn (thread = query row): score
-//               scale, mask, maximum, P back into tensor memory.  All of them bring Q into shared
-//               memory and write the result.
+//   warps 20-27 softmax, four warps to an accumulator (thread = query row): Q into shared memory, score
+//               scale, mask, maximum, P back into tensor memory, the result
 //   warps 4-11  unpack K, 12-19 V: a warp fetches its 16 keys of every tile with 16-byte asynchronous copies
-//               (three tiles in flight), and writes code * scale in fp16 into two stages of tiles
-//               [128 keys][d] (128-byte swizzle)
+//               a tile ahead, and writes code * scale in fp16 into two stages of tiles [128 keys][d]
+//               (128-byte swizzle)
 //   warp 3      tensor memory, and the MMAs: S = Q K^T (both operands in shared memory), O += P V (P in
 //               tensor memory over the columns of S; V's tile read with d as its leading dimension,
 //               so that neither K nor V is ever transposed)
 //
-// Bounds per 128 keys and SM: MMA 1024 cycles, exponentials (16 a cycle) 1024, unpacking about 700 on
-// the same pipes as the rest of the softmax.  What it takes to get near them is that no step waits for
-// the round trip score -> softmax -> P V: there are three S buffers (with O they fill tensor memory at
-// d = 128), and the MMA order is S(0) S(1) S(2) | P V(0) S(3) | P V(1) S(4) | ...  With two accumulators
-// of two buffers, where S(t + 2) followed P V(t), a step took 3400 cycles.  Tensor operations execute
-// in issue order, so S(t + 3) may overwrite the P that P V(t) has read.
-// With two stages a tile has two steps' time from the end of S(t) to S(t + 2) for its signals and its
-// unpacking; hence eight warps each.
-// The groups share the running maximum: a group loads and reduces its scores while the other one is at
-// its exponentials, and only the decision on the maximum is passed from tile to tile.
+// Two accumulators: with more than 128 rows they hold the two halves of the rows and both see every key
+// tile; with fewer they hold the same rows and take the key tiles in turn, and their results (same lanes
+// of tensor memory) are merged at the end.  The MMA order is S(0) S(1) | P V(0) S(2) | P V(1) S(3) | ...:
+// tensor operations execute in issue order, so S(u + 2) may overwrite the P that P V(u) has read.
+//
+// What bounds it is instruction issue: per 128 x 128 step about 3000 warp instructions to unpack (shared
+// by two steps where there are more than 128 rows), 2000 of softmax, beside 1024 cycles of MMA and as many
+// of exponentials (16 a cycle).
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
-// (Loading by warps of their own was tried: issuing the copies of 64 keys took such a warp 500 to 1500
-// cycles beside the others, with bulk copies as with these, and bounded the kernel.)
 //
 // Every wait is bounded.  One that gives up raises the block's abort flag; all roles fall through to
 // the common end, the sequence's status becomes MARS_SEQ_TIMEOUT, tensor memory is freed.
@@ -45,28 +40,24 @@ constexpr int kTileThreads = 896;
 constexpr int kSoftThreads = 256;
 constexpr int kTileKeys = 128;
 constexpr int kUnpackWarps = 8;                        // per K and V: 16 keys each
-constexpr int kRing = 3;                               // tiles in flight per warp
-constexpr int kBufs = 3;                               // S buffers
 constexpr uint32_t kTmemAll = 512;
-constexpr uint32_t kColO = 384;                        // S buffer i at 128 i, then O
+constexpr uint32_t kColO = 256;                        // accumulator i: S at 128 i, O at 256 + 128 i
 
 template <int D> constexpr uint32_t tile_bytes() { return 128u * D * 2; }    // 128 rows of d fp16
 template <int D> constexpr uint32_t slot_bytes() { return 9 * D; }           // a block's K or V: codes [16][d/2], scales [16][d/16]
-template <int D> constexpr uint32_t ring_bytes() { return 2 * kUnpackWarps * kRing * slot_bytes<D>(); }
+template <int D> constexpr uint32_t ring_bytes() { return 2 * kUnpackWarps * slot_bytes<D>(); }
 template <int D> constexpr int tile_slot_floats() { return TileShape::M * (D + 2); }
 
 constexpr int kMaskWords = kTileMaxTree / 32;
 
-// shared memory: Q | K (2 stages) | V (2 stages) | rings of the unpacking warps | the rest
+// shared memory: Q (2 tiles) | K (2 stages) | V (2 stages) | a slot per unpacking warp | the rest
 struct TileSmem {
     uint32_t mask[kTileMaxTree * kMaskWords];
     int par[kTileMaxTree];
     unsigned char live[kTileMaxTree];
     AttnSeqs seqs;
-    float xch[2][128];                                  // [group][row]: largest of q's halves; sums
-    float mref[2][128];                                 // [group][row]: the maximum as its last tile left it
-    uint64_t kfull[2], kempty[2], vfull[2], vempty[2], sfull[kBufs], pfull[kBufs], odone[kBufs];
-    uint64_t chain[4][2];                               // [quarter of the rows][group]: maximum decided
+    float xm[2][128], xl[2][128];                       // [accumulator][row]: maxima and sums
+    uint64_t kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], odone[2];
     uint64_t qfull, drain;
     uint32_t tmem;
     int abort, bad, last, ok;
@@ -75,7 +66,7 @@ struct TileSmem {
 
 template <int D> constexpr size_t tile_smem_bytes()
 {
-    const size_t need = 1024 + 5 * (size_t)tile_bytes<D>() + ring_bytes<D>() + sizeof(TileSmem);
+    const size_t need = 1024 + 6 * (size_t)tile_bytes<D>() + ring_bytes<D>() + sizeof(TileSmem);
     return need > 120 * 1024 ? need : 120 * 1024;      // one block per SM: each takes all of tensor memory
 }
 static_assert(tile_smem_bytes<128>() <= 227 * 1024 - 1024, "shared memory of one SM, with room for the static part");
@@ -146,9 +137,6 @@ __device__ __forceinline__ void add2(float &a0, float &a1, float b0, float b1)
 }
 
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-// the two warps of 32 query rows
-__device__ __forceinline__ void quarter_sync(int quarter) { asm volatile("bar.sync %0, 64;" ::"r"(2 + quarter) : "memory"); }
-
 // Instruction descriptors: D fp32, A and B fp16, M = 128; S: N = 128 keys, both operands K-major;
 // O: N = d, B with d as its leading dimension.
 constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)(kTileKeys >> 3) << 17) | ((128u >> 4) << 24);
@@ -172,7 +160,8 @@ __device__ __forceinline__ uint32_t visible32(int p0, int len, int node, bool tr
 // A segment as this kernel sees it.
 struct TileSegment : AttnSegment {
     int rows, row0;          // query rows of the tile, its first one
-    int key0, tiles;         // first key, key tiles
+    int key0, tiles, steps;  // first key, key tiles, S / P V steps
+    bool two;                // the accumulators hold different rows (else they take turns on the keys)
     bool whole;
 };
 
@@ -182,66 +171,35 @@ __device__ __forceinline__ TileSegment tile_segment(const AttnParams &p, const T
     static_cast<AttnSegment &>(s) = attn_segment<TileShape>(p, &sh->seqs, r, u);
     s.rows = attn_tile_rows<TileShape>(p, s.n, s.tile);
     s.row0 = s.tile * TileShape::M;
-    s.key0 = s.unit0 * kTileKeys;
-    s.tiles = max(s.unit1 - s.unit0, 0);
-    s.whole = s.tiles == s.units;
+    s.two = s.rows > 128;
+    const int uk = TileShape::unit_keys(s.rows);
+    s.key0 = s.unit0 * uk;
+    s.tiles = s.unit1 > s.unit0 ? (min(s.keys, s.unit1 * uk) - s.key0 + kTileKeys - 1) / kTileKeys : 0;
+    s.steps = s.two ? 2 * s.tiles : s.tiles;
+    s.whole = s.unit1 - s.unit0 == s.units;
     return s;
 }
 
 // ------------------------------------------------------------------------------------- warps 4-19
 
-// A warp's 16 keys of K or V from its ring slot into rows key0 .. key0 + 15 of a tile: two threads per key,
-// chunks of 32 codes, the order of a row's halves alternating with the key so that both the reads
-// (rows d/2 bytes apart) and the swizzled writes are free of bank conflicts.  have: the slot holds the
-// block and the key was written; else zeros, and `scale` for its scales.
-template <int D>
-__device__ __forceinline__ void tile_unpack(const unsigned char *slot, int key0, bool have, uint32_t scale, unsigned char *tile)
-{
-    constexpr int kN = D / 64;
-    const int lane = threadIdx.x & 31, in = lane >> 1, odd = lane & 1, key = key0 + in;
-    const int swap = D == 128 ? (in >> 1) & 1 : 0;
-    const unsigned char *blk = slot + in * (D / 2), *scl = slot + 8 * D + in * (D / 16);
-    uint4 c[kN];
-    uint32_t s[kN];
-#pragma unroll
-    for (int a = 0; a < kN; ++a) {
-        const int part = ((a ^ swap) << 1) | odd;
-        c[a] = make_uint4(0u, 0u, 0u, 0u);
-        s[a] = scale;
-        if (have) {
-            c[a] = *reinterpret_cast<const uint4 *>(blk + part * 16);
-            s[a] = *reinterpret_cast<const unsigned short *>(scl + part * 2);
-        }
-    }
-#pragma unroll
-    for (int a = 0; a < kN; ++a) {
-        const uint32_t sh = e4m3x2_to_f16x2(s[a]);
-        const uint32_t sc[2] = {__byte_perm(sh, sh, 0x1010), __byte_perm(sh, sh, 0x3232)};
-        const uint32_t w[4] = {c[a].x, c[a].y, c[a].z, c[a].w};
-        unsigned char *dst = tile + (a ^ swap) * (128 * 128) + key * 128;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t h[4];
-            e2m1x8_to_f16x2(w[k], h);
-            const uint32_t f = sc[k >> 1];
-            *reinterpret_cast<uint4 *>(dst + (((odd * 4 + k) ^ (key & 7)) * 16)) =
-                make_uint4(hmul2(h[0], f), hmul2(h[1], f), hmul2(h[2], f), hmul2(h[3], f));
-        }
-    }
-}
-
-// K (v = 0) or V (v = 1); w: which 16 keys of a tile.  A tile's copies are one group of the warp's, in
-// order over all segments, so the ring needs no barriers.
+// K (v = 0) or V (v = 1) of the warp's 16 keys (w: which of a tile).  Two threads per key; chunks of 32
+// codes, the order of a row's halves alternating with the key so that both the reads (rows d/2 bytes
+// apart) and the swizzled writes are free of bank conflicts.  A tile's codes go from the warp's slot to
+// registers as soon as they are there; then the slot takes the next tile's, while this one waits for its
+// place (until S, or P V, of two tiles ago is done).  Copies are groups of the warp's own: no barriers.
 template <int D>
 __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange r, TileSmem *sh, unsigned char *tiles,
-                                                 unsigned char *ring, int v, int w)
+                                                 unsigned char *slot, int v, int w)
 {
-    const int lane = threadIdx.x & 31;
+    constexpr int kN = D / 64;
+    const int lane = threadIdx.x & 31, in = lane >> 1, odd = lane & 1, key = w * kKvBlock + in;
+    const int swap = D == 128 ? (in >> 1) & 1 : 0;
+    const unsigned char *blk = slot + in * (D / 2), *scl = slot + 8 * D + in * (D / 16);
     volatile int *abort_flag = &sh->abort;
     uint64_t *full = v ? sh->vfull : sh->kfull, *empty = v ? sh->vempty : sh->kempty;
-    const uint32_t ring_u32 = smem_u32(ring) + lane * 16;
+    const uint32_t slot_u32 = smem_u32(slot) + lane * 16;
     constexpr uint64_t kNoPage = 1;          // address that stands for a page outside the pool; 0: no key
-    uint32_t n = 0, at = 0, put = 0;         // tiles unpacked; ring slots to read and to fill next
+    uint32_t n = 0;                          // tiles unpacked
     bool ok = true;
     for (int64_t u = r.begin; u < r.end && ok;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
@@ -255,38 +213,55 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
             return id < 0 ? kNoPage : (uint64_t)(kv_block<D>(p.kv, p.layer, id, sg.head, pos) + v * 8 * D);
         };
         uint64_t here = locate(0), next = sg.tiles > 32 ? locate(32) : 0;
-        auto issue = [&](int t) {            // tile t of the segment, 32 tiles of addresses from t & ~31 in `here`
-            if (t < sg.tiles) {
-                const uint64_t from = __shfl_sync(0xffffffffu, here, t & 31);
-                if (from > kNoPage) {
-                    const unsigned char *src = (const unsigned char *)from + lane * 16;
-                    const uint32_t dst = ring_u32 + put * slot_bytes<D>();
+        uint64_t from = 0;                   // of the tile in the slot
+        auto issue = [&](int t) {
+            if (t && (t & 31) == 0) { here = next; next = locate(t + 32); }
+            from = t < sg.tiles ? __shfl_sync(0xffffffffu, here, t & 31) : 0;
+            if (from > kNoPage) {
+                const unsigned char *src = (const unsigned char *)from + lane * 16;
 #pragma unroll
-                    for (int i = 0; i < D / 64; ++i) cp_async16_to(dst + i * 512, src + i * 512);
-                    // the scales follow K's codes by 16d bytes, V's by 9d
-                    if (lane < D / 16) cp_async16_to(dst + 8 * D, src + 16 * D - v * 7 * D);
-                }
-                put = put == kRing - 1 ? 0u : put + 1;
+                for (int i = 0; i < D / 64; ++i) cp_async16_to(slot_u32 + i * 512, src + i * 512);
+                // the scales follow K's codes by 16d bytes, V's by 9d
+                if (lane < D / 16) cp_async16_to(slot_u32 + 8 * D, src + 16 * D - v * 7 * D);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        uint64_t seen = here;                // addresses of the tiles being unpacked (issue runs ahead)
-#pragma unroll
-        for (int t = 0; t < kRing - 1; ++t) issue(t);
+        issue(0);
         for (int t = 0; t < sg.tiles; ++t, ++n) {
-            if ((t & 31) == 0) seen = here;
-            const uint64_t from = __shfl_sync(0xffffffffu, seen, t & 31);
-            if (((t + kRing - 1) & 31) == 0) { here = next; next = locate(t + kRing - 1 + 32); }
-            issue(t + kRing - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
+            uint4 c[kN];
+            uint32_t s[kN];
+            const bool have = from > kNoPage && first + t * kTileKeys + in < valid;
+#pragma unroll
+            for (int a = 0; a < kN; ++a) {
+                const int part = ((a ^ swap) << 1) | odd;
+                c[a] = make_uint4(0u, 0u, 0u, 0u);
+                s[a] = v && from == kNoPage ? 0x7f7fu : 0u;       // V of a page outside the pool: NaN
+                if (have) {
+                    c[a] = *reinterpret_cast<const uint4 *>(blk + part * 16);
+                    s[a] = *reinterpret_cast<const unsigned short *>(scl + part * 2);
+                }
+            }
+            __syncwarp();
+            issue(t + 1);
             const uint32_t st = n & 1u;
             ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[st]), ((n >> 1) & 1u) ^ 1u, abort_flag, &sh->word)) != 0;
             if (!ok) break;
-            const bool have = from > kNoPage && first + t * kTileKeys + (lane >> 1) < valid;
-            // V of a page outside the pool: NaN
-            tile_unpack<D>(ring + at * slot_bytes<D>(), w * kKvBlock, have, v && from == kNoPage ? 0x7f7fu : 0u, tiles + st * tile_bytes<D>());
-            at = at == kRing - 1 ? 0u : at + 1;
+#pragma unroll
+            for (int a = 0; a < kN; ++a) {
+                const uint32_t sb = e4m3x2_to_f16x2(s[a]);
+                const uint32_t sc[2] = {__byte_perm(sb, sb, 0x1010), __byte_perm(sb, sb, 0x3232)};
+                const uint32_t cw[4] = {c[a].x, c[a].y, c[a].z, c[a].w};
+                unsigned char *dst = tiles + st * tile_bytes<D>() + (a ^ swap) * (128 * 128) + key * 128;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t h[4];
+                    e2m1x8_to_f16x2(cw[k], h);
+                    const uint32_t f = sc[k >> 1];
+                    *reinterpret_cast<uint4 *>(dst + (((odd * 4 + k) ^ (key & 7)) * 16)) =
+                        make_uint4(hmul2(h[0], f), hmul2(h[1], f), hmul2(h[2], f), hmul2(h[3], f));
+                }
+            }
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&full[st]));
@@ -307,51 +282,57 @@ __device__ __forceinline__ void tile_mma(const AttnParams &p, AttnRange r, TileS
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_any, 0);
     const uint32_t lead = elect_one();
     const uint64_t qdesc = umma_desc_k_sw128(q_at), kdesc = umma_desc_k_sw128(k_at), vdesc = umma_desc_mn_sw128(v_at, 128 * 128);
-    uint32_t kst = 0, kpar = 0, sbuf = 0;            // next S: K stage and its phase, buffer
-    uint32_t vst = 0, vpar = 0, pbuf = 0, ppar = 0;  // next P V: V stage and phase, buffer and phase
-    uint32_t n_seg = 0;
+    uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;   // K and V stage in use, its phase
+    uint32_t ppar[2] = {0, 0}, n_seg = 0;
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) {
         return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, abort_flag, &sh->word)) != 0;
     };
-    auto issue_s = [&]() {
-        if (!wait(&sh->kfull[kst], kpar)) return false;
+    // S of accumulator i; `opens`, `closes`: the first and the last to read the K tile
+    auto issue_s = [&](int i, bool two) {
+        const bool opens = !two || i == 0, closes = !two || i == 1;
+        if (opens && !wait(&sh->kfull[kst], kpar)) return false;
         tc_fence_after();
-        const uint64_t b = kdesc + kst * (kT >> 4);
+        const uint64_t a = qdesc + (two ? i * (kT >> 4) : 0), b = kdesc + kst * (kT >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
             const uint32_t off = (k >> 2) * ((128 * 128) >> 4) + 2 * (k & 3);
-            tc_mma_f16_ss(lead, tmem + 128 * sbuf, qdesc + off, b + off, kIdescS, k != 0);
+            tc_mma_f16_ss(lead, tmem + 128 * i, a + off, b + off, kIdescS, k != 0);
         }
-        tc_commit_if(lead, smem_u32(&sh->sfull[sbuf]));
-        tc_commit_if(lead, smem_u32(&sh->kempty[kst]));
-        kpar ^= kst;
-        kst ^= 1u;
-        sbuf = sbuf == kBufs - 1 ? 0u : sbuf + 1;
+        tc_commit_if(lead, smem_u32(&sh->sfull[i]));
+        if (closes) {
+            tc_commit_if(lead, smem_u32(&sh->kempty[kst]));
+            kpar ^= kst;
+            kst ^= 1u;
+        }
         return true;
     };
     for (int64_t u = r.begin; u < r.end && ok;) {
         const TileSegment sg = tile_segment(p, sh, r, u);
         if (sg.tiles == 0) { u += sg.span; continue; }
-        const int tiles = __shfl_sync(0xffffffffu, sg.tiles, 0);
+        const int steps = __shfl_sync(0xffffffffu, sg.steps, 0);
+        const bool two = __shfl_sync(0xffffffffu, (int)sg.two, 0) != 0;
         ok = wait(&sh->qfull, n_seg & 1u);
         ++n_seg;
-        for (int t = 0; t < min(kBufs, tiles) && ok; ++t) ok = issue_s();
-        for (int t = 0; t < tiles && ok; ++t) {
-            ok = wait(&sh->vfull[vst], vpar) && wait(&sh->pfull[pbuf], ppar);
+        for (int s = 0; s < min(2, steps) && ok; ++s) ok = issue_s(s, two);
+        for (int s = 0; s < steps && ok; ++s) {
+            const int i = s & 1;
+            const bool opens = !two || i == 0, closes = !two || i == 1;
+            ok = (!opens || wait(&sh->vfull[vst], vpar)) && wait(&sh->pfull[i], ppar[i]);
             if (!ok) break;
+            ppar[i] ^= 1u;
             tc_fence_after();
             const uint64_t b = vdesc + vst * (kT >> 4);
 #pragma unroll
             for (int k = 0; k < kTileKeys / 16; ++k)
-                tc_mma_f16_ts(lead, tmem + kColO, tmem + 128 * pbuf + 8 * k, b + k * (2048 >> 4), idesc_o<D>(), k != 0 || t > 0);
-            tc_commit_if(lead, smem_u32(&sh->odone[pbuf]));
-            tc_commit_if(lead, smem_u32(&sh->vempty[vst]));
-            vpar ^= vst;
-            vst ^= 1u;
-            if (pbuf == kBufs - 1) { pbuf = 0; ppar ^= 1u; }
-            else ++pbuf;
-            if (t + kBufs < tiles) ok = issue_s();
+                tc_mma_f16_ts(lead, tmem + kColO + 128 * i, tmem + 128 * i + 8 * k, b + k * (2048 >> 4), idesc_o<D>(), k != 0 || s >= 2);
+            tc_commit_if(lead, smem_u32(&sh->odone[i]));
+            if (closes) {
+                tc_commit_if(lead, smem_u32(&sh->vempty[vst]));
+                vpar ^= vst;
+                vst ^= 1u;
+            }
+            if (s + 2 < steps) ok = issue_s(i, two);
         }
         u += sg.span;
     }
@@ -393,16 +374,15 @@ __device__ __forceinline__ void exp64(float *v, float rs, float minus, uint32_t 
 }
 
 template <int D, int DT>
-__device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, TileSmem *sh, uint32_t tmem, unsigned char *q_tile)
+__device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, TileSmem *sh, uint32_t tmem, unsigned char *q_tiles)
 {
     const int tid = threadIdx.x - 640, warp = tid >> 5, lane = tid & 31;
-    const int group = warp >> 2, quarter = warp & 3;
-    const int rr = quarter * 32 + lane;      // row of the tile, lane of tensor memory
+    const int acc = warp >> 2, quarter = warp & 3;
+    const int rr = quarter * 32 + lane;      // row of the accumulator, lane of tensor memory
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    constexpr int kPart = D / 2;             // d values per thread for Q and for the result
-    const uint32_t oc = lanes + kColO;
+    const uint32_t sc = lanes + 128 * acc, oc = lanes + kColO;
     volatile int *abort_flag = &sh->abort;
-    uint32_t n0 = 0;                         // tiles of earlier segments
+    uint32_t n_s = 0;                        // S tiles of this accumulator so far
     int mask_b = -1, status = MARS_SEQ_OK;   // sequence whose masks are in shared memory, its status
     auto wait = [&](uint64_t *bar, uint32_t parity) {
         return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, abort_flag, &sh->word)) != 0;
@@ -412,25 +392,21 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         if (sg.tiles == 0) { u += sg.span; continue; }
         const bool tree = p.parent != nullptr;
         const int words = (sg.n + 31) >> 5;
-        const int node = rr < sg.rows ? attn_node(p, sg.row0 + rr) : -1;
-        const int head = sg.head * p.group + (node >= 0 ? sg.row0 + rr - node * p.group : 0);
-        const bool idle = quarter * 32 >= sg.rows;           // no query row in this warp
+        const int row = (sg.two ? acc * 128 : 0) + rr;
+        const int node = row < sg.rows ? attn_node(p, sg.row0 + row) : -1;
+        const int head = sg.head * p.group + (node >= 0 ? sg.row0 + row - node * p.group : 0);
+        const bool idle = row - lane >= sg.rows;             // no query row in this warp
 
-        // ---- Q: this thread's half of its row, scaled to fp16, into the row's swizzled tile
+        // ---- Q: this thread's row, scaled to fp16, into its swizzled tile (in four quarters: registers)
         float rs;                            // score scale of the row in log2 units
         {
-            uint4 w[kPart / 8];
-            if (node >= 0) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + 2 * (((int64_t)sg.b * p.N + node) * p.q_row + head * p.q_head + group * kPart));
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + 2 * (((int64_t)sg.b * p.N + (node >= 0 ? node : 0)) * p.q_row + head * p.q_head));
+            uint4 w[D / 8];
 #pragma unroll
-                for (int c = 0; c < kPart / 8; ++c) w[c] = src[c];
-            } else {
-#pragma unroll
-                for (int c = 0; c < kPart / 8; ++c) w[c] = make_uint4(0u, 0u, 0u, 0u);
-            }
+            for (int c = 0; c < D / 8; ++c) w[c] = node >= 0 ? src[c] : make_uint4(0u, 0u, 0u, 0u);
             float m = 0.0f;
 #pragma unroll
-            for (int c = 0; c < kPart / 8; ++c) {
+            for (int c = 0; c < D / 8; ++c) {
                 const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -438,26 +414,24 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                     m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
                 }
             }
-            sh->xch[group][rr] = m;
-            quarter_sync(quarter);
-            m = fmaxf(m, sh->xch[group ^ 1][rr]);
             float down, up;
             row_scale(m, &down, &up);
             rs = fmaxf(p.scale_log2 * p.scales[sg.head] * up, 1.17549435e-38f);
-            unsigned char *dst = q_tile + rr * 128;
+            if (sg.two || acc == 0) {
+                unsigned char *dst = q_tiles + acc * tile_bytes<D>() + rr * 128;
 #pragma unroll
-            for (int c = 0; c < kPart / 8; ++c) {
-                const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-                uint32_t h[4];
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+                    uint32_t h[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = widen2<DT>(x[j]);
-                    h[j] = f16x2_from(f.x * down, f.y * down);
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 f = widen2<DT>(x[j]);
+                        h[j] = f16x2_from(f.x * down, f.y * down);
+                    }
+                    *reinterpret_cast<uint4 *>(dst + (c >> 3) * (128 * 128) + (((c & 7) ^ (rr & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
                 }
-                const int cc = group * (kPart / 8) + c;      // 16-byte chunk of the row
-                *reinterpret_cast<uint4 *>(dst + (cc >> 3) * (128 * 128) + (((cc & 7) ^ (rr & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
+                fence_proxy_async();
             }
-            fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->qfull));
         }
@@ -469,17 +443,16 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         if (tid == 0 && p.status && sg.head == 0 && sg.tile == 0 && sg.unit0 == 0) p.status[sg.b] = status;
 
         const uint32_t *mask = sh->mask + (tree && node >= 0 ? node : 0) * words;
-        float lref = -INFINITY, l = 0.0f;    // sum of this group's keys, and the maximum that it refers to
+        float mref = -INFINITY, l = 0.0f;    // reference maximum of the row in this accumulator, its sum
+        const int my = sg.two ? sg.tiles : (sg.tiles + 1 - acc) >> 1;        // this accumulator's key tiles
         bool ok = true;
-        for (int t = (int)((n0 ^ (uint32_t)group) & 1u); t < sg.tiles; t += 2) {
-            const uint32_t n = n0 + t, buf = n % kBufs;
-            const int pos0 = sg.key0 + t * kTileKeys;
-            const uint32_t sc = lanes + 128 * buf;
-            ok = wait(&sh->sfull[buf], (n / kBufs) & 1u);
+        for (int j = 0; j < my; ++j, ++n_s) {
+            const int pos0 = sg.key0 + (sg.two ? j : 2 * j + acc) * kTileKeys;
+            ok = wait(&sh->sfull[acc], n_s & 1u);
             if (!ok) break;
             if (idle) {
                 // rows without a query: whatever S holds may stand for their P
-                if (lane == 0) { mbar_arrive(smem_u32(&sh->chain[quarter][group])); mbar_arrive(smem_u32(&sh->pfull[buf])); }
+                if (lane == 0) mbar_arrive(smem_u32(&sh->pfull[acc]));
                 continue;
             }
             tc_fence_after();
@@ -504,41 +477,28 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             tc_ld32_wait(x);
             if (edge) mask32(x, visible32(pos0 + 96, sg.len, node, tree, mask, words));
             mx = fmaxf(mx, max32(x)) * rs;
-            // the other group's decision on the tile before
-            float mref = -INFINITY;
-            if (t > 0) {
-                ok = wait(&sh->chain[quarter][group ^ 1], ((n - 1) >> 1) & 1u);
-                if (!ok) break;
-                mref = sh->mref[group ^ 1][rr];
-            }
-            // the maximum moves only when it grows by more than 2^8; the first tile just sets it
+            // the reference moves only when a score exceeds it by more than 2^8; the first tile just sets it
             const bool grow = mx > mref + 8.0f;
-            const float to = grow ? mx : mref;
-            sh->mref[group][rr] = to;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->chain[quarter][group]));
-            if (t > 0 && __any_sync(0xffffffffu, grow)) {
-                ok = wait(&sh->odone[(n - 1) % kBufs], ((n - 1) / kBufs) & 1u);
-                if (!ok) break;
+            if (__any_sync(0xffffffffu, grow)) {
+                const float to = grow ? mx : mref;
                 const float f = to == -INFINITY || mref == to ? 1.0f : ex2(mref - to);
-                tc_fence_after();
+                mref = to;
+                l *= f;
+                if (j > 0) {
+                    // P V of the accumulator's tile before is complete: the S that was just read came after it
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    float y[16];
-                    uint32_t z[8];
-                    tc_ld16(oc + c, y);
+                    for (int c = 0; c < D; c += 16) {
+                        float y[16];
+                        uint32_t z[8];
+                        tc_ld16(oc + 128 * acc + c, y);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[k] * f);
-                    tc_st8(oc + c, z);
+                        for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[k] * f);
+                        tc_st8(oc + 128 * acc + c, z);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[8 + k] * f);
-                    tc_st8(oc + c + 8, z);
+                        for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[8 + k] * f);
+                        tc_st8(oc + 128 * acc + c + 8, z);
+                    }
                 }
-            }
-            mref = to;
-            if (lref != mref) {
-                l = lref == -INFINITY ? 0.0f : l * ex2(lref - mref);
-                lref = mref;
             }
             // P = 2^(s - mref + 7), see mars_attention.cu; over columns of S that were read for good
             const float minus = mref == -INFINITY ? 0.0f : 7.0f - mref;
@@ -557,40 +517,59 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->pfull[buf]));
+            if (lane == 0) mbar_arrive(smem_u32(&sh->pfull[acc]));
         }
-        const uint32_t end = n0 + sg.tiles - 1;              // the segment's last tile
-        if (ok && (end & 1u) == (uint32_t)group) (void)wait(&sh->odone[end % kBufs], (end / kBufs) & 1u);
+        if (ok && my > 0) ok = wait(&sh->odone[acc], (n_s - 1u) & 1u);
+        sh->xm[acc][rr] = mref;
+        sh->xl[acc][rr] = l;
         tc_fence_before();
-        softmax_sync();                      // O complete, the last maxima decided and read
+        softmax_sync();                      // both accumulators complete
         tc_fence_after();
-        const float m_end = idle ? 0.0f : sh->mref[end & 1u][rr];
-        sh->xch[group][rr] = l = lref == -INFINITY ? 0.0f : l * ex2(lref - m_end);
         if (tid == 0) sh->ok = *abort_flag == 0;
         softmax_sync();
         if (!sh->ok) {
             if (tid == 0 && p.status) p.status[sg.b] = MARS_SEQ_TIMEOUT;
             break;
         }
-        n0 += sg.tiles;
 
-        // ---- result of the segment: a thread has half of d of its row
-        float m = m_end, sum = sh->xch[0][rr] + sh->xch[1][rr];
+        // ---- result of the segment: with two halves a thread has its row, else half of d of it
+        const bool merge = !sg.two && sg.tiles > 1;
+        float m = mref, sum = l, f0 = 1.0f, f1 = 0.0f;
+        if (!sg.two) {
+            m = sh->xm[0][rr];
+            sum = sh->xl[0][rr];
+            if (merge) {
+                const float m1 = sh->xm[1][rr], mm = fmaxf(m, m1);
+                f0 = m == -INFINITY ? 0.0f : ex2(m - mm);
+                f1 = m1 == -INFINITY ? 0.0f : ex2(m1 - mm);
+                sum = sum * f0 + sh->xl[1][rr] * f1;
+                m = mm;
+            }
+        }
+        const int d0 = sg.two ? 0 : acc * (D / 2), d1 = sg.two ? D : d0 + D / 2;
+        const uint32_t o0 = oc + (sg.two ? 128 * acc : 0);
         const bool out_row = node >= 0 && (!tree || sh->live[node]);
-        const int64_t out_at = out_row ? ((int64_t)sg.b * p.N + node) * p.out_row + (int64_t)head * p.out_head + group * kPart : 0;
+        const int64_t out_at = out_row ? ((int64_t)sg.b * p.N + node) * p.out_row + (int64_t)head * p.out_head : 0;
         const float vscale = p.scales[p.kv.kv_heads + sg.head];
         constexpr int kF = tile_slot_floats<D>();
         if (!idle) {
-            float *dst = p.partial + (int64_t)(2 * blockIdx.x + (u == r.begin ? 0 : 1)) * kF + rr;
+            float *dst = p.partial + (int64_t)(2 * blockIdx.x + (u == r.begin ? 0 : 1)) * kF + row;
             const float norm = vscale / sum;
-#pragma unroll
-            for (int c = 0; c < kPart; c += 32) {
+#pragma unroll 1
+            for (int c = d0; c < d1; c += 32) {
                 float v[32];
-                tc_ld32_issue(oc + group * kPart + c, v);
+                tc_ld32_issue(o0 + c, v);
                 tc_ld32_wait(v);
+                if (merge) {
+                    float x[32];
+                    tc_ld32_issue(o0 + 128 + c, x);        // the second accumulator, same lanes
+                    tc_ld32_wait(x);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = v[k] * f0 + x[k] * f1;
+                }
                 if (!sg.whole) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) dst[(group * kPart + c + k) * TileShape::M] = v[k];
+                    for (int k = 0; k < 32; ++k) dst[(c + k) * TileShape::M] = v[k];
                 } else if (out_row) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] *= norm;
@@ -598,7 +577,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                     for (int k = 0; k < 32; k += 8) store_out8<DT>(p.out, out_at + c + k, v + k);
                 }
             }
-            if (!sg.whole && group == 0) {
+            if (!sg.whole && d0 == 0) {
                 dst[D * TileShape::M] = m;
                 dst[(D + 1) * TileShape::M] = sum;
             }
@@ -614,7 +593,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                 if (!idle) {
                     // block order, running maximum; 32 of a block's values at once
 #pragma unroll 1
-                    for (int d0 = group * kPart; d0 < (group + 1) * kPart; d0 += 32) {
+                    for (int c32 = d0; c32 < d1; c32 += 32) {
                         float o[32];
                         m = -INFINITY;
                         sum = 0.0f;
@@ -622,9 +601,9 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                         for (int k = 0; k < 32; ++k) o[k] = 0.0f;
 #pragma unroll 1
                         for (int c = c0; c <= c1; ++c) {
-                            const float *src = p.partial + (int64_t)(2 * c + (r.per * c >= sg.item ? 0 : 1)) * kF + rr;
+                            const float *src = p.partial + (int64_t)(2 * c + (r.per * c >= sg.item ? 0 : 1)) * kF + row;
                             const float pm = __ldcg(src + D * TileShape::M), pl = __ldcg(src + (D + 1) * TileShape::M);
-                            src += d0 * TileShape::M;
+                            src += c32 * TileShape::M;
                             float x[32];
 #pragma unroll
                             for (int k = 0; k < 32; ++k) x[k] = __ldcg(src + k * TileShape::M);
@@ -640,7 +619,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
 #pragma unroll
                             for (int k = 0; k < 32; ++k) o[k] *= norm;
 #pragma unroll
-                            for (int k = 0; k < 32; k += 8) store_out8<DT>(p.out, out_at + d0 - group * kPart + k, o + k);
+                            for (int k = 0; k < 32; k += 8) store_out8<DT>(p.out, out_at + c32 + k, o + k);
                         }
                     }
                 }
@@ -648,7 +627,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             }
         }
         tc_fence_before();
-        softmax_sync();                   // masks, exchange arrays and O are free for the next segment
+        softmax_sync();                   // masks, exchange arrays and accumulators are free for the next segment
         tc_fence_after();
         u += sg.span;
     }
@@ -664,7 +643,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
     const uint32_t base = (raw + 1023u) & ~1023u;
     unsigned char *sm = smem_raw + (base - raw);
     constexpr uint32_t kT = tile_bytes<D>();
-    unsigned char *ring = sm + 5 * kT;
+    unsigned char *ring = sm + 6 * kT;
     TileSmem *sh = reinterpret_cast<TileSmem *>(ring + ring_bytes<D>());
     const int tid = threadIdx.x, warp = tid >> 5;
 
@@ -675,9 +654,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
             mbar_init(smem_u32(&sh->vfull[i]), 8);
             mbar_init(smem_u32(&sh->kempty[i]), 1);
             mbar_init(smem_u32(&sh->vempty[i]), 1);
-            for (int k = 0; k < 4; ++k) mbar_init(smem_u32(&sh->chain[k][i]), 1);
         }
-        for (int i = 0; i < kBufs; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh->sfull[i]), 1);
             mbar_init(smem_u32(&sh->pfull[i]), 4);
             mbar_init(smem_u32(&sh->odone[i]), 1);
@@ -705,10 +683,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
     } else if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         const int v = warp >= 4 + kUnpackWarps;
-        tile_unpack_role<D>(p, r, sh, sm + (v ? 3 : 1) * kT, ring + (warp - 4) * kRing * slot_bytes<D>(), v, (warp - 4) & (kUnpackWarps - 1));
+        tile_unpack_role<D>(p, r, sh, sm + (v ? 4 : 2) * kT, ring + (warp - 4) * slot_bytes<D>(), v, (warp - 4) & (kUnpackWarps - 1));
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == 3) tile_mma<D>(p, r, sh, tmem, base, base + kT, base + 3 * kT);
+        if (warp == 3) tile_mma<D>(p, r, sh, tmem, base, base + 2 * kT, base + 4 * kT);
     }
 
     tc_fence_before();
