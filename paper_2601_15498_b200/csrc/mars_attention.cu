@@ -546,7 +546,7 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     p.q_row = q_row; p.q_head = q_head; p.out_row = out_row; p.out_head = out_head;
     p.parent = parent; p.count = count; p.status = seq_status;
     p.shared_parent = (flags & MARS_SHARED_PARENT) != 0;
-    p.B = B; p.N = N; p.group = q_heads / cache->kv_heads;
+    p.B = B; p.N = N; p.group = q_heads / cache->kv_heads; p.tile_rows = 0;
     p.group_inv = p.group > 1 ? ~0ull / (unsigned)p.group + 1 : 0;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.counters = (unsigned *)workspace;

@@ -20,19 +20,21 @@
 
 namespace mars {
 
-// Tile shapes: query rows per tile, keys per unit of the split, and what an item costs besides its keys
+// Tile shapes: query rows per tile, keys per unit of the split, the least number of units per block (a
+// block more costs a partial result and its merge), and what an item costs besides its keys
 // (decoding, Q, masks, the pipeline's fill and drain, the result) in units.  Counting that in evens out
-// the blocks where items are short.  Measured, us at 0 / this / twice this: 64 trees 485 / 437 / 446,
-// four prompts 200 / 147 / 156 (TileShape); 64 tokens 115 / 105 / 109, 64 chains 232 / 202 / 212.
+// the blocks where items are short.  Measured, us without / as here / with twice that: 64 tokens 115 / 104 /
+// 109, 64 chains 232 / 201 / 212; four prompts 200 / 132 / 145 (TileShape).
 template <int kRows>
 struct RowsShape {
-    static constexpr int M = kRows;
-    static constexpr int kFixed = kRows == 32 ? 8 : 6;
+    static __device__ constexpr int rows(int) { return kRows; }
+    static constexpr int kFixed = kRows == 32 ? 8 : 6, kLeast = 2;
     static __host__ __device__ constexpr int unit_keys(int) { return 64; }
 };
 struct TileShape {
-    static constexpr int M = 256;
-    static constexpr int kFixed = 6;
+    static constexpr int kMost = 256;
+    static __device__ int rows(int tile_rows) { return tile_rows; }    // 128 or 256, chosen per call
+    static constexpr int kFixed = 4, kLeast = 4;
     // up to 128 rows fill one of the kernel's two accumulators; the two then share the keys
     static __host__ __device__ constexpr int unit_keys(int rows) { return rows > 128 ? 128 : 256; }
 };
@@ -49,6 +51,7 @@ struct AttnParams {
     int32_t *status;                 // or null
     int shared_parent;
     int B, N, group;
+    int tile_rows;                   // query rows per tile of TileShape
     uint64_t group_inv;              // floor(2^64 / group) + 1 (unused for 1)
     float scale_log2;                // softmax scale * log2(e)
     unsigned *counters;              // [grid]
@@ -80,10 +83,10 @@ __device__ __forceinline__ int attn_node(const AttnParams &p, int row)
 }
 
 template <class S>
-__device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + S::M - 1) / S::M; }
+__device__ __forceinline__ int attn_tiles(const AttnParams &p, int n) { return (n * p.group + S::rows(p.tile_rows) - 1) / S::rows(p.tile_rows); }
 
 template <class S>
-__device__ __forceinline__ int attn_tile_rows(const AttnParams &p, int n, int mt) { return min(S::M, n * p.group - mt * S::M); }
+__device__ __forceinline__ int attn_tile_rows(const AttnParams &p, int n, int mt) { return min(S::rows(p.tile_rows), n * p.group - mt * S::rows(p.tile_rows)); }
 
 // Keys that the rows of tile mt (rows mt*M .. of n*group) may see: all nodes of a tree, the nodes up
 // to the tile's last one of a chain.
@@ -91,7 +94,7 @@ template <class S>
 __device__ __forceinline__ int attn_keys(const AttnParams &p, int len, int n, int mt)
 {
     if (p.parent) return len + n;
-    return len + min(n, attn_node(p, (mt + 1) * S::M - 1) + 1);
+    return len + min(n, attn_node(p, (mt + 1) * S::rows(p.tile_rows) - 1) + 1);
 }
 
 // Units of an item: its fixed cost, then its keys.
@@ -148,7 +151,7 @@ __device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // sequences go to threads in contiguous chunks; where a sequence has many tiles, to warps
-    const bool by_warp = !p.parent && (int64_t)p.N * p.group > S::M;
+    const bool by_warp = !p.parent && (int64_t)p.N * p.group > S::rows(p.tile_rows);
     const int who = by_warp ? warp : tid, of = by_warp ? kThreads / 32 : kThreads;
     const int chunk = (p.B + of - 1) / of;
     const int lo = min(who * chunk, p.B), hi = min(lo + chunk, p.B);
@@ -177,7 +180,7 @@ __device__ AttnRange attn_split(const AttnParams &p, AttnSeqs *seqs)
         total += s_sum[w];
     }
     AttnRange r;
-    r.per = max(attn_div(total + gridDim.x - 1, gridDim.x), (int64_t)1);
+    r.per = max(attn_div(total + gridDim.x - 1, gridDim.x), (int64_t)S::kLeast);
     r.begin = min(r.per * blockIdx.x, total);
     r.end = min(r.begin + r.per, total);
     int64_t at = before + inc - sum;
