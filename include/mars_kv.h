@@ -29,7 +29,8 @@
  * Sequences.  Sequence b's token at position p lies in page block_table[b][p / page_size], slot
  * p % page_size.  seq_len[b] tokens are committed; the nodes of a draft tree (or the tokens of a
  * prompt) take the positions seq_len[b] + i until mars_kv_commit.  In calls with a batch, batch row b
- * is sequence b.
+ * is sequence b.  seq_len may be set by the program, but not back into a page that another sequence
+ * holds too (count above 1): rows appended there would be the other's as well.
  *
  * Pages.  page_refs[p] counts the sequences that hold page p; bit p%32 of free_bits[p/32] is set iff
  * page p is free.  A new cache has all counts and tables at zero / -1 and all bits of existing pages
@@ -87,6 +88,7 @@ size_t mars_kv_pool_bytes(int layers, int num_pages, int kv_heads, int head_dim,
  * nearest even and saturating; NaN counts as 0; s * g = 0 gives zero codes.
  *   k, v       `dt` (MARS_BF16, MARS_FP32, MARS_FP16); row b*N + i, head h at k + (b*N + i)*k_row +
  *              h*k_head (elements), unit inner stride; rows and heads must start on 16-byte boundaries.
+ *   N          at most 2^24.
  *   count      int32 [B], rows of sequence b that are taken (the first ones), or NULL: all N.
  *              Counts below 0 read as 0, above N as N.
  *   seq_status int32 [B] or NULL: MARS_SEQ_OK, or MARS_SEQ_NO_ROOM: nothing of that sequence written.
@@ -112,9 +114,11 @@ mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void
  *              once and used by completed calls of this function only since; otherwise the call
  *              clears its counters (one stream operation more).
  *   seq_status int32 [B] or NULL: MARS_SEQ_OK, MARS_SEQ_NO_ROOM (no row written), MARS_SEQ_BAD_TREE
- *              (only the root's row is computed).
+ *              (only the root's row is computed).  MARS_SEQ_TIMEOUT: a bounded wait inside the kernel
+ *              gave up (a second without progress); rows of that sequence may be missing, and the
+ *              workspace has to be zeroed before MARS_COUNTERS_ZERO is given again.
  *   Rows i >= count[b] and rows of absent nodes (parent -1, i > 0, and what hangs below them) stay as
- *   they were.
+ *   they were; the slots of such nodes in the cache need not have been written.
  *   Scores, maxima, sums and the output are accumulated in fp32; products run on the tensor cores
  *   with K, V and q exact in fp16 (q scaled by a power of two per row) and the probabilities rounded
  *   to fp16.  Results do not vary from run to run.
@@ -146,8 +150,8 @@ mars_status_t mars_kv_commit(const mars_kv_cache_t *cache, const int32_t *path_n
  * Sequence dst[p] becomes a copy of sequence src[p], for every pair p: full pages are shared (their
  * counts rise), the rows of a last page that is not full are copied to a new page in every layer, so
  * that both may be continued.  dst must hold no pages.  Sources are read as they stood before the call.
- *   status     int32 [pairs], required: MARS_SEQ_OK, MARS_SEQ_OUT_OF_PAGES, MARS_SEQ_BAD_FORK,
- *              MARS_SEQ_NO_ROOM is not used; a pair that is not OK changes nothing.
+ *   status     int32 [pairs], required: MARS_SEQ_OK, MARS_SEQ_OUT_OF_PAGES or MARS_SEQ_BAD_FORK; a pair
+ *              that is not OK changes nothing.
  */
 mars_status_t mars_kv_fork(const mars_kv_cache_t *cache, const int32_t *src, const int32_t *dst, int pairs,
                            int32_t *status, void *cuda_stream);
@@ -168,7 +172,8 @@ mars_status_t mars_kv_resize(const mars_kv_cache_t *cache, const int32_t *extra,
 /*
  * Rows of the cache as values: for layers layer0 .. layer0+layers-1 and sequences b < B, positions
  * start[b] .. start[b] + count[b] - 1 to rows 0 .. of k_out and v_out, [layers][B][rows][kv_heads]
- * [head_dim] contiguous, of `dt` (MARS_BF16, MARS_FP32, MARS_FP16), rounded once.  Rows from count[b]
+ * [head_dim] contiguous on 16-byte boundaries, of `dt` (MARS_BF16, MARS_FP32, MARS_FP16), rounded once;
+ * `rows` is at most 2^24.  Rows from count[b]
  * on, and positions that lie outside the sequence's pages, stay as they were.
  *   start      int32 [B] or NULL: 0.      count  int32 [B] or NULL: all `rows`.
  */

@@ -274,9 +274,9 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kerne
                 const unsigned char *sp = blk + 17 * D;
                 uint32_t a = D == 128 ? sp[(8 * w + k0) * 8 + g] : sp[(8 * w + k0) * 4 + (g >> 1)];
                 uint32_t c = D == 128 ? sp[(8 * w + k1) * 8 + g] : sp[(8 * w + k1) * 4 + (g >> 1)];
-                if (edge) {      // slots behind the last key may hold anything, a NaN scale too
-                    if (pos0 + 8 * w + k0 >= sg.len + sg.n) a = 0u;
-                    if (pos0 + 8 * w + k1 >= sg.len + sg.n) c = 0u;
+                if (edge) {      // slots of absent nodes and behind the last key may hold anything, NaN scales too
+                    if ((a & 0x7fu) == 0x7fu) a = 0u;
+                    if ((c & 0x7fu) == 0x7fu) c = 0u;
                 }
                 vs[w] = e4m3x2_to_f16x2(__byte_perm(a, c, 0x0040));
 #pragma unroll

@@ -240,6 +240,8 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
                 if (have) {
                     c[a] = *reinterpret_cast<const uint4 *>(blk + part * 16);
                     s[a] = *reinterpret_cast<const unsigned short *>(scl + part * 2);
+                    // slots of absent nodes may hold anything: NaN scales among the draft nodes count as 0
+                    if (first + t * kTileKeys + in >= sg.len) s[a] &= ~(((((s[a] & 0x7f7fu) + 0x0101u) >> 7) & 0x0101u) * 0xffu);
                 }
             }
             __syncwarp();
@@ -397,7 +399,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         const int head = sg.head * p.group + (node >= 0 ? sg.row0 + row - node * p.group : 0);
         const bool idle = row - lane >= sg.rows;             // no query row in this warp
 
-        // ---- Q: this thread's row, scaled to fp16, into its swizzled tile (in four quarters: registers)
+        // ---- Q: this thread's row, scaled to fp16, into its swizzled tile
         float rs;                            // score scale of the row in log2 units
         {
             const uint4 *src = reinterpret_cast<const uint4 *>(p.q + 2 * (((int64_t)sg.b * p.N + (node >= 0 ? node : 0)) * p.q_row + head * p.q_head));
@@ -528,7 +530,11 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         if (tid == 0) sh->ok = *abort_flag == 0;
         softmax_sync();
         if (!sh->ok) {
-            if (tid == 0 && p.status) p.status[sg.b] = MARS_SEQ_TIMEOUT;
+            while (u < r.end) {              // nor is anything else of the block's share
+                const TileSegment rest = tile_segment(p, sh, r, u);
+                if (tid == 0 && p.status) p.status[rest.b] = MARS_SEQ_TIMEOUT;
+                u += rest.span;
+            }
             break;
         }
 

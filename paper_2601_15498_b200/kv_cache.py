@@ -23,7 +23,7 @@ from .mars import MarsError, _check, lib
 
 FP16 = 2
 MAX_SEQS = 8192
-STATUS = {0: "ok", 1: "bad tree", 5: "no room", 7: "out of pages", 8: "bad path", 9: "bad fork"}
+STATUS = {0: "ok", 1: "bad tree", 3: "timeout", 5: "no room", 7: "out of pages", 8: "bad path", 9: "bad fork"}
 
 _DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: FP16}
 
@@ -238,7 +238,9 @@ def gather(cache: KVCache, layer0: int, layers: int, start: torch.Tensor | None,
     dev = cache._index
     B = start.numel() if start is not None else count.numel() if count is not None else cache.seqs
     if out is None:
-        shape = (layers, B, int(rows), cache.kv_heads, cache.head_dim)
+        if rows is None:
+            raise MarsError("gather needs `rows` or `out`")
+        shape = (layers, B, rows, cache.kv_heads, cache.head_dim)
         out = (torch.zeros(shape, dtype=dtype, device=cache.device), torch.zeros(shape, dtype=dtype, device=cache.device))
     k, v = out
     shape = k.shape

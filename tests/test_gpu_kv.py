@@ -546,6 +546,41 @@ def test_attention_of_many_sequences_most_of_them_idle(B, N):
         check_attention(pr, q)
 
 
+@pytest.mark.parametrize("d,N,group", [(128, 7, 4), (64, 9, 1), (128, 60, 4), (64, 100, 2), (64, 130, 1)])
+def test_attention_of_trees_padded_with_nodes_that_were_never_appended(d, N, group):
+    """Behind a sequence's nodes the parents are -1 and the slots hold what they held, here NaN scales
+    in every byte; inside it too, and with parents that are no tree only the root's row is there."""
+    pr = Pair(pages=60, heads=2, d=d, page=32, seqs=3, width=16, seed=d + N)
+    pr.c.pages.fill_(0x7f)
+    pr.grow([70, 0, 33])
+    pr.resize([N] * 3)
+    real = [N // 2, 1, N]
+    pr.append(3, N, count=real)
+    parent = trees(np.random.default_rng(N), 3, N)
+    for b in range(3):
+        parent[b, real[b]:] = -1
+    q = torch.randn((3, N, 2 * group, d), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, parent=parent)
+    parent[1, 1:] = N + 3
+    check_attention(pr, q, parent=parent)
+
+
+@pytest.mark.parametrize("N,group", [(80, 4), (33, 1)])
+def test_attention_of_many_ragged_chains(N, group):
+    """More sequences than warps share the split of chains of several tiles."""
+    B = 70
+    rng = np.random.default_rng(N)
+    pr = Pair(pages=B * 11, heads=1, d=64, page=16, seqs=B, width=11, seed=N)
+    lens = [int(x) for x in rng.integers(0, 90, B)]
+    pr.grow(lens)
+    pr.resize([N] * B)
+    count = rng.integers(0, N + 1, B).astype(np.int32)
+    pr.append(B, N, count=count)
+    q = torch.randn((B, N, group, 64), device=DEV).to(torch.float16)
+    check_attention(pr, q, count=count)
+    check_attention(pr, q[:30].contiguous(), count=count[:30])
+
+
 def test_attention_of_an_idle_batch_writes_nothing():
     pr = Pair(pages=10, heads=2, d=64, page=16, seqs=3, width=4, seed=40)
     pr.grow([20, 3, 0])
