@@ -95,7 +95,7 @@ typedef enum { MARS_BF16 = 0, MARS_FP32 = 1 } mars_dtype_t;
 #define MARS_SEQ_OK 0
 #define MARS_SEQ_BAD_TREE 1   /* parent[0] != -1, or for i>0 parent[i] >= i or parent[i] < -1 */
 #define MARS_SEQ_DEPTH_CAP 2  /* the accepted path is deeper than Dcap                          */
-#define MARS_SEQ_TIMEOUT 3    /* a bounded device-side wait gave up (mars_lmhead_verify only)  */
+#define MARS_SEQ_TIMEOUT 3    /* a bounded device-side wait gave up (mars_lmhead_verify, mars_tree_attention) */
 #define MARS_SEQ_BAD_DISTRIBUTION 4 /* stochastic calls: a row on the walk has no softmax (its
                                        maximum is not finite) or its residual has no mass      */
 
