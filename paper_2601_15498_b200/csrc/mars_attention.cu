@@ -22,6 +22,11 @@
 //     are one vector, all of one scale.
 // The running maximum needs no reduction per block: a vote finds whether any score exceeds the row's
 // reference by 2^8; only then (rarely after the first blocks) is it recomputed and O rescaled.
+// Measured: 64 tokens over contexts of 300 to 32768 (8 KV heads of 4, 451 MB of cache) 104 us, 67 % of the copy
+// rate with launch and ragged ends; over 500000 tokens 455 us for 2.3 GB, 78 % of it.  There issue bounds it:
+// 54 % of the slots are taken and a warp's next instruction waits for its last one's result, with 16 warps per
+// SM.  Tiles of 32 rows, 255 registers and 8 warps per SM, take 200 us for 64 chains of 8 nodes (401 MB); of
+// 16 rows 133 us.  The tile kernel takes 244 us for the same chains, with rows or without, so 32 is the border.
 #include "mars_attention.cuh"
 #include "mars_hooks.cuh"
 
@@ -492,7 +497,8 @@ static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
 }
 
 // The kernel for tiles of query rows takes over where a KV head has more of them than the largest
-// tile of the other holds.
+// tile of the other holds.  Measured, us with rows / tiles: 64 chains of 8 nodes (32 rows) 200 / 235, of 4 nodes (16
+// rows) 133 / 234; one such chain 43 / 39, 4 chains 45 / 47, 16 chains 80 / 92.
 static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > kRowsMax && !(tree && N > kTileMaxTree); }
 static int attn_rows(int N, int group) { return (int64_t)N * group <= 8 ? 8 : (int64_t)N * group <= 16 ? 16 : 32; }
 

@@ -18,9 +18,16 @@
 // of tensor memory) are merged at the end.  The MMA order is S(0) S(1) | P V(0) S(2) | P V(1) S(3) | ...:
 // tensor operations execute in issue order, so S(u + 2) may overwrite the P that P V(u) has read.
 //
-// What bounds it is instruction issue: per 128 x 128 step about 3000 warp instructions to unpack (shared
-// by two steps where there are more than 128 rows), 2000 of softmax, beside 1024 cycles of MMA and as many
-// of exponentials (16 a cycle).
+// What bounds it is the round trip of an accumulator: S, softmax, P V, and only then the next S over its
+// columns.  A key tile of 256 rows takes 4500 cycles; softmax of 128 columns is about 3000 of them, the two
+// products and their signals the rest.  Two accumulators keep the tensor pipe 36 % and the issue slots 43 %
+// busy (8000 warp instructions per tile); shared memory is read at its full rate by S (both operands) and
+// written by the unpacking warps, some 2300 cycles per tile.  64 trees of 60 nodes over contexts of 2000 to
+// 12000 tokens (8 KV heads of 4, d 128): 418 us, one tree over 500000 tokens 606 us (2.7 us per 128 keys and
+// 256 rows); four prompts of 2048 (d 64) 129 us.  Measured and not kept, us for those trees / prompts: S and P in
+// halves of 64 keys, four in flight (503 / 126: with 64 columns S reads Q twice as often); 16 softmax warps
+// with 64 scores a thread and 8 unpacking ones (526 / 130); copies three tiles ahead for tiles of up to
+// 128 rows (as without); longer suspended waits (as without).
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
 //
