@@ -115,23 +115,25 @@ __device__ __forceinline__ uint32_t e2m1x8_from(const float *t)
     return r;
 }
 
-// Sixteen values against their scale: IEEE quotients x / sg, as the definition has it, in place.  With
-// 8-bit significands and a power of two as g many quotients lie exactly on the border of two codes,
-// where a reciprocal's last bit would decide.  Fast form: x * r and one residual correction
+// Sixteen values against their scale: the negated IEEE quotients -(x / sg), as the definition has them, in
+// place.  With 8-bit significands and a power of two as g many quotients lie exactly on the border of
+// two codes, where a reciprocal's last bit would decide.  Fast form: x * r and one residual correction
 // (Markstein 1990: with r the rounded reciprocal, fma(fma(-q, sg, x), r, q) is the rounded quotient
-// while nothing over- or underflows); |x / sg| <= 6.4 there, since the scale did not saturate.
+// while nothing over- or underflows), two values at a time; |x / sg| <= 6.4 there, since the scale did not
+// saturate.  The sign is turned since fma(0, r, -0) is +0 and a zero would lose its sign bit.
 __device__ __forceinline__ void quotients16(float (&x)[16], float sg, bool plain)
 {
     if (plain) {
-        const float r = __frcp_rn(sg);
+        const float r = -__frcp_rn(sg);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float q = __fmul_rn(x[i], r);
-            x[i] = __fmaf_rn(__fmaf_rn(-q, sg, x[i]), r, q);
+        for (int i = 0; i < 16; i += 2) {
+            asm("{\n\t.reg .b64 x, r, d, q, e;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 r, {%2, %2};\n\tmov.b64 d, {%3, %3};\n\t"
+                "mul.rn.f32x2 q, x, r;\n\tfma.rn.f32x2 e, q, d, x;\n\tfma.rn.f32x2 q, e, r, q;\n\tmov.b64 {%0, %1}, q;\n\t}"
+                : "+f"(x[i]), "+f"(x[i + 1]) : "f"(r), "f"(sg));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = sg > 0.0f ? __fdiv_rn(x[i], sg) : 0.0f;
+        for (int i = 0; i < 16; ++i) x[i] = sg > 0.0f ? -__fdiv_rn(x[i], sg) : -0.0f;
     }
 }
 
@@ -161,18 +163,21 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
     const int per_row = p.kv.kv_heads * 2 * kG, at_once = rows_at_once(per_row);
     const int lane_row = per_row >= 256 ? 0 : (int)threadIdx.x / per_row;
     if (lane_row >= at_once) return;
-    int row = blockIdx.x * at_once * p.iters + lane_row;
+    const int row0 = blockIdx.x * at_once * p.iters + lane_row;
+    // a thread keeps its head and place in the row and goes down the rows
 #pragma unroll 1
-    for (int it = 0; it < p.iters && row < n; ++it, row += at_once) {
-        const int pos = len + row, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+    for (int c = (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
+        const int h = c / (2 * kG), kv = (c / kG) & 1, grp = c % kG;
+        const int64_t stride = kv ? p.row[1] : p.row[0];
+        const unsigned char *src0 = (kv ? p.src[1] : p.src[0]) + ((int64_t)b * p.N * stride + h * (kv ? p.head[1] : p.head[0]) + grp * 16) * elem_bytes(DT);
+        const float g = p.scales[kv * p.kv.kv_heads + h];
+        int row = row0;
 #pragma unroll 1
-        for (int c = per_row >= 256 ? threadIdx.x : (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
-            if (id < 0) break;
-            const int h = c / (2 * kG), kv = (c / kG) & 1, grp = c % kG;
-            const unsigned char *src = (kv ? p.src[1] : p.src[0]) +
-                                       (((int64_t)b * p.N + row) * (kv ? p.row[1] : p.row[0]) + h * (kv ? p.head[1] : p.head[0]) + grp * 16) * elem_bytes(DT);
+        for (int it = 0; it < p.iters && row < n; ++it, row += at_once) {
+            const int pos = len + row, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+            if (id < 0) continue;
             float x[16];
-            load16<DT>(src, p.wide, x);
+            load16<DT>(src0 + row * stride * elem_bytes(DT), p.wide, x);
             float a = fabsf(x[0]);
 #pragma unroll
             for (int i = 1; i < 16; ++i) a = max_nan(a, fabsf(x[i]));
@@ -184,12 +189,11 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
                     a = fmaxf(a, fabsf(x[i]));
                 }
             }
-            const float g = p.scales[kv * p.kv.kv_heads + h];
             const uint32_t s8 = e4m3_from(__fdiv_rn(__fdiv_rn(a, 6.0f), g));
             const float sg = __fmul_rn(f16x2_to_float2(e4m3x2_to_f16x2(s8)).x, g);
             quotients16(x, sg, s8 != 0x7eu && sg > 1e-30f && sg < 1e30f);
             unsigned char *blk = kv_block<D>(p.kv, p.layer, id, h, pos);
-            *reinterpret_cast<uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8) = make_uint2(e2m1x8_from(x), e2m1x8_from(x + 8));
+            *reinterpret_cast<uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8) = make_uint2(e2m1x8_from(x) ^ 0x88888888u, e2m1x8_from(x + 8) ^ 0x88888888u);
             blk[16 * D + D * kv + slot * kG + grp] = (unsigned char)s8;
         }
     }
@@ -221,21 +225,24 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams p)
     if (lane_row >= at_once) return;
     unsigned char *layer = p.kv.pages + (int64_t)(p.layer0 + lay) * p.kv.layer_bytes;
     const float *scales = p.kv.scales + (int64_t)(p.layer0 + lay) * 2 * H;
-    int row = blockIdx.x * at_once * p.iters + lane_row;
+    const int row0 = blockIdx.x * at_once * p.iters + lane_row;
 #pragma unroll 1
-    for (int it = 0; it < p.iters && row < n; ++it, row += at_once) {
-        const int64_t pos64 = (int64_t)start + row;
-        if (pos64 < 0 || pos64 >= cap) continue;
-        const int pos = (int)pos64, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+    for (int c = (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
+        const int kv = c >= H * kG, h = (c / kG) - kv * H, grp = c % kG;
+        const float g = scales[kv * H + h];
+        unsigned char *dst = (kv ? p.dst[1] : p.dst[0]) + ((((int64_t)lay * p.B + b) * p.rows * H + h) * D + grp * 16) * elem_bytes(DT);
+        const int64_t dst_row = (int64_t)H * D * elem_bytes(DT);
+        int row = row0;
 #pragma unroll 1
-        for (int c = per_row >= 256 ? threadIdx.x : (int)threadIdx.x - lane_row * per_row; c < per_row; c += 256) {
-            if (id < 0) break;
-            const int kv = c >= H * kG, h = (c / kG) - kv * H, grp = c % kG;
+        for (int it = 0; it < p.iters && row < n; ++it, row += at_once) {
+            const int64_t pos64 = (int64_t)start + row;
+            if (pos64 < 0 || pos64 >= cap) continue;
+            const int pos = (int)pos64, id = kv_page_id(p.kv, b, pos), slot = pos & 15;
+            if (id < 0) continue;
             const unsigned char *blk = kv_block<D>(p.kv, layer, id, h, pos);
             const uint2 codes = *reinterpret_cast<const uint2 *>(blk + 8 * D * kv + slot * (D / 2) + grp * 8);
             const uint32_t s = e4m3x2_to_f16x2(blk[16 * D + D * kv + slot * kG + grp] * 0x101u);
             // code * scale is exact in fp16, so the product with g is the only rounding before the output's
-            const float g = scales[kv * H + h];
             float x[16];
             uint32_t hh[4];
 #pragma unroll
@@ -248,8 +255,7 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams p)
                     x[8 * w + 2 * j + 1] = f.y * g;
                 }
             }
-            const int64_t at = ((((int64_t)lay * p.B + b) * p.rows + row) * H + h) * D + grp * 16;
-            unsigned char *o = (kv ? p.dst[1] : p.dst[0]) + at * elem_bytes(DT);
+            unsigned char *o = dst + row * dst_row;
             uint32_t w[8];
             if constexpr (DT == MARS_FP32) {
 #pragma unroll

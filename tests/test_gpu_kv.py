@@ -160,6 +160,20 @@ def test_append_types_scales_and_special_values(dtype, scales):
     pr.stored()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_append_keeps_the_sign_of_zeros(dtype):
+    """-0 / (s * g) is -0 and has the code 8; under a scale of 0 all codes are 0."""
+    pr = Pair(d=64, page=16, seqs=2, width=4, seed=90)
+    pr.resize([9, 9, -2, -2][:pr.c.seqs])
+    k, v = pr.rand(2, 9, dtype), pr.rand(2, 9, dtype)
+    k[..., ::3] = -0.0
+    v[..., 1::2] = 0.0
+    v[:, 4] = -0.0
+    pr.append(2, 9, k=k, v=v)
+    pr.m.len[:2] = 9
+    pr.stored()
+
+
 def test_append_of_strided_slices_and_gather_back():
     pr = Pair(heads=2, d=128, page=64, seqs=3, width=4, seed=6)
     pr.resize([30, 30, 30])
