@@ -18,16 +18,17 @@
 // of tensor memory) are merged at the end.  The MMA order is S(0) S(1) | P V(0) S(2) | P V(1) S(3) | ...:
 // tensor operations execute in issue order, so S(u + 2) may overwrite the P that P V(u) has read.
 //
-// What bounds it is the round trip of an accumulator: S, softmax, P V, and only then the next S over its
-// columns.  A key tile of 256 rows takes 4500 cycles; softmax of 128 columns is about 3000 of them, the two
-// products and their signals the rest.  Two accumulators keep the tensor pipe 36 % and the issue slots 43 %
-// busy (8000 warp instructions per tile); shared memory is read at its full rate by S (both operands) and
-// written by the unpacking warps, some 2300 cycles per tile.  64 trees of 60 nodes over contexts of 2000 to
-// 12000 tokens (8 KV heads of 4, d 128): 418 us, one tree over 500000 tokens 606 us (2.7 us per 128 keys and
-// 256 rows); four prompts of 2048 (d 64) 129 us.  Measured and not kept, us for those trees / prompts: S and P in
-// halves of 64 keys, four in flight (503 / 126: with 64 columns S reads Q twice as often); 16 softmax warps
-// with 64 scores a thread and 8 unpacking ones (526 / 130); copies three tiles ahead for tiles of up to
-// 128 rows (as without); longer suspended waits (as without).
+// What bounds it: a key tile of 256 rows takes 4500 cycles, and nothing is full in them (issue slots 43 %, 8000
+// warp instructions; tensor pipe 36 %; shared memory about half).  S reads both operands from shared
+// memory at its full rate, beside the unpacking warps' stores, so that the MMA warp takes 1400 to 1700 cycles
+// for the two products of a step (1026 alone); softmax of a step takes about 3000 of an accumulator's 4500, and
+// two accumulators overlap only in part.  64 trees of 60 nodes over contexts of 2000 to 12000 tokens (8 KV heads of
+// 4, d 128): 418 us; one tree over 500000 tokens 606 us (2.7 us per 128 keys and 256 rows); four prompts of 2048
+// (4 KV heads of 4, d 64) 131 us.  Measured and not kept, us for those trees / prompts: S and P in halves of 64
+// keys, four in flight (503 / 126: with 64 columns S reads Q twice as often); 16 softmax warps with 64
+// scores a thread and 8 unpacking ones (526 / 130); P by the old reference in one pass over S, the
+// maximum looked at afterwards (412 / 135); copies three tiles ahead for tiles of up to 128 rows, longer
+// suspended waits (both as without).
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
 //

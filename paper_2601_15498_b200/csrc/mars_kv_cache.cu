@@ -4,10 +4,11 @@
 // their rows with a thread per 16 values (one scale); commit and fork move packed rows with 16-byte
 // loads; resize and fork's bookkeeping run in one thread block cluster / block, since the page
 // tables are a few hundred kilobytes at most and a grid-wide step would cost more than it moves.
-// Measured: append 70 us and gather 52 us for 49300 ragged rows of 8 heads of 128 (259 MB moved each: 3.7 and
-// 5.0 TB/s; append has the issue slots 74 % taken, by conversions and quotients); the rows of 64 forks' last
-// pages 22 us for 150 MB (6.8 TB/s), their tables 12 us; the page decisions of 2048 sequences 24 us, of 64
-// 11 us (latency of dependent steps: 5 % of the issue slots, nothing of DRAM); the paths out of 64 trees in four layers 6 us.
+// Measured: append and gather of 49300 ragged rows of 8 heads of 128 (259 MB moved each) 65 and
+// 49 us: 4.0 and 5.3 TB/s; issue bounds both (67 and 73 % of the slots, conversions and quotients).  The rows of
+// 64 forks' last pages 21 us for 150 MB (7.1 TB/s, partly in L2), their tables 12 us; the page decisions of 2048 sequences
+// 24 us, of 64 11 us (latency of dependent steps: 5 % of the issue slots, nothing of DRAM); the paths out of 64
+// trees in four layers 6 us.
 #include "mars_kv.cuh"
 #include "mars_stream.cuh"
 #include "mars_hooks.cuh"
