@@ -7,7 +7,7 @@
 // bits down to 2^-14 of the row's largest and an error below 2^-25 of it beyond.  The heads' fp32
 // scales are factored out of both sums.
 //
-// Kernel for few query rows per KV head (`attn_rows_kernel`, tiles of 8, 16 or 32 rows): bound by
+// Kernel for few query rows per KV head (`attn_rows_kernel`, tiles of 8, 16, 24 or 32 rows): bound by
 // reading the cache.  The page bytes go through a small shared-memory ring straight into the register
 // fragments of mma.sync -- no unpacked copy of K or V exists anywhere.  Keys and values are the 16-row
 // operand, the query rows the 8-column one, so a token of four heads to a KV head wastes half of a
@@ -40,8 +40,14 @@ constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = 32 * kRowsWarps;
 constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
 constexpr int kRowsMax = 32;          // largest tile
-constexpr int rows_occ(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }   // blocks per SM (registers)
-constexpr int rows_grid(int rows) { return kAttnSms * rows_occ(rows); }
+// Blocks per SM: as many as registers allow.  Measured, us with this many / one more: 64 tokens 109 / 151, 64 chains
+// of 4 nodes (16 rows) 132 / 225, of 6 nodes (24 rows) 157 / 176; d 64: 72 / 74, 82 / 84, 105 / 109, and of 8
+// nodes (32 rows) 130 / 132.  Tiles of 24 rows are there since chains of 6 nodes take 157 in them, 196 in tiles of 32.
+constexpr int rows_occ(int rows, int d)
+{
+    return d == 128 ? (rows == 8 ? 4 : rows == 16 ? 3 : 2) : (rows == 8 ? 4 : rows == 16 ? 3 : rows == 24 ? 3 : 2);
+}
+constexpr int rows_grid(int rows, int d) { return kAttnSms * rows_occ(rows, d); }
 constexpr int kUnit = RowsShape<8>::unit_keys(8);
 constexpr float kNone = 1e30f;
 
@@ -70,21 +76,23 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
 template <int D>
 __host__ __device__ constexpr int rows_slot_floats(int rows) { return rows * (D + 2); }
 
+__host__ __device__ constexpr bool rows_q_shared(int rows) { return rows >= 24; }
+
 template <int D>
 constexpr size_t rows_smem_bytes(int rows)
 {
     const size_t ring = (size_t)kRowsWarps * kRowsStages * kv_block_bytes(D), sums = (size_t)kRowsWarps * rows * (D + 4) * 4;
-    return (rows == kRowsMax ? (size_t)rows * D * 2 : 0) + (ring > sums ? ring : sums);
+    return (rows_q_shared(rows) ? (size_t)rows * D * 2 : 0) + (ring > sums ? ring : sums);
 }
 
 template <int D, int DT, int kRows>
-__global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows)) attn_rows_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_kernel(const AttnParams p)
 {
     pdl_launch_dependents();
     pdl_wait();
     using Shape = RowsShape<kRows>;
     constexpr int kNT = kRows / 8;            // n-tiles of query rows
-    constexpr bool kQShared = kRows == kRowsMax;   // Q fragments in shared memory (64 registers less)
+    constexpr bool kQShared = rows_q_shared(kRows);   // Q fragments in shared memory (48, 64 registers less)
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_par[MARS_MAX_NODES];
     __shared__ uint32_t s_mask[kRows * (MARS_MAX_NODES / 32)];
@@ -476,7 +484,7 @@ static mars_status_t rows_launch(const AttnParams &p, cudaStream_t st)
     if (rows_smem_bytes<D>(kRows) > 40 * 1024)
         e = cudaFuncSetAttribute(attn_rows_kernel<D, DT, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<D>(kRows));
     if (e == cudaSuccess)
-        e = launch_pdl(hook(kHookNoOverlap) == 0, attn_rows_kernel<D, DT, kRows>, dim3(rows_grid(kRows)), dim3(kRowsThreads),
+        e = launch_pdl(hook(kHookNoOverlap) == 0, attn_rows_kernel<D, DT, kRows>, dim3(rows_grid(kRows, D)), dim3(kRowsThreads),
                        rows_smem_bytes<D>(kRows), st, p);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     return MARS_OK;
@@ -485,10 +493,13 @@ static mars_status_t rows_launch(const AttnParams &p, cudaStream_t st)
 template <int D, int DT>
 static mars_status_t rows_launch(const AttnParams &p, int rows, cudaStream_t st)
 {
-    return rows == 8 ? rows_launch<D, DT, 8>(p, st) : rows == 16 ? rows_launch<D, DT, 16>(p, st) : rows_launch<D, DT, 32>(p, st);
+    return rows == 8    ? rows_launch<D, DT, 8>(p, st)
+           : rows == 16 ? rows_launch<D, DT, 16>(p, st)
+           : rows == 24 ? rows_launch<D, DT, 24>(p, st)
+                        : rows_launch<D, DT, 32>(p, st);
 }
 
-static_assert(rows_grid(8) * sizeof(unsigned) <= kAttnCounterBytes, "one counter per block");
+static_assert(rows_grid(8, 64) * sizeof(unsigned) <= kAttnCounterBytes && rows_grid(8, 128) * sizeof(unsigned) <= kAttnCounterBytes, "one counter per block");
 
 static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
 {
@@ -500,12 +511,16 @@ static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
 // tile of the other holds.  Measured, us with rows / tiles: 64 chains of 8 nodes (32 rows) 200 / 235, of 4 nodes (16
 // rows) 133 / 234; one such chain 43 / 39, 4 chains 45 / 47, 16 chains 80 / 92.
 static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > kRowsMax && !(tree && N > kTileMaxTree); }
-static int attn_rows(int N, int group) { return (int64_t)N * group <= 8 ? 8 : (int64_t)N * group <= 16 ? 16 : 32; }
+static int attn_rows(int N, int group)
+{
+    const int64_t rows = (int64_t)N * group;
+    return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : 32;
+}
 
 static size_t attn_workspace(int N, int group, int d)
 {
     const int n = attn_rows(N, group);
-    const size_t rows = sizeof(float) * 2 * rows_grid(n) * (size_t)(d == 128 ? rows_slot_floats<128>(n) : rows_slot_floats<64>(n));
+    const size_t rows = sizeof(float) * 2 * rows_grid(n, d) * (size_t)(d == 128 ? rows_slot_floats<128>(n) : rows_slot_floats<64>(n));
     const size_t tile = attn_use_tiles(N, group, false) ? attn_tile_partial_bytes(d) : 0;
     return kAttnCounterBytes + (rows > tile ? rows : tile);
 }

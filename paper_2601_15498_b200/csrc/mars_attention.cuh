@@ -28,7 +28,7 @@ namespace mars {
 template <int kRows>
 struct RowsShape {
     static __device__ constexpr int rows(int) { return kRows; }
-    static constexpr int kFixed = kRows == 32 ? 8 : 6, kLeast = 2;
+    static constexpr int kFixed = kRows >= 24 ? 8 : 6, kLeast = 2;
     static __host__ __device__ constexpr int unit_keys(int) { return 64; }
 };
 struct TileShape {

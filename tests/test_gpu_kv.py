@@ -164,7 +164,7 @@ def test_append_types_scales_and_special_values(dtype, scales):
 def test_append_keeps_the_sign_of_zeros(dtype):
     """-0 / (s * g) is -0 and has the code 8; under a scale of 0 all codes are 0."""
     pr = Pair(d=64, page=16, seqs=2, width=4, seed=90)
-    pr.resize([9, 9, -2, -2][:pr.c.seqs])
+    pr.resize([9, 9])
     k, v = pr.rand(2, 9, dtype), pr.rand(2, 9, dtype)
     k[..., ::3] = -0.0
     v[..., 1::2] = 0.0
@@ -530,6 +530,81 @@ def test_attention_at_the_borders_of_the_row_tiles(N, group):
     q = torch.randn((3, N, group, 128), device=DEV).to(torch.bfloat16)
     check_attention(pr, q)
     check_attention(pr, q, parent=trees(np.random.default_rng(N), 3, N), count=[N, N, max(N // 2, 1)])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("N,group", [(17, 1), (6, 4), (24, 1), (5, 5), (3, 8)])
+def test_attention_of_tiles_of_24_rows_and_beside_them(N, group, d):
+    pr = Pair(pages=60, heads=2, d=d, page=16, seqs=3, width=20, seed=N * group)
+    pr.grow([257, 15, 0])
+    pr.resize([N] * 3)
+    pr.append(3, N)
+    q = torch.randn((3, N, 2 * group, d), device=DEV).to(torch.float16)
+    check_attention(pr, q)
+    check_attention(pr, q, parent=trees(np.random.default_rng(N), 3, N, absent=0.1), count=[N, N, max(N // 2, 1)])
+
+
+def test_attention_of_a_tree_above_the_mask_store_with_few_rows_each():
+    """Trees that only the kernel for few rows takes, in tiles of 32 rows that begin inside a node's heads."""
+    pr = Pair(pages=60, heads=1, d=64, page=32, seqs=2, width=16, seed=131)
+    pr.grow([100, 1])
+    pr.resize([150] * 2)
+    pr.append(2, 150)
+    q = torch.randn((2, 150, 3, 64), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, parent=trees(np.random.default_rng(5), 2, 150, absent=0.03))
+
+
+def test_attention_of_a_prompt_of_many_tiles():
+    """More than 32 tiles of query rows in an item list: every lane of a warp holds more than one."""
+    pr = Pair(pages=60, heads=1, d=64, page=64, seqs=2, width=50, seed=132)
+    pr.grow([33, 0])
+    pr.resize([2300, 17])
+    pr.append(2, 2300, count=[2300, 17])
+    q = torch.randn((2, 2300, 4, 64), device=DEV).to(torch.bfloat16)
+    check_attention(pr, q, count=[2300, 17])
+
+
+def test_pools_beyond_32_bit_offsets():
+    """The same calls in a small pool and in one of 5.5 GB whose only free pages are its last ones: the same
+    rows, lengths and results, pages shifted."""
+    L, H, d, page, few = 2, 4, 128, 16, 40
+    many = 300000
+    caches = []
+    for n in (few, many):
+        c = kv.KVCache.empty(L, n, H, d, page, 6, 16, DEV)
+        if n == many:
+            c.free_bits.zero_()
+            c.free_bits[-1] = -1                     # 32 pages, and 8 before them
+            c.free_bits[-2] = -(1 << 24)
+        caches.append(c)
+    assert caches[1].pages.nbytes > 1 << 32 and many % 32 == 0
+    rng = np.random.default_rng(7)
+    k, v = (torch.as_tensor(rng.standard_normal((3, 70, H, d)), device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.as_tensor(rng.standard_normal((3, 70, 2 * H, d)), device=DEV).to(torch.bfloat16)
+    par = i32(trees(rng, 3, 30))
+    got = []
+    for c in caches:
+        r = []
+        kv.resize(c, i32([100, 70, 75, -2, -2, -2]))
+        for layer in range(L):
+            kv.append(c, layer, k, v, count=i32([70, 35, 64]))
+        kv.commit(c, None, i32([69, 34, 63]))
+        kv.resize(c, i32([30, 30, 30, -2, -2, -2]))
+        for layer in range(L):
+            kv.append(c, layer, v[:, :30].contiguous(), k[:, :30].contiguous())
+            r.append(kv.tree_attention(q[:, :30].contiguous(), c, layer, par))
+            r.append(kv.tree_attention(q[:, :3].contiguous(), c, layer))
+            r.append(kv.tree_attention(q[:, :1], c, layer))
+        kv.commit(c, i32([[0, 2, 5, 9]] * 3), i32([3, 2, 0]))
+        r.append(kv.fork(c, i32([0, 1]), i32([3, 5])))
+        r += kv.gather(c, 0, L, None, c.seq_len.clone(), rows=80)
+        kv.resize(c, i32([0, -1, 0, 16, -2, 0]))
+        r += [c.seq_len.clone(), c.seq_pages.clone(), c.block_table - (c.num_pages - few) * (c.block_table >= 0),
+              c.page_refs[c.num_pages - few:].clone()]
+        got.append(r)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert int(got[0][-3].sum()) > 0 and bool((caches[1].block_table.max() > many - few).item())
 
 
 @pytest.mark.parametrize("N", [128, 129])
