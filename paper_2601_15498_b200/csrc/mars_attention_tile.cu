@@ -27,8 +27,9 @@
 // (4 KV heads of 4, d 64) 131 us.  Measured and not kept, us for those trees / prompts: S and P in halves of 64
 // keys, four in flight (503 / 126: with 64 columns S reads Q twice as often); 16 softmax warps with 64
 // scores a thread and 8 unpacking ones (526 / 130); P by the old reference in one pass over S, the
-// maximum looked at afterwards (412 / 135); copies three tiles ahead for tiles of up to 128 rows, longer
-// suspended waits (both as without).
+// maximum looked at afterwards (412 / 135); the MMA warp waiting for V and the next K before P, with fewer
+// commits (436 / 132); a warp of its own for each accumulator's products (519 / 136); copies three tiles
+// ahead for tiles of up to 128 rows, longer suspended waits (both as without).
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
 //
