@@ -122,8 +122,8 @@ mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void
  *   Scores, maxima, sums and the output are accumulated in fp32; products run on the tensor cores
  *   with K, V and q exact in fp16 (q scaled by a power of two per row) and the probabilities rounded
  *   to fp16.  Results do not vary from run to run.
- *   workspace  mars_tree_attention_workspace_bytes() bytes, 256-byte aligned; two calls that may
- *              overlap on the GPU need separate workspaces.
+ *   workspace  mars_tree_attention_workspace_bytes() bytes (never less for a larger N, whatever B),
+ *              256-byte aligned; two calls that may overlap on the GPU need separate workspaces.
  */
 size_t mars_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_heads, int head_dim);
 mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const void *q, int64_t q_row,

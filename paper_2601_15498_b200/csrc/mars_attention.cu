@@ -519,8 +519,11 @@ static int attn_rows(int N, int group)
 
 static size_t attn_workspace(int N, int group, int d)
 {
-    const int n = attn_rows(N, group);
-    const size_t rows = sizeof(float) * 2 * rows_grid(n, d) * (size_t)(d == 128 ? rows_slot_floats<128>(n) : rows_slot_floats<64>(n));
+    size_t rows = 0;                     // what smaller calls need counts too, so that it never falls with N
+    for (int n = 8; n <= attn_rows(N, group); n += 8) {
+        const size_t need = sizeof(float) * 2 * rows_grid(n, d) * (size_t)(d == 128 ? rows_slot_floats<128>(n) : rows_slot_floats<64>(n));
+        rows = rows > need ? rows : need;
+    }
     const size_t tile = attn_use_tiles(N, group, false) ? attn_tile_partial_bytes(d) : 0;
     return kAttnCounterBytes + (rows > tile ? rows : tile);
 }

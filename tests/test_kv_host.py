@@ -107,6 +107,13 @@ def test_attention_refusals(lib):
         assert call(*args(**bad)) == 2, bad
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 3, 4, 8])
+def test_workspace_never_falls_with_the_nodes(lib, d, group):
+    size = [lib.mars_tree_attention_workspace_bytes(B, n, 2 * group, 2, d) for n in range(1, 300) for B in (1, 64)]
+    assert size[0::2] == size[1::2] and size[0] > 0 and (np.diff(size[0::2]) >= 0).all()
+
+
 def test_commit_fork_gather_refusals(lib):
     assert lib.mars_kv_commit(cache(), P, 4, N, 2, P, N, N) == 1
     assert lib.mars_kv_commit(cache(), P, 4, P, 2, N, N, N) == 1
