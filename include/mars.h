@@ -551,6 +551,8 @@ mars_status_t mars_device_check(int *sm_count, int *sm_tuned);
  *            consecutive calls; a measurement aid)
  *         4: mars_topk_rows: 1 = 8 vectors per batch and 4 blocks per SM, 2 = 4 vectors per
  *            batch and 6 blocks per SM, whatever the size
+ *         6: mars_tree_attention with more than 32 query rows per KV head: blocks from number value - 1
+ *            on give up at their first wait
  *   value 0 clears the hook.  Returns the previous value, or -1 for an unknown hook / negative value.
  */
 int mars_test_hook(int which, int value);

@@ -573,6 +573,8 @@ mars_status_t mars_tree_attention(const mars_kv_cache_t *cache, int layer, const
     p.B = B; p.N = N; p.group = q_heads / cache->kv_heads; p.tile_rows = 0;
     p.group_inv = p.group > 1 ? ~0ull / (unsigned)p.group + 1 : 0;
     p.scale_log2 = scale * 1.4426950408889634f;
+    const int give_up = hook(kHookAttentionGiveUp);
+    p.give_up = give_up ? (unsigned)give_up - 1u : ~0u;
     p.counters = (unsigned *)workspace;
     p.partial = (float *)((unsigned char *)workspace + kAttnCounterBytes);
     if (attn_use_tiles(N, p.group, parent != nullptr)) return attn_tile_launch(p, cache->head_dim, dt, st);

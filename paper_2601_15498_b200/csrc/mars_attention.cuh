@@ -54,6 +54,7 @@ struct AttnParams {
     int tile_rows;                   // query rows per tile of TileShape
     uint64_t group_inv;              // floor(2^64 / group) + 1 (unused for 1)
     float scale_log2;                // softmax scale * log2(e)
+    unsigned give_up;                // blocks from this one on give up (test hook)
     unsigned *counters;              // [grid]
     float *partial;                  // [2 * grid] slots of rows * (d + 2) floats
 };

@@ -295,7 +295,7 @@ __device__ __forceinline__ void tile_mma(const AttnParams &p, AttnRange r, TileS
     const uint64_t qdesc = umma_desc_k_sw128(q_at), kdesc = umma_desc_k_sw128(k_at), vdesc = umma_desc_mn_sw128(v_at, 128 * 128);
     uint32_t kst = 0, kpar = 0, vst = 0, vpar = 0;   // K and V stage in use, its phase
     uint32_t ppar[2] = {0, 0}, n_seg = 0;
-    bool ok = true;
+    bool ok = __all_sync(0xffffffffu, *abort_flag == 0) != 0;
     auto wait = [&](uint64_t *bar, uint32_t parity) {
         return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, abort_flag, &sh->word)) != 0;
     };
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
         }
         mbar_init(smem_u32(&sh->qfull), 8);
         mbar_init(smem_u32(&sh->drain), 1);
-        sh->abort = 0;
+        sh->abort = blockIdx.x >= p.give_up;
         sh->word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import hookctl as hooks
 from oracle import kv_oracle as ko
 from paper_2601_15498_b200 import kv_cache as kv, mars, synth
 
@@ -755,3 +756,45 @@ def test_quotients_on_every_border():
             code = raw[:, slot * 32:(slot + 1) * 32]
             assert np.array_equal(code & 15, m.code[0, p, slot, :, 0, 0::2]) and np.array_equal(code >> 4, m.code[0, p, slot, :, 0, 1::2])
             assert np.array_equal(raw[:, 16 * 64 + slot * 4:16 * 64 + slot * 4 + 4], m.scale[0, p, slot, :, 0])
+
+
+# ------------------------------------------------------------------------------------- waits that give up
+
+GIVE_UP = [("trees", 128, 60, 4), ("trees", 64, 33, 1), ("chain", 128, 100, 1), ("chain", 64, 90, 8)]
+
+
+def give_up_case(kind, d, N, group, seed=95):
+    """A batch for the kernel for many query rows: (pair, q, parent, count, call) with call(hook, workspace) ->
+    (out, status).  Sequence 3 has no work."""
+    rng = np.random.default_rng(seed)
+    pr = Pair(pages=260, heads=3, d=d, page=64, seqs=5, width=60, seed=seed)
+    pr.grow([1500, 40, 2100, 5, 900])
+    pr.resize([N] * 5)
+    pr.append(5, N)
+    q = torch.randn((5, N, 3 * group, d), device=DEV).to(torch.bfloat16)
+    parent = trees(rng, 5, N, absent=0.05) if kind == "trees" else None
+    count = [N, N - 1, N, 0, N // 2]
+
+    def call(hook, workspace):
+        hooks.set("HOOK_ATTENTION_GIVE_UP", hook)
+        out = torch.full(q.shape, 7.25, dtype=q.dtype, device=DEV)
+        st = torch.full((5,), -7, dtype=torch.int32, device=DEV)
+        kv.tree_attention(q, pr.c, 0, None if parent is None else i32(parent), count=i32(count), out=out, status=st,
+                          workspace=workspace)
+        torch.cuda.synchronize()
+        hooks.clear("HOOK_ATTENTION_GIVE_UP")
+        return out, host(st)
+    return pr, q, parent, count, call
+
+
+@pytest.mark.parametrize("kind,d,N,group", GIVE_UP)
+def test_waits_that_give_up_are_reported(kind, d, N, group):
+    """The kernel returns, every sequence with work says so, and with the workspace zeroed the next call is as ever."""
+    pr, q, parent, count, call = give_up_case(kind, d, N, group)
+    ws = kv.attention_workspace(q, pr.c)
+    good = check_attention(pr, q, parent=parent, count=count, workspace=ws)
+    out, st = call(1, ws)
+    assert st.tolist() == [3, 3, 3, 0, 3] and torch.equal(out[3], good[3])
+    ws.zero_()
+    out, st = call(0, ws)
+    assert torch.equal(out, good) and (st == 0).all()
