@@ -33,8 +33,10 @@
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
 //
-// Every wait is bounded.  One that gives up raises the block's abort flag; all roles fall through to
-// the common end, the sequence's status becomes MARS_SEQ_TIMEOUT, tensor memory is freed.
+// Every wait is bounded.  One that gives up raises the block's abort flag.  Unpacking and MMA then fall
+// through to the common end, where tensor memory is freed; the softmax warps walk the rest of the block's
+// segments without keys: their rows become NaN, shared items get a partial result of NaN and their arrival,
+// so that every counter is back at zero when the call ends, and the sequences say MARS_SEQ_TIMEOUT.
 #include "mars_attention.cuh"
 #include "mars_hooks.cuh"
 #include "mars_tcgen05.cuh"
@@ -69,7 +71,8 @@ struct TileSmem {
     uint64_t kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], odone[2];
     uint64_t qfull, drain;
     uint32_t tmem;
-    int abort, bad, last, ok;
+    int abort, bad, last;
+    int ok;                                             // no wait gave up up to the last segment's end
     unsigned word;
 };
 
@@ -409,8 +412,8 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         const bool idle = row - lane >= sg.rows;             // no query row in this warp
 
         // ---- Q: this thread's row, scaled to fp16, into its swizzled tile
-        float rs;                            // score scale of the row in log2 units
-        {
+        float rs = 0.0f;                     // score scale of the row in log2 units
+        if (sh->ok) {
             const uint4 *src = reinterpret_cast<const uint4 *>(p.q + 2 * (((int64_t)sg.b * p.N + (node >= 0 ? node : 0)) * p.q_row + head * p.q_head));
             uint4 w[D / 8];
 #pragma unroll
@@ -455,7 +458,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
 
         const uint32_t *mask = sh->mask + (tree && node >= 0 ? node : 0) * words;
         float mref = -INFINITY, l = 0.0f;    // reference maximum of the row in this accumulator, its sum
-        const int my = sg.two ? sg.tiles : (sg.tiles + 1 - acc) >> 1;        // this accumulator's key tiles
+        const int my = !sh->ok ? 0 : sg.two ? sg.tiles : (sg.tiles + 1 - acc) >> 1;   // this accumulator's key tiles
         bool ok = true;
         for (int j = 0; j < my; ++j, ++n_s) {
             const int pos0 = sg.key0 + (sg.two ? j : 2 * j + acc) * kTileKeys;
@@ -538,14 +541,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         tc_fence_after();
         if (tid == 0) sh->ok = *abort_flag == 0;
         softmax_sync();
-        if (!sh->ok) {
-            while (u < r.end) {              // nor is anything else of the block's share
-                const TileSegment rest = tile_segment(p, sh, r, u);
-                if (tid == 0 && p.status) p.status[rest.b] = MARS_SEQ_TIMEOUT;
-                u += rest.span;
-            }
-            break;
-        }
+        if (!sh->ok && tid == 0 && p.status) p.status[sg.b] = MARS_SEQ_TIMEOUT;
 
         // ---- result of the segment: with two halves a thread has its row, else half of d of it
         const bool merge = !sg.two && sg.tiles > 1;
@@ -561,6 +557,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                 m = mm;
             }
         }
+        if (!sh->ok) { m = -INFINITY; sum = NAN; }           // NaN rows here, and in whoever merges this
         const int d0 = sg.two ? 0 : acc * (D / 2), d1 = sg.two ? D : d0 + D / 2;
         const uint32_t o0 = oc + (sg.two ? 128 * acc : 0);
         const bool out_row = node >= 0 && (!tree || sh->live[node]);
@@ -575,7 +572,10 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                 float v[32];
                 tc_ld32_issue(o0 + c, v);
                 tc_ld32_wait(v);
-                if (merge) {
+                if (!sh->ok) {               // products may still be in flight
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = 0.0f;
+                } else if (merge) {
                     float x[32];
                     tc_ld32_issue(o0 + 128 + c, x);        // the second accumulator, same lanes
                     tc_ld32_wait(x);
@@ -678,6 +678,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnPa
         mbar_init(smem_u32(&sh->qfull), 8);
         mbar_init(smem_u32(&sh->drain), 1);
         sh->abort = blockIdx.x >= p.give_up;
+        sh->ok = 1;
         sh->word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }

@@ -798,3 +798,21 @@ def test_waits_that_give_up_are_reported(kind, d, N, group):
     ws.zero_()
     out, st = call(0, ws)
     assert torch.equal(out, good) and (st == 0).all()
+
+
+@pytest.mark.parametrize("kind,d,N,group", GIVE_UP)
+def test_rows_and_workspace_after_waits_that_gave_up(kind, d, N, group):
+    """What a block that gave up owes is NaN, everything else as ever, and the workspace serves the next call."""
+    pr, q, parent, count, call = give_up_case(kind, d, N, group)
+    ws = kv.attention_workspace(q, pr.c)
+    good, _ = call(0, ws)
+    untouched = (good == 7.25).all(-1)
+    missing = 0
+    for first in (1, 2, 9, 20, 30, 12):
+        out, st = call(first, ws)
+        same, none = (out == good).all(-1), out.isnan().all(-1)
+        assert bool((same | none).all()) and bool(same[untouched].all())
+        missing += int(none.sum())
+        out, st = call(0, ws)
+        assert torch.equal(out, good) and (st == 0).all(), first
+    assert missing
