@@ -116,7 +116,8 @@ mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void
  *   seq_status int32 [B] or NULL: MARS_SEQ_OK, MARS_SEQ_NO_ROOM (no row written), MARS_SEQ_BAD_TREE
  *              (only the root's row is computed).  MARS_SEQ_TIMEOUT: a bounded wait inside the kernel
  *              gave up (a second without progress); rows of that sequence that were not computed are
- *              NaN.  The other sequences' rows and the workspace are sound.
+ *              NaN.  The other sequences' rows and the workspace are sound.  With more than
+ *              32 query rows per KV head it costs one stream operation (the statuses begin as OK).
  *   Rows i >= count[b] and rows of absent nodes (parent -1, i > 0, and what hangs below them) stay as
  *   they were; the slots of such nodes in the cache need not have been written.
  *   Scores, maxima, sums and the output are accumulated in fp32; products run on the tensor cores

@@ -454,7 +454,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             status = attn_tree_masks(p, sg.b, sg.n, 0, sg.n, sh->par, sh->mask, words, sh->live, &sh->bad, tid, kSoftThreads,
                                      softmax_sync);
         }
-        if (tid == 0 && p.status && sg.head == 0 && sg.tile == 0 && sg.unit0 == 0) p.status[sg.b] = status;
+        if (tid == 0 && p.status && status != MARS_SEQ_OK) atomicMax(p.status + sg.b, status);
 
         const uint32_t *mask = sh->mask + (tree && node >= 0 ? node : 0) * words;
         float mref = -INFINITY, l = 0.0f;    // reference maximum of the row in this accumulator, its sum
@@ -541,7 +541,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
         tc_fence_after();
         if (tid == 0) sh->ok = *abort_flag == 0;
         softmax_sync();
-        if (!sh->ok && tid == 0 && p.status) p.status[sg.b] = MARS_SEQ_TIMEOUT;
+        if (!sh->ok && tid == 0 && p.status) atomicMax(p.status + sg.b, MARS_SEQ_TIMEOUT);
 
         // ---- result of the segment: with two halves a thread has its row, else half of d of it
         const bool merge = !sg.two && sg.tiles > 1;
@@ -737,6 +737,13 @@ static mars_status_t tile_launch(const AttnParams &p, cudaStream_t st)
 mars_status_t attn_tile_launch(const AttnParams &q, int d, int dt, cudaStream_t st)
 {
     AttnParams p = q;
+    // Blocks come to a sequence in any order, so none of them may write OK: the statuses begin there, and each
+    // block only raises what it has to say (OK < BAD_TREE < TIMEOUT)
+    static_assert(MARS_SEQ_OK == 0 && MARS_SEQ_BAD_TREE < MARS_SEQ_TIMEOUT, "statuses in rising order");
+    if (p.status && cudaMemsetAsync(p.status, 0, sizeof(int32_t) * p.B, st) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MARS_ERR_CUDA;
+    }
     p.tile_rows = (int64_t)p.B * p.kv.kv_heads * (((int64_t)p.N * p.group + 255) / 256) < kTileFewItems ? 128 : 256;
     if (d == 128) return dt == MARS_BF16 ? tile_launch<128, MARS_BF16>(p, st) : tile_launch<128, MARS_FP16>(p, st);
     return dt == MARS_BF16 ? tile_launch<64, MARS_BF16>(p, st) : tile_launch<64, MARS_FP16>(p, st);

@@ -816,3 +816,35 @@ def test_rows_and_workspace_after_waits_that_gave_up(kind, d, N, group):
         out, st = call(0, ws)
         assert torch.equal(out, good) and (st == 0).all(), first
     assert missing
+
+
+@pytest.mark.parametrize("d,group", [(128, 4), (64, 8)])
+def test_a_sequence_with_a_block_that_gave_up_never_says_ok(d, group):
+    """The block that reports on a sequence comes to it late, long after another block's waits for it ran out."""
+    N, lens = 60, [60000, 60000]
+    pr = Pair(pages=2000, heads=2, d=d, page=128, seqs=2, width=480, seed=96)
+    pr.resize([n + N for n in lens])
+    k = torch.randn((2, 60000 + N, 2, d), device=DEV).to(torch.bfloat16)
+    kv.append(pr.c, 0, k, k.flip(1))
+    pr.c.seq_len.copy_(i32(lens))
+    q = torch.randn((2, N, 2 * group, d), device=DEV).to(torch.bfloat16)
+    parent = i32(trees(np.random.default_rng(3), 2, N))
+    ws = kv.attention_workspace(q, pr.c)
+    st = torch.full((2,), -7, dtype=torch.int32, device=DEV)
+    good = kv.tree_attention(q, pr.c, 0, parent, status=st, workspace=ws)
+    assert (host(st) == 0).all()
+    told = set()
+    for first in [1, 20, 40, 60, 70, 74, 75, 76, 80, 90, 100, 110, 120, 130, 140, 146, 147, 148]:
+        for _ in range(3):
+            out = torch.full(q.shape, 7.25, dtype=q.dtype, device=DEV)
+            st.fill_(-7)
+            hooks.set("HOOK_ATTENTION_GIVE_UP", first)
+            kv.tree_attention(q, pr.c, 0, parent, out=out, status=st, workspace=ws)
+            torch.cuda.synchronize()
+            hooks.clear("HOOK_ATTENTION_GIVE_UP")
+            for b in range(2):
+                s = int(st[b])
+                told.add((b, s))
+                assert s in (0, 3) and (s == 3) == bool(out[b].isnan().any()), (first, b, s)
+                assert torch.equal(out[b][~out[b].isnan()], good[b][~out[b].isnan()])
+    assert told == {(0, 0), (0, 3), (1, 3)}
