@@ -75,7 +75,7 @@ typedef struct {
     int head_dim;         /* 64 or 128                                                             */
     int page_size;        /* 16, 32, 64 or 128 tokens                                              */
     int seqs;             /* <= MARS_KV_MAX_SEQS                                                   */
-    int table_width;
+    int table_width;      /* table_width * page_size <= 2^30, seqs * table_width < 2^31            */
 } mars_kv_cache_t;
 
 /* Bytes of the page pool of a cache with these sizes; 0 for unsupported sizes.  Host, pure. */

@@ -36,9 +36,10 @@ inline mars_status_t kv_check(const mars_kv_cache_t *c)
         ((uintptr_t)c->free_bits & 3))
         return MARS_ERR_INVALID_ARG;
     if ((c->head_dim != 64 && c->head_dim != 128) || kv_page_log2(c->page_size) < 0) return MARS_ERR_UNSUPPORTED;
-    // positions (table_width * page_size) stay below 2^30, page ids below 2^30
+    // positions (table_width * page_size) stay below 2^30, page ids below 2^30; the pages that all sequences
+    // together may ask for (seqs * table_width) below 2^31, since the prefix sums over them are 32-bit
     if (c->seqs > MARS_KV_MAX_SEQS || c->num_pages > (1 << 30) || c->kv_heads > 1024 || c->layers > 4096 ||
-        (long long)c->table_width * c->page_size > (1ll << 30))
+        (long long)c->table_width * c->page_size > (1ll << 30) || (long long)c->seqs * c->table_width >= (1ll << 31))
         return MARS_ERR_UNSUPPORTED;
     return MARS_OK;
 }

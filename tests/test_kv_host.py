@@ -152,3 +152,15 @@ def test_binding_checks_tensors():
     with pytest.raises(mars.MarsError, match="int32"):
         kv_cache._i32(t(4), 3, -1, "count")
     assert kv_cache._rows(t(3, 4, 9, 64, dt=torch.float32)[:, :, 2:4], 2, 64, -1, "k")[1:] == (576, 64)
+
+
+def test_tables_whose_requests_pass_32_bits_are_refused(lib):
+    """mars_kv_resize adds up pages in 32 bits: at most seqs * table_width of them can be asked for."""
+    for seqs, width in ((8192, 1 << 18), (32, 1 << 26), (8192, 1 << 26), (8191, 262177)):
+        c = cache(seqs=seqs, table_width=width, page_size=16)
+        assert seqs * width >= 1 << 31
+        assert lib.mars_kv_resize(c, P, N, N) == 3, (seqs, width)
+        assert lib.mars_kv_fork(c, P, P, 1, P, N) == 3, (seqs, width)
+    # the largest that is taken: refused for its missing argument only
+    for seqs, width in ((8192, (1 << 18) - 1), (31, 1 << 26), (1, 1 << 26)):
+        assert lib.mars_kv_resize(cache(seqs=seqs, table_width=width, page_size=16), N, N, N) == 1, (seqs, width)
