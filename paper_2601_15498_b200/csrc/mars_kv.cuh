@@ -23,6 +23,17 @@ inline int kv_page_log2(int page_size)
     return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : page_size == 128 ? 7 : -1;
 }
 
+// Bytes of one layer of the pool for sizes that each are in range (below 2^55), and of all of it; 0: no 63-bit count.
+inline int64_t kv_layer_bytes(int num_pages, int kv_heads, int head_dim, int page_size)
+{
+    return (int64_t)num_pages * kv_heads * (page_size / kKvBlock) * kv_block_bytes(head_dim);
+}
+inline int64_t kv_pool_bytes(int layers, int num_pages, int kv_heads, int head_dim, int page_size)
+{
+    const int64_t layer = kv_layer_bytes(num_pages, kv_heads, head_dim, page_size);
+    return layer <= INT64_MAX / layers ? layer * layers : 0;
+}
+
 // Host check of a descriptor: what every call needs of it.
 inline mars_status_t kv_check(const mars_kv_cache_t *c)
 {
@@ -41,6 +52,7 @@ inline mars_status_t kv_check(const mars_kv_cache_t *c)
     if (c->seqs > MARS_KV_MAX_SEQS || c->num_pages > (1 << 30) || c->kv_heads > 1024 || c->layers > 4096 ||
         (long long)c->table_width * c->page_size > (1ll << 30) || (long long)c->seqs * c->table_width >= (1ll << 31))
         return MARS_ERR_UNSUPPORTED;
+    if (kv_pool_bytes(c->layers, c->num_pages, c->kv_heads, c->head_dim, c->page_size) == 0) return MARS_ERR_UNSUPPORTED;
     return MARS_OK;
 }
 
@@ -64,7 +76,7 @@ inline KvView kv_view(const mars_kv_cache_t *c)
     v.seq_pages = c->seq_pages;
     v.scales = c->scales;
     v.page_log2 = kv_page_log2(c->page_size);
-    v.layer_bytes = (int64_t)c->num_pages * c->kv_heads * (c->page_size / kKvBlock) * kv_block_bytes(c->head_dim);
+    v.layer_bytes = kv_layer_bytes(c->num_pages, c->kv_heads, c->head_dim, c->page_size);
     v.num_pages = c->num_pages;
     v.kv_heads = c->kv_heads;
     v.table_width = c->table_width;

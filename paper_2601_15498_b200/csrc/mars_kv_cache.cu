@@ -814,7 +814,7 @@ size_t mars_kv_pool_bytes(int layers, int num_pages, int kv_heads, int head_dim,
     if (layers < 1 || num_pages < 1 || kv_heads < 1 || (head_dim != 64 && head_dim != 128) || kv_page_log2(page_size) < 0 ||
         num_pages > (1 << 30) || kv_heads > 1024 || layers > 4096)
         return 0;
-    return (size_t)layers * num_pages * kv_heads * (page_size / kKvBlock) * kv_block_bytes(head_dim);
+    return (size_t)kv_pool_bytes(layers, num_pages, kv_heads, head_dim, page_size);
 }
 
 mars_status_t mars_kv_append(const mars_kv_cache_t *cache, int layer, const void *k, int64_t k_row, int64_t k_head,

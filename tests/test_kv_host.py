@@ -164,3 +164,17 @@ def test_tables_whose_requests_pass_32_bits_are_refused(lib):
     # the largest that is taken: refused for its missing argument only
     for seqs, width in ((8192, (1 << 18) - 1), (31, 1 << 26), (1, 1 << 26)):
         assert lib.mars_kv_resize(cache(seqs=seqs, table_width=width, page_size=16), N, N, N) == 1, (seqs, width)
+
+
+def test_pools_whose_bytes_pass_63_bits_are_refused(lib):
+    """Sizes that are each in range, but whose product is no 63-bit count."""
+    big = dict(layers=4096, num_pages=1 << 30, kv_heads=1024, head_dim=128, page_size=128)
+    fits = dict(big, layers=400)
+    for kw in (big, dict(big, layers=500), dict(big, head_dim=64, layers=1000)):
+        assert kw["layers"] * kw["num_pages"] * kw["kv_heads"] * kw["page_size"] * kw["head_dim"] * 9 // 8 > (1 << 63) - 1
+        assert lib.mars_kv_pool_bytes(*kw.values()) == 0, kw
+        assert lib.mars_kv_resize(cache(**kw), N, N, N) == 3, kw
+        assert lib.mars_kv_gather(cache(**kw), 0, 1, 2, N, N, 0, P, P, 0, N) == 3, kw
+    want = fits["layers"] * fits["num_pages"] * fits["kv_heads"] * fits["page_size"] * 144
+    assert want < 1 << 63 and lib.mars_kv_pool_bytes(*fits.values()) == want
+    assert lib.mars_kv_resize(cache(**fits), N, N, N) == 1
