@@ -5,7 +5,7 @@ One decode cycle of a speculative-decoding program, with ``c`` a :class:`KVCache
     kv_cache.resize(c, extra)                               # room for the next tree's nodes
     for each layer:
         kv_cache.append(c, layer, k, v)                     # [B, N, kv_heads, d] of the draft nodes
-        o = kv_cache.tree_attention(q, c, layer, parent)    # [B, N, q_heads, d]
+        o = kv_cache.tree_attention(q, c, layer, parent, out=o, status=st, workspace=ws)    # [B, N, q_heads, d]
     out = mars.lmhead_verify(...)                           # or mars.verify_tree on logits
     kv_cache.commit(c, out["path_nodes"], out["accept_len"])
 
@@ -169,14 +169,16 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, parent: torch.Te
                    status: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """mars_tree_attention: q [B, N, q_heads, head_dim] over the cache; parent int32 [B, N], [N] or None
     (chains).  `workspace` comes from ``attention_workspace`` and is used by these calls only; without
-    one, a call allocates its own.  Rows without a result keep what `out` holds."""
+    one, a call allocates and clears its own.  Rows without a result (behind `count`, absent nodes, sequences
+    whose `status` is not 0) keep what `out` holds, and are zero in an output that the call allocates.  A
+    sequence whose status is 3 (timeout) has NaN in the rows that were not computed."""
     dev, H = cache._index, cache.kv_heads
     if q.dim() != 4 or q.shape[2] % H:
         raise MarsError("q must be [B, N, q_heads, head_dim] with q_heads a multiple of kv_heads")
     B, N, Hq, d = q.shape
     qp, qr, qh = _rows(q, Hq, cache.head_dim, dev, "q")
     if out is None:
-        out = torch.empty((B, N, Hq, d), dtype=q.dtype, device=cache.device)
+        out = torch.zeros((B, N, Hq, d), dtype=q.dtype, device=cache.device)
     op, orow, oh = _rows(out, Hq, cache.head_dim, dev, "out")
     if out.dtype is not q.dtype or out.shape != q.shape:
         raise MarsError("out must have the shape and dtype of q")

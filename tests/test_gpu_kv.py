@@ -848,3 +848,25 @@ def test_a_sequence_with_a_block_that_gave_up_never_says_ok(d, group):
                 assert s in (0, 3) and (s == 3) == bool(out[b].isnan().any()), (first, b, s)
                 assert torch.equal(out[b][~out[b].isnan()], good[b][~out[b].isnan()])
     assert told == {(0, 0), (0, 3), (1, 3)}
+
+
+@pytest.mark.parametrize("N", [3, 40])
+def test_rows_without_a_result_are_zero_in_an_output_of_the_calls_own(N):
+    """Short counts, absent nodes, no room, no tree: nothing of what the memory held before shows."""
+    pr = Pair(pages=60, heads=2, d=64, page=16, seqs=4, width=8, seed=97)
+    pr.grow([20, 16, 40, 5])
+    pr.resize([N, 0, N, N])
+    pr.append(4, N)
+    q = torch.randn((4, N, 4, 64), device=DEV).to(torch.bfloat16)
+    parent = trees(np.random.default_rng(1), 4, N)
+    parent[2, 1] = 2                              # no tree
+    parent[3, N - 1] = -1                         # absent
+    count = [N - 1, N, N, N]
+    par, cnt = i32(parent), i32(count)
+    held = [torch.full(q.shape, 9.0, dtype=q.dtype, device=DEV) for _ in range(50)]
+    places = {x.data_ptr() for x in held}
+    del held                                      # memory that held nines
+    out = kv.tree_attention(q, pr.c, 0, par, count=cnt)
+    assert out.data_ptr() in places
+    want = check_attention(pr, q, parent=parent, count=count, out=torch.zeros_like(q))
+    assert torch.equal(out, want) and bool((out[1] == 0).all()) and bool((out[0, N - 1] == 0).all())
