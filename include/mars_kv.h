@@ -173,8 +173,8 @@ mars_status_t mars_kv_resize(const mars_kv_cache_t *cache, const int32_t *extra,
 /*
  * Rows of the cache as values: for layers layer0 .. layer0+layers-1 and sequences b < B, positions
  * start[b] .. start[b] + count[b] - 1 to rows 0 .. of k_out and v_out, [layers][B][rows][kv_heads]
- * [head_dim] contiguous on 16-byte boundaries, of `dt` (MARS_BF16, MARS_FP32, MARS_FP16), rounded once;
- * `rows` is at most 2^24.  Rows from count[b]
+ * [head_dim] contiguous on 16-byte boundaries, of `dt` (MARS_BF16, MARS_FP32, MARS_FP16), rounded once
+ * (bf16 results below 2^-126 after a rounding to fp32); `rows` is at most 2^24.  Rows from count[b]
  * on, and positions that lie outside the sequence's pages, stay as they were.
  *   start      int32 [B] or NULL: 0.      count  int32 [B] or NULL: all `rows`.
  */

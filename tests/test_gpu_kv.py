@@ -870,3 +870,53 @@ def test_rows_without_a_result_are_zero_in_an_output_of_the_calls_own(N):
     assert out.data_ptr() in places
     want = check_attention(pr, q, parent=parent, count=count, out=torch.zeros_like(q))
     assert torch.equal(out, want) and bool((out[1] == 0).all()) and bool((out[0, N - 1] == 0).all())
+
+
+# ------------------------------------------------------------------------------------- rounding on the way out
+
+def round_once(x, dtype):
+    """64-bit values to the nearest of a type, ties to even, beyond its range to infinity."""
+    bits, low, top = {torch.bfloat16: (8, -126, 3.3895313892515355e38), torch.float16: (11, -14, 65504.0),
+                      torch.float32: (24, -126, 3.4028234663852886e38)}[dtype]
+    e = np.maximum(np.frexp(x)[1] - 1, low)
+    step = np.exp2(e - (bits - 1.0))
+    y = np.rint(x / step) * step
+    return np.where(np.abs(y) > top, np.copysign(np.inf, y), y)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_gather_rounds_once(dtype):
+    """Every code under every scale byte, under head scales for which a product rounded to fp32 and then again is
+    another number, and under the smallest and largest ones."""
+    rng = np.random.default_rng(100)
+    f = np.unique(np.outer(ko.E2M1, ko.E4M3))
+    hard = []
+    while len(hard) < 12 and dtype != torch.float32:
+        g = (rng.uniform(1.0, 2.0, 20000) * np.exp2(rng.integers(-9, 9, 20000))).astype(np.float32)
+        x = f[None, :] * g[:, None].astype(np.float64)
+        hard += g[(round_once(round_once(x, torch.float32), dtype) != round_once(x, dtype)).any(1)].tolist()
+    g = rng.uniform(1.0, 2.0, 240).astype(np.float32)
+    g = np.concatenate([np.float32(hard), (g[:200] * np.float32(2.0 ** -100)) * np.exp2(rng.integers(-40, 0, 200)).astype(np.float32),
+                        g[200:240] * np.float32(2.0 ** 118), np.exp2(rng.integers(-149, 128, 40)).astype(np.float32),
+                        np.float32([1.401298464324817e-45, 1.1754942106924411e-38, 1.1754943508222875e-38, 3.4028234663852886e38])])
+    g = np.maximum(g, np.float32(1.401298464324817e-45))
+    H = len(g)
+    c = kv.KVCache.empty(1, 2, H, 64, 16, 1, 2, DEV, scales=np.stack([g, g[::-1]])[None])
+    kv.resize(c, i32([32]))
+    page = np.zeros((2, 1152), np.uint8)           # token t, group j: scale byte 4 t + j; codes 0 .. 15 in each
+    for t in range(32):
+        p, s = divmod(t, 16)
+        for side in range(2):
+            at = 512 * side + s * 32
+            page[p, at:at + 32] = np.tile(np.arange(0, 16, 2) | (np.arange(1, 16, 2) << 4), 4)
+            page[p, 1024 + 64 * side + s * 4:1024 + 64 * side + s * 4 + 4] = np.minimum(np.arange(4 * t, 4 * t + 4), 126)
+    c.pages.copy_(torch.as_tensor(page)[None, :, None, :].expand(1, 2, H, 1152))
+    k, v = kv.gather(c, 0, 1, i32([0]), i32([32]), rows=32, dtype=dtype)
+    codes = np.tile(np.arange(16), 4)[None]
+    mag = ko.values(np.repeat(codes, 32, 0), np.minimum(np.arange(128).reshape(32, 4), 126), 1.0)
+    for got, gs in ((k, g), (v, g[::-1])):
+        true = mag[:, None, :] * gs[None, :, None].astype(np.float64)
+        got, want = got[0, 0].double().cpu().numpy(), round_once(true, dtype)
+        # bf16 below its normal numbers goes through fp32: off by half a step, 2^-134, and half an fp32 step more
+        low = (np.abs(true) < 2.0 ** -126) & (dtype == torch.bfloat16)
+        assert np.array_equal(got[~low], want[~low]) and (np.abs(got - true)[low] <= 2.0 ** -134 + 2.0 ** -149).all()
