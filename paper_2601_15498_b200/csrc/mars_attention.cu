@@ -49,7 +49,7 @@ constexpr int rows_occ(int rows, int d)
 }
 constexpr int rows_grid(int rows, int d) { return kAttnSms * rows_occ(rows, d); }
 constexpr int kUnit = RowsShape<8>::unit_keys(8);
-constexpr float kNone = 1e30f;
+constexpr float kNone = -3.40282347e38f;     // reference maximum before a row's first key
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
@@ -71,6 +71,15 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
     return r;
+}
+
+// x = (s - ref) * rs + 7, two at a time (both halves rounded as by themselves)
+__device__ __forceinline__ void score2(float &x0, float &x1, float s0, float s1, float r0, float r1, float m0, float m1)
+{
+    asm("{\n\t.reg .b64 s, r, m, c, o;\n\tmov.b64 s, {%2, %3};\n\tmov.b64 r, {%4, %5};\n\tmov.b64 m, {%6, %7};\n\t"
+        "mov.b64 c, {0f40E00000, 0f40E00000};\n\tmov.b64 o, {0fBF800000, 0fBF800000};\n\t"
+        "fma.rn.f32x2 s, r, o, s;\n\tfma.rn.f32x2 s, s, m, c;\n\tmov.b64 {%0, %1}, s;\n\t}"
+        : "=f"(x0), "=f"(x1) : "f"(s0), "f"(s1), "f"(r0), "f"(r1), "f"(m0), "f"(m1));
 }
 
 template <int D>
@@ -97,7 +106,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
     __shared__ int s_par[MARS_MAX_NODES];
     __shared__ uint32_t s_mask[kRows * (MARS_MAX_NODES / 32)];
     __shared__ unsigned char s_live[kRows];
-    __shared__ float s_m[kRowsWarps][kRows], s_l[kRowsWarps][kRows];
+    __shared__ float s_m[kRowsWarps][kRows], s_l[kRowsWarps][kRows], s_rs[kRows];
     __shared__ int s_last;
     __shared__ AttnSeqs s_seqs;
     constexpr int kBlk = kv_block_bytes(D);
@@ -192,7 +201,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
             float down, up;
             row_scale(m, &down, &up);
-            const float scale = fmaxf(p.scale_log2 * p.scales[sg.head] * up, 1.17549435e-38f);
+            const float scale = row_log2(p, sg.head, up);
+            if (warp == 0 && t == 0) s_rs[8 * n + g] = scale;
             const int local = in ? nd - node0 : -1;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -220,11 +230,11 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
             for (int n = 0; n < kNT; ++n)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[j][n][k] = 0.0f;
-        // base = 7 - reference maximum; kNone stands for "no key yet" and needs no case of its own: every
-        // score exceeds it, and ex2 of anything minus it is 0
-        float base[kNT][2], l[kNT][2];
+        // reference maximum; kNone needs no case of its own: scores exceed it by so much that they replace it,
+        // unless all of them come to nothing in log2 units (then any reference is as good)
+        float ref[kNT][2], l[kNT][2];
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) { base[n][0] = base[n][1] = kNone; l[n][0] = l[n][1] = 0.0f; }
+        for (int n = 0; n < kNT; ++n) { ref[n][0] = ref[n][1] = kNone; l[n][0] = l[n][1] = 0.0f; }
         // rows and columns of the 16-key tile are permuted inside pairs so that neither the K rows nor the
         // V rows that a quarter warp reads together fall on the same banks
         const int key = (g & 6) + ((g ^ (g >> 1)) & 1);
@@ -323,26 +333,26 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
 #pragma unroll
             for (int n = 0; n < kNT; ++n)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[n][k] = fmaf(s[n][k], rs[n][k & 1], base[n][k & 1]);
-                    top = fmaxf(top, x[n][k]);
+                for (int k = 0; k < 4; k += 2) {
+                    score2(x[n][k], x[n][k + 1], s[n][k], s[n][k + 1], ref[n][0], ref[n][1], rs[n][0], rs[n][1]);
+                    top = fmaxf(top, fmaxf(x[n][k], x[n][k + 1]));
                 }
             if (__any_sync(0xffffffffu, top > 15.0f)) {
 #pragma unroll
                 for (int n = 0; n < kNT; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[n][e], s[n][2 + e]) * rs[n][e];
+                        float mx = fmaxf(s[n][e], s[n][2 + e]);
 #pragma unroll
                         for (int k = 4; k < 32; k <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
-                        if (mx + base[n][e] > 15.0f) {
-                            const float f = ex2(7.0f - mx - base[n][e]);
-                            base[n][e] = 7.0f - mx;
+                        if ((mx - ref[n][e]) * rs[n][e] > 8.0f) {
+                            const float f = ex2((ref[n][e] - mx) * rs[n][e]);
+                            ref[n][e] = mx;
                             l[n][e] *= f;
 #pragma unroll
                             for (int j = 0; j < kSteps; ++j) { o[j][n][e] *= f; o[j][n][2 + e] *= f; }
-                            x[n][e] = fmaf(s[n][e], rs[n][e], base[n][e]);
-                            x[n][2 + e] = fmaf(s[n][2 + e], rs[n][e], base[n][e]);
+                            x[n][e] = fmaf(s[n][e] - mx, rs[n][e], 7.0f);
+                            x[n][2 + e] = fmaf(s[n][2 + e] - mx, rs[n][e], 7.0f);
                         }
                     }
             }
@@ -396,7 +406,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
 #pragma unroll
                 for (int k = 4; k < 32; k <<= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
                 const int row = 8 * n + 2 * t + e;
-                if (g == 0) { s_m[warp][row] = 7.0f - base[n][e]; s_l[warp][row] = x; }
+                if (g == 0) { s_m[warp][row] = ref[n][e]; s_l[warp][row] = x; }
                 float *to = s_o + (warp * kRows + row) * (D + 4) + g * (D / 8);
 #pragma unroll
                 for (int j = 0; j < kSteps; j += 2)
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
             for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
 #pragma unroll
             for (int w = 0; w < kRowsWarps; ++w) {
-                const float f = ex2(s_m[w][orow] - m);
+                const float f = ex2((s_m[w][orow] - m) * s_rs[orow]);
                 sum += s_l[w][orow] * f;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) acc[k] += s_o[(w * kRows + orow) * (D + 4) + od + k] * f;
@@ -451,7 +461,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
             if (write) {
                 __threadfence();
                 for (int orow = tid / kAcross; orow < rows; orow += kAtOnce) {
-                    float m = -kNone, sum = 0.0f, acc[kPer];
+                    float m = kNone, sum = 0.0f, acc[kPer];
 #pragma unroll
                     for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
 #pragma unroll 4
@@ -461,7 +471,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_ke
                         const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od));
                         const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + orow * D + od + 4));
                         const float mm = fmaxf(m, pm);
-                        const float a = ex2(m - mm), b = ex2(pm - mm);
+                        const float a = ex2((m - mm) * s_rs[orow]), b = ex2((pm - mm) * s_rs[orow]);
                         m = mm;
                         sum = sum * a + pl * b;
                         acc[0] = acc[0] * a + x.x * b; acc[1] = acc[1] * a + x.y * b; acc[2] = acc[2] * a + x.z * b; acc[3] = acc[3] * a + x.w * b;

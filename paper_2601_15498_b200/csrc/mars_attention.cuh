@@ -59,6 +59,10 @@ struct AttnParams {
     float *partial;                  // [2 * grid] slots of rows * (d + 2) floats
 };
 
+// The reference maximum of a row is kept in units of S = q K^T (q scaled, see row_scale), where it is finite and
+// exact; `rs` (below) brings differences of scores to log2 units.  Kept in log2 units, its rounding would pass
+// the 2^15 that P has room for once scores pass 2^28, and overflow with them.
+
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -303,6 +307,12 @@ __device__ __forceinline__ AttnSegment attn_segment(const AttnParams &p, const A
     s.c1 = (int)attn_div(item + S::kFixed + s.units - 1, r.per);
     s.item = item;
     return s;
+}
+
+// Score scale of a query row in log2 units: never 0 or infinite, so that differences of 0 and of infinity stay that.
+__device__ __forceinline__ float row_log2(const AttnParams &p, int head, float up)
+{
+    return fminf(fmaxf(p.scale_log2 * p.scales[head] * up, 1.17549435e-38f), 3.40282347e38f);
 }
 
 template <int DT>

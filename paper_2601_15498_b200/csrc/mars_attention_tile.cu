@@ -430,7 +430,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             }
             float down, up;
             row_scale(m, &down, &up);
-            rs = fmaxf(p.scale_log2 * p.scales[sg.head] * up, 1.17549435e-38f);
+            rs = row_log2(p, sg.head, up);
             if (sg.two || acc == 0) {
                 unsigned char *dst = q_tiles + acc * tile_bytes<D>() + rr * 128;
 #pragma unroll
@@ -458,6 +458,8 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
 
         const uint32_t *mask = sh->mask + (tree && node >= 0 ? node : 0) * words;
         float mref = -INFINITY, l = 0.0f;    // reference maximum of the row in this accumulator, its sum
+        float minus = 0.0f;
+        bool far = false;                    // the row's scores are beyond the fused step
         const int my = !sh->ok ? 0 : sg.two ? sg.tiles : (sg.tiles + 1 - acc) >> 1;   // this accumulator's key tiles
         bool ok = true;
         for (int j = 0; j < my; ++j, ++n_s) {
@@ -490,13 +492,16 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             tc_ld32_issue(sc + 96, x);
             tc_ld32_wait(x);
             if (edge) mask32(x, visible32(pos0 + 96, sg.len, node, tree, mask, words));
-            mx = fmaxf(mx, max32(x)) * rs;
+            mx = fmaxf(mx, max32(x));
             // the reference moves only when a score exceeds it by more than 2^8; the first tile just sets it
-            const bool grow = mx > mref + 8.0f;
-            if (__any_sync(0xffffffffu, grow)) {
-                const float to = grow ? mx : mref;
-                const float f = to == -INFINITY || mref == to ? 1.0f : ex2(mref - to);
-                mref = to;
+            const bool grow = (mx - mref) * rs > 8.0f;
+            if (__any_sync(0xffffffffu, grow || far)) {
+                const float f = grow ? ex2((mref - mx) * rs) : 1.0f;
+                if (grow) {
+                    mref = mx;
+                    far = fabsf(mx * rs) > 4096.0f;
+                    minus = far ? 7.0f : 7.0f - mx * rs;
+                }
                 l *= f;
                 if (j > 0) {
                     // P V of the accumulator's tile before is complete: the S that was just read came after it
@@ -513,9 +518,25 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
                         tc_st8(oc + 128 * acc + c + 8, z);
                     }
                 }
+                if (__any_sync(0xffffffffu, far)) {
+                    const float less = far ? mref : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 64; ++k) v[k] -= less;
+#pragma unroll 1
+                    for (int c = 64; c < 128; c += 8) {
+                        float y[8];
+                        uint32_t z[8];
+                        tc_ld8(sc + c, y);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[k] - less);
+                        tc_st8(sc + c, z);
+                    }
+                    tc_wait_st();
+                }
             }
-            // P = 2^(s - mref + 7), see mars_attention.cu; over columns of S that were read for good
-            const float minus = mref == -INFINITY ? 0.0f : 7.0f - mref;
+            // P = 2^((s - mref) * rs + 7), see mars_attention.cu; over columns of S that were read for good.  A fused
+            // step per score, s * rs + minus with minus = 7 - mref * rs, off by 2^-13 at most below scores of 2^12; of
+            // rows beyond that (`far`) mref is off S already
             float l4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             exp64(v, rs, minus, sc, l4);
             tc_ld32_issue(sc + 64, v);
@@ -551,8 +572,8 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
             sum = sh->xl[0][rr];
             if (merge) {
                 const float m1 = sh->xm[1][rr], mm = fmaxf(m, m1);
-                f0 = m == -INFINITY ? 0.0f : ex2(m - mm);
-                f1 = m1 == -INFINITY ? 0.0f : ex2(m1 - mm);
+                f0 = m == -INFINITY ? 0.0f : ex2((m - mm) * rs);
+                f1 = m1 == -INFINITY ? 0.0f : ex2((m1 - mm) * rs);
                 sum = sum * f0 + sh->xl[1][rr] * f1;
                 m = mm;
             }
@@ -623,7 +644,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
 #pragma unroll
                             for (int k = 0; k < 32; ++k) x[k] = __ldcg(src + k * TileShape::kMost);
                             const float mm = fmaxf(m, pm);
-                            const float a = m == -INFINITY ? 0.0f : ex2(m - mm), b = pm == -INFINITY ? 0.0f : ex2(pm - mm);
+                            const float a = m == -INFINITY ? 0.0f : ex2((m - mm) * rs), b = pm == -INFINITY ? 0.0f : ex2((pm - mm) * rs);
                             m = mm;
                             sum = sum * a + pl * b;
 #pragma unroll

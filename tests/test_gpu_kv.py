@@ -920,3 +920,58 @@ def test_gather_rounds_once(dtype):
         # bf16 below its normal numbers goes through fp32: off by half a step, 2^-134, and half an fp32 step more
         low = (np.abs(true) < 2.0 ** -126) & (dtype == torch.bfloat16)
         assert np.array_equal(got[~low], want[~low]) and (np.abs(got - true)[low] <= 2.0 ** -134 + 2.0 ** -149).all()
+
+
+# ------------------------------------------------------------------------------------- extreme rows of q
+
+def check_huge(pr, q, parent=None):
+    """Rows whose best score is ahead of the next by more than both can be off are that key's V; all rows lie
+    between V's smallest and largest value.  A score is a sum of d products with fp32 accumulation, off by at most
+    d * 2^-23 of sum |q||k|, and four more roundings at 2^-23 of its size; a lead of 60 beyond that leaves
+    e^-60 of each other key.  P of the best key is 2^7 and rounds to fp16 by 2^-11 at most."""
+    B, N, Hq, d = q.shape
+    st = torch.full((B,), -7, dtype=torch.int32, device=DEV)
+    out = torch.full(q.shape, 7.25, dtype=q.dtype, device=DEV)
+    kv.tree_attention(q, pr.c, 0, None if parent is None else i32(parent), out=out, status=st)
+    assert (host(st) == 0).all()
+    got, qq = host(out).astype(np.float64), q.double().cpu().numpy()
+    half, ahead = torch.finfo(q.dtype).eps / 2, 0
+    for b in range(B):
+        ln = int(pr.m.len[b])
+        see, _, _ = ko.ancestors(None if parent is None else parent[b], N)
+        k, v = pr.m.rows(0, b, 0, ln + N)
+        for i in range(N):
+            use = np.concatenate([np.arange(ln), ln + np.flatnonzero(see[i])])
+            for h in range(Hq):
+                kk, vv = k[use, h * pr.m.H // Hq], v[use, h * pr.m.H // Hq]
+                z = kk @ qq[b, i, h] * d ** -0.5
+                off = (d + 4) * 2.0 ** -23 * (np.abs(kk) @ np.abs(qq[b, i, h])).max() * d ** -0.5
+                top = int(z.argmax())
+                x, lo, hi = got[b, i, h], vv.min(0), vv.max(0)
+                slack = (2.0 ** -10 + half) * np.maximum(np.abs(lo), np.abs(hi))
+                assert ((x >= lo - slack) & (x <= hi + slack)).all(), (b, i, h, z[top])
+                if np.delete(z, top).max(initial=-np.inf) < z[top] - 2 * off - 60:
+                    ahead += 1
+                    rest = len(use) * np.exp(-60.0) * np.abs(vv).max(0)     # where the best key's V is 0
+                    assert (np.abs(x - vv[top]) <= (2.0 ** -10 + half) * np.abs(vv[top]) + rest).all(), (b, i, h, z[top])
+    return ahead
+
+
+@pytest.mark.parametrize("N", [2, 60])
+@pytest.mark.parametrize("dtype,qmag,kscale", [(torch.float16, 500.0, 1.0), (torch.float16, 1.2e4, 2.0 ** 6), (torch.float16, 1.2e4, 2.0 ** 14),
+                                               (torch.bfloat16, 1e12, 2.0 ** 4), (torch.bfloat16, 1e30, 2.0 ** 10),
+                                               (torch.bfloat16, 1e37, 2.0 ** 30), (torch.bfloat16, 1e30, 2.0 ** -90)])
+def test_attention_of_huge_scores(N, dtype, qmag, kscale):
+    pr = Pair(pages=80, heads=1, d=128, page=16, seqs=3, width=20, seed=101)
+    g = np.array([[[kscale], [1.0]]], np.float32)
+    pr.c.scales.copy_(torch.as_tensor(g))
+    pr.m.scales = g
+    pr.resize([203 + N, 17 + N, N])
+    k, v = ((pr.rand(3, 203 + N, torch.float32, loud=False) * s).contiguous() for s in (kscale, 1.0))
+    pr.append(3, 203 + N, torch.float32, count=[203 + N, 17 + N, N], k=k, v=v)
+    pr.m.len[:] = [203, 17, 0]
+    pr.c.seq_len.copy_(i32(pr.m.len))
+    q = (torch.randn((3, N, 4, 128), device=DEV) * qmag).to(dtype)
+    assert bool(torch.isfinite(q).all())
+    assert check_huge(pr, q) > 6 * N
+    assert check_huge(pr, q, parent=trees(np.random.default_rng(N), 3, N)) > 6 * N
