@@ -326,10 +326,10 @@ __device__ __forceinline__ float2 widen2(uint32_t w)
 __device__ __forceinline__ void row_scale(float m, float *down, float *up)
 {
     const uint32_t e = (__float_as_uint(m) >> 23) & 0xffu;
-    if (e == 0u || e >= 254u) { *down = e == 0u ? 1.0f : 0.0078125f; *up = e == 0u ? 1.0f : 128.0f; }
+    if (e == 0u || e >= 254u) { *down = e == 0u ? 1.0f : 0x1p-127f; *up = e == 0u ? 1.0f : 0x1p127f; }
     else { *down = __uint_as_float((254u - e) << 23); *up = __uint_as_float(e << 23); }
     // e == 0: zero or subnormal rows count as they are (their products vanish next to any other term);
-    // e >= 254: the row's fp16 form would need 2^-127; 2^-7 leaves infinities to the conversion
+    // e >= 254: 2^-127 is subnormal; infinities stay infinities
 }
 
 // 8 consecutive output values at element `at` (16-byte aligned).

@@ -975,3 +975,27 @@ def test_attention_of_huge_scores(N, dtype, qmag, kscale):
     assert bool(torch.isfinite(q).all())
     assert check_huge(pr, q) > 6 * N
     assert check_huge(pr, q, parent=trees(np.random.default_rng(N), 3, N)) > 6 * N
+
+
+@pytest.mark.parametrize("N", [2, 60])
+@pytest.mark.parametrize("kscale", [2.0 ** -120, 2.0 ** -70, 1.0])
+def test_attention_of_the_largest_finite_q(N, kscale):
+    """Rows of bf16 q whose largest element is 2^127 or more, over small and ordinary K."""
+    pr = Pair(pages=80, heads=1, d=64, page=16, seqs=3, width=20, seed=102)
+    g = np.array([[[kscale], [1.0]]], np.float32)
+    pr.c.scales.copy_(torch.as_tensor(g))
+    pr.m.scales = g
+    pr.resize([203 + N, 17 + N, N])
+    k, v = ((pr.rand(3, 203 + N, torch.float32, loud=False) * s).contiguous() for s in (kscale, 1.0))
+    pr.append(3, 203 + N, torch.float32, count=[203 + N, 17 + N, N], k=k, v=v)
+    pr.m.len[:] = [203, 17, 0]
+    pr.c.seq_len.copy_(i32(pr.m.len))
+    q = (torch.randn((3, N, 4, 64), device=DEV) * 2.0 ** 124).to(torch.bfloat16)
+    q[..., 3] = torch.finfo(torch.bfloat16).max
+    q[:, 1, 2] = 2.0 ** 127
+    q[:, 0, 1] = -torch.finfo(torch.bfloat16).max
+    assert bool(torch.isfinite(q).all())
+    if kscale < 2.0 ** -100:
+        check_attention(pr, q)
+    else:
+        assert check_huge(pr, q) > 6 * N
