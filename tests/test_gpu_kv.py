@@ -999,3 +999,94 @@ def test_attention_of_the_largest_finite_q(N, kscale):
         check_attention(pr, q)
     else:
         assert check_huge(pr, q) > 6 * N
+
+
+# ------------------------------------------------------------------------------------- damaged tables and special rows, tiles
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", ["trees", "chain"])
+def test_page_ids_outside_the_pool_are_not_followed_by_tiles(kind, d):
+    """As above for many query rows; the damaged entry also behind the 32 key tiles that are located at once."""
+    N, B, H = 60, 12, 12
+    rng = np.random.default_rng(d)
+    pr = Pair(pages=B * 50, heads=H, d=d, page=128, seqs=B, width=50, seed=103)
+    lens = [6000, 5800] + [6100] * (B - 3) + [20]
+    pr.resize([n + N for n in lens])
+    k = torch.randn((B, 6160, H, d), device=DEV).to(torch.bfloat16)
+    kv.append(pr.c, 0, k, k.flip(1).contiguous(), count=i32([n + N for n in lens]))
+    pr.c.seq_len.copy_(i32(lens))
+    q = torch.randn((B, N, 4 * H, d), device=DEV).to(torch.bfloat16)
+    parent = i32(trees(rng, B, N)) if kind == "trees" else None
+    ws = kv.attention_workspace(q, pr.c)
+    good = kv.tree_attention(q, pr.c, 0, parent, workspace=ws)
+    assert torch.isfinite(good).all()
+    table = pr.c.block_table.clone()
+    for b, entry in ((1, 0), (1, 31), (1, 40), (1, 45), (11, 0)):
+        for bad in (-1, B * 50, 1 << 30, -(1 << 31)):
+            pr.c.block_table[b, entry] = bad
+            st = torch.full((B,), -7, dtype=torch.int32, device=DEV)
+            out = kv.tree_attention(q, pr.c, 0, parent, status=st, workspace=ws)
+            assert out[b].isnan().all() and (host(st) == 0).all()
+            out[b] = good[b]
+            assert torch.equal(out, good)
+            pr.c.block_table.copy_(table)
+
+
+@pytest.mark.parametrize("kind", ["trees", "chain"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_special_rows_of_q_in_tiles(kind, dtype):
+    """Rows of nothing, of one element, with a NaN or an infinity: NaN where the formula has it, for their row alone."""
+    N = 60
+    pr = Pair(pages=120, heads=2, d=128, page=16, seqs=3, width=40, seed=104)
+    pr.grow([390, 17, 0])
+    pr.resize([N] * 3)
+    pr.append(3, N)
+    q = torch.randn((3, N, 8, 128), device=DEV)
+    q[0, 0] = 0
+    q[0, 1] *= 1e-30
+    q[1, 2] *= 3e-3
+    q[2, 3, :, ::2] *= 1e-4
+    q[0, 4] *= 40
+    q[1, 5:9, 1] *= 300
+    parent = trees(np.random.default_rng(1), 3, N) if kind == "trees" else None
+    q = q.to(dtype)
+    good = check_attention(pr, q, parent=parent).clone()
+    special = [(0, 7, 0, float("nan")), (1, 20, 7, float("inf")), (2, 59, 3, -float("inf")), (0, 33, 5, float("nan")), (2, 0, 1, float("inf"))]
+    for b, i, h, x in special:
+        q[b, i, h, 5] = x
+    out = kv.tree_attention(q, pr.c, 0, None if parent is None else i32(parent))
+    for b, i, h, _ in special:
+        assert out[b, i, h].isnan().all(), (b, i, h)
+        out[b, i, h] = good[b, i, h]
+    assert torch.equal(out, good)
+
+
+def test_captured_calls_of_many_rows_share_a_workspace():
+    """Two graphs with one workspace and one status tensor, replayed in turn on new lengths and rows of q."""
+    N, B = 40, 3
+    pr = Pair(pages=200, heads=2, d=64, page=32, seqs=B, width=40, seed=105)
+    pr.grow([700, 20, 130])
+    pr.resize([2 * N] * B)
+    pr.append(B, 2 * N)
+    qs = [torch.randn((B, n, 8, 64), device=DEV).to(torch.bfloat16) for n in (N, N // 2)]
+    parents = [i32(trees(np.random.default_rng(1), B, N)), None]
+    outs = [torch.full(q.shape, 7.25, dtype=q.dtype, device=DEV) for q in qs]
+    ws, st, count = kv.attention_workspace(qs[0], pr.c), torch.full((B,), -7, dtype=torch.int32, device=DEV), i32([N] * B)
+    graphs = []
+    for q, p, o in zip(qs, parents, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            kv.tree_attention(q, pr.c, 0, p, count=count, out=o, status=st, workspace=ws)
+    for step in range(3):
+        count.copy_(i32([N, 7 * step, N - step]))
+        for q in qs:
+            q.normal_()
+        lens = [700 + step, 20, 130 + 2 * step]          # rows behind the committed ones are there
+        pr.m.len[:] = lens
+        pr.c.seq_len.copy_(i32(lens))
+        for g, q, p, o in zip(graphs, qs, parents, outs):
+            o.fill_(7.25)
+            g.replay()
+            torch.cuda.synchronize()
+            want = check_attention(pr, q, parent=None if p is None else host(p), count=host(count))
+            assert torch.equal(o, want) and (host(st) == 0).all()
