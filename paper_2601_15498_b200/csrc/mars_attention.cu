@@ -51,10 +51,6 @@ constexpr int rows_grid(int rows, int d) { return kAttnSms * rows_occ(rows, d); 
 constexpr int kUnit = RowsShape<8>::unit_keys(8);
 constexpr float kNone = -3.40282347e38f;     // reference maximum before a row's first key
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }

@@ -70,6 +70,11 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // Nodes of sequence b that take part, and whether its pages hold them; len < 0 counts as no room.
 __device__ __forceinline__ int attn_nodes(const AttnParams &p, int b, int *len, int *status)
 {

@@ -126,10 +126,6 @@ __device__ __forceinline__ uint32_t elect_one()
     return r;
 }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void cp_async16_to(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
@@ -232,9 +228,9 @@ __device__ __forceinline__ void tile_unpack_role(const AttnParams &p, AttnRange 
             if (from > kNoPage) {
                 const unsigned char *src = (const unsigned char *)from + lane * 16;
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) cp_async16_to(slot_u32 + i * 512, src + i * 512);
+                for (int i = 0; i < D / 64; ++i) cp_async16(slot_u32 + i * 512, src + i * 512);
                 // the scales follow K's codes by 16d bytes, V's by 9d
-                if (lane < D / 16) cp_async16_to(slot_u32 + 8 * D, src + 16 * D - v * 7 * D);
+                if (lane < D / 16) cp_async16(slot_u32 + 8 * D, src + 16 * D - v * 7 * D);
             }
         };
         issue(0);

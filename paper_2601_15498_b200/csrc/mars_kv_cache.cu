@@ -120,8 +120,9 @@ __device__ __forceinline__ uint32_t e2m1x8_from(const float *t)
 // place.  With 8-bit significands and a power of two as g many quotients lie exactly on the border of
 // two codes, where a reciprocal's last bit would decide.  Fast form: x * r and one residual correction
 // (Markstein 1990: with r the rounded reciprocal, fma(fma(-q, sg, x), r, q) is the rounded quotient
-// while nothing over- or underflows), two values at a time; |x / sg| <= 6.4 there, since the scale did not
-// saturate.  The sign is turned since fma(0, r, -0) is +0 and a zero would lose its sign bit.
+// while nothing over- or underflows), two values at a time.  The scale did not saturate, so |x / sg| <= 6.4 for
+// a normal s; for a subnormal one, off by up to a third, it reaches 9, and the conversion to codes saturates.
+// The sign is turned since fma(0, r, -0) is +0 and a zero would lose its sign bit.
 __device__ __forceinline__ void quotients16(float (&x)[16], float sg, bool plain)
 {
     if (plain) {

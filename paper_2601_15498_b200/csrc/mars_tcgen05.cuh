@@ -38,7 +38,9 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
-// Bounded wait.  Returns false if the budget ran out or another role already gave up.
+// Bounded wait.  Returns false if the budget ran out or another role already gave up.  The flag and the clock are
+// looked at after every try (a try itself suspends for a while).  The LM head's step of 64 trees of 60 nodes
+// (V 151936, d 4096) takes 2.97 to 3.14 ms so, and 3.09 to 3.12 with 64 tries between two looks.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag,
                                           unsigned *status, long long budget = kWaitCycles)
 {
