@@ -22,11 +22,14 @@
 //     are one vector, all of one scale.
 // The running maximum needs no reduction per block: a vote finds whether any score exceeds the row's
 // reference by 2^8; only then (rarely after the first blocks) is it recomputed and O rescaled.
-// Measured: 64 tokens over contexts of 300 to 32768 (8 KV heads of 4, 451 MB of cache) 104 us, 67 % of the copy
-// rate with launch and ragged ends; over 500000 tokens 455 us for 2.3 GB, 78 % of it.  There issue bounds it:
-// 54 % of the slots are taken and a warp's next instruction waits for its last one's result, with 16 warps per
-// SM.  Tiles of 32 rows, 255 registers and 8 warps per SM, take 200 us for 64 chains of 8 nodes (401 MB); of
-// 16 rows 133 us.  The tile kernel takes 244 us for the same chains, with rows or without, so 32 is the border.
+// Measured (calls one after the other on the same inputs; on inputs that change from call to call the tokens take
+// 114): 64 tokens over contexts of 300 to 32768 (8 KV heads of 4, 451 MB of cache) 106 us, 66 % of the copy rate
+// with launch and ragged ends; four over 500000 tokens 452 us for 2.3 GB, 79 % of it.  There latency bounds it: 55 %
+// of the issue slots are taken, and a warp's next instruction waits for its last one's result, with 16 warps per
+// SM at 126 registers.  Tiles of 32 rows, 255 registers and 8 warps per SM, take 197 us for 64 chains of 8 nodes
+// (401 MB); of 16 rows 131 us.  The tile kernel takes 235 us for either, so 32 is the border.
+// Spills: 90 bytes stored and 154 loaded in tiles of 16 rows of d 128 (168 registers for 3 blocks per SM), 18 / 30 in tiles
+// of 32 of d 128, none elsewhere.
 #include "mars_attention.cuh"
 #include "mars_hooks.cuh"
 
@@ -40,9 +43,9 @@ constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = 32 * kRowsWarps;
 constexpr int kRowsStages = 4;        // 16-key blocks in flight per warp
 constexpr int kRowsMax = 32;          // largest tile
-// Blocks per SM: as many as registers allow.  Measured, us with this many / one more: 64 tokens 109 / 151, 64 chains
-// of 4 nodes (16 rows) 132 / 225, of 6 nodes (24 rows) 157 / 176; d 64: 72 / 74, 82 / 84, 105 / 109, and of 8
-// nodes (32 rows) 130 / 132.  Tiles of 24 rows are there since chains of 6 nodes take 157 in them, 196 in tiles of 32.
+// Blocks per SM: as many as registers allow.  Measured, us with this many / one more: 64 tokens 106 / 147, 64 chains
+// of 4 nodes (16 rows) 131 / 213, of 6 nodes (24 rows) 158 / 176, of 8 nodes (32 rows) 197 / 611; d 64: 73 / 74,
+// 81 / 83, 103 / 110, 127 / 131.  Tiles of 24 rows are there since chains of 6 nodes take 158 in them, 193 in tiles of 32.
 constexpr int rows_occ(int rows, int d)
 {
     return d == 128 ? (rows == 8 ? 4 : rows == 16 ? 3 : 2) : (rows == 8 ? 4 : rows == 16 ? 3 : rows == 24 ? 3 : 2);
@@ -514,8 +517,12 @@ static bool attn_sizes_ok(int B, int N, int q_heads, int kv_heads, int d)
 }
 
 // The kernel for tiles of query rows takes over where a KV head has more of them than the largest
-// tile of the other holds.  Measured, us with rows / tiles: 64 chains of 8 nodes (32 rows) 200 / 235, of 4 nodes (16
-// rows) 133 / 234; one such chain 43 / 39, 4 chains 45 / 47, 16 chains 80 / 92.
+// tile of the other holds.  Measured, us with rows / tiles: 64 chains of 8 nodes (32 rows) 197 / 236, of 4 nodes (16
+// rows) 131 / 234; one chain of 8 41 / 39, 4 chains 45 / 47, 16 chains 78 / 91.
+// Trees of more nodes than the tile kernel's mask store holds stay with the rows, which unpack K and V again for
+// every 32 of them.  That costs (4 heads to a KV head, 8 KV heads of 128, 4000 tokens; 128 / 129 / 256 / 1024 nodes): one
+// tree 43 / 68 / 102 / 437 us, 16 trees 203 / 639 / 1227 / 6378, where chains of as many nodes, in tiles, take 43 / 43 /
+// 53 / 127 and 199 / 240 / 360 / 1444.
 static bool attn_use_tiles(int N, int group, bool tree) { return (int64_t)N * group > kRowsMax && !(tree && N > kTileMaxTree); }
 static int attn_rows(int N, int group)
 {

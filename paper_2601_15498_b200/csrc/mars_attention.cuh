@@ -23,8 +23,8 @@ namespace mars {
 // Tile shapes: query rows per tile, keys per unit of the split, the least number of units per block (a
 // block more costs a partial result and its merge), and what an item costs besides its keys
 // (decoding, Q, masks, the pipeline's fill and drain, the result) in units.  Counting that in evens out
-// the blocks where items are short.  Measured, us without / as here / with twice that: 64 tokens 115 / 104 /
-// 109, 64 chains 232 / 201 / 212; four prompts 200 / 132 / 145 (TileShape).
+// the blocks where items are short.  Measured, us without / as here / with twice that: 64 tokens 122 / 106 /
+// 110, 64 chains 236 / 197 / 206; four prompts 188 / 131 / 143, 64 trees 485 / 419 / 413 (TileShape).
 template <int kRows>
 struct RowsShape {
     static __device__ constexpr int rows(int) { return kRows; }

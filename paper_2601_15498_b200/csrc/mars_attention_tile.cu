@@ -23,13 +23,13 @@
 // memory at its full rate, beside the unpacking warps' stores, so that the MMA warp takes 1400 to 1700 cycles
 // for the two products of a step (1026 alone); softmax of a step takes about 3000 of an accumulator's 4500, and
 // two accumulators overlap only in part.  64 trees of 60 nodes over contexts of 2000 to 12000 tokens (8 KV heads of
-// 4, d 128): 418 us; one tree over 500000 tokens 606 us (2.7 us per 128 keys and 256 rows); four prompts of 2048
-// (4 KV heads of 4, d 64) 131 us.  Measured and not kept, us for those trees / prompts: S and P in halves of 64
-// keys, four in flight (503 / 126: with 64 columns S reads Q twice as often); 16 softmax warps with 64
-// scores a thread and 8 unpacking ones (526 / 130); P by the old reference in one pass over S, the
-// maximum looked at afterwards (412 / 135); the MMA warp waiting for V and the next K before P, with fewer
-// commits (436 / 132); a warp of its own for each accumulator's products (519 / 136); copies three tiles
-// ahead for tiles of up to 128 rows, longer suspended waits (both as without).
+// 4, d 128): 420 us; one tree over 500000 tokens 580 us; four prompts of 2048 (4 KV heads of 4, d 64) 130 us.  Spills at
+// d 128 (d 64): 284 (104) bytes stored and 432 (244) loaded, under the split of 136, 48 and 40 registers to the roles.
+// Measured and not kept, us for those trees / prompts: S and P in halves of 64 keys, four in flight (503 / 126:
+// with 64 columns S reads Q twice as often); 16 softmax warps with 64 scores a thread and 8 unpacking ones (526 /
+// 130); P by the old reference in one pass over S, the maximum looked at afterwards (412 / 135); the MMA warp
+// waiting for V and the next K before P, with fewer commits (436 / 132); a warp of its own for each accumulator's
+// products (519 / 136); copies three tiles ahead for tiles of up to 128 rows, longer suspended waits (both as without).
 //
 // Each role walks the block's segments by itself; unpacking and MMA run ahead into the next one.
 //
@@ -749,8 +749,8 @@ static mars_status_t tile_launch(const AttnParams &p, cudaStream_t st)
 
 // Tiles of 256 rows share what is unpacked; of 128 rows there are twice as many, which a batch with
 // fewer items than half of the SMs is better off with (lengths are not known here).  Measured, us with
-// 128 / 256 rows, 60-node trees over 4000 tokens (8 KV heads): 1 tree 35 / 48, 4 trees 48 / 52, 10 trees
-// 83 / 81, 16 trees 119 / 108, 48 trees 303 / 260; one prompt of 512 (4 KV heads) 19 / 24, of 2048 87 / 80.
+// 128 / 256 rows, 60-node trees over 4000 tokens (8 KV heads): 1 tree 35 / 47, 4 trees 45 / 53, 10 trees
+// 80 / 78, 16 trees 116 / 107, 48 trees 290 / 267; one prompt of 512 (4 KV heads) 20 / 24, of 2048 55 / 50.
 mars_status_t attn_tile_launch(const AttnParams &q, int d, int dt, cudaStream_t st)
 {
     AttnParams p = q;

@@ -5,7 +5,8 @@
 // loads; resize and fork's bookkeeping run in one thread block cluster / block, since the page
 // tables are a few hundred kilobytes at most and a grid-wide step would cost more than it moves.
 // Measured: append and gather of 49300 ragged rows of 8 heads of 128 (259 MB moved each) 65 and
-// 49 us: 4.0 and 5.3 TB/s; issue bounds both (67 and 73 % of the slots, conversions and quotients).  The rows of
+// 52 us: 4.0 and 5.0 TB/s; 67 and 75 % of the issue slots are taken (conversions and quotients).  In fp32 (461 MB)
+// 70 and 80 us: 6.6 and 5.8 TB/s.  The rows of
 // 64 forks' last pages 21 us for 150 MB (7.1 TB/s, partly in L2), their tables 12 us; the page decisions of 2048 sequences
 // 24 us, of 64 11 us (latency of dependent steps: 5 % of the issue slots, nothing of DRAM); the paths out of 64
 // trees in four layers 6 us.
@@ -219,7 +220,7 @@ struct GatherParams {
 // Another g ends within the last 6 of its 24 bits, and so does the product within the last 6 of its 24 to 30: too
 // low for it to be a border itself, and off a border the bit may be set whether or not something was lost.  (Both
 // hold while fp32 does not underflow; it does for bf16 results below 2^-126 only.)  16 prompts in and out 117 us, with
-// products to nearest 116, from remainders 135.
+// products to nearest 115, from remainders 135.
 __device__ __forceinline__ uint32_t odd_bit(float g) { return (__float_as_uint(g) & 63u) != 0u; }
 __device__ __forceinline__ float product_to_odd(float f, float g, uint32_t last)
 {
