@@ -217,11 +217,11 @@ struct GatherParams {
 // rounds the exact product: cut off to 24 bits, the last bit set if anything was lost (rounding to odd, Boldo and
 // Melquiond 2008).  Rounded to nearest first, a product just off a border of two 16-bit values can land on it.
 // `last` (odd_bit) is that bit for all f of a head, without a remainder.  A g of at most 18 bits has exact products: 0.
-// Another g ends within the last 6 of its 24 bits, and so does the product within the last 6 of its 24 to 30: too
-// low for it to be a border itself, and off a border the bit may be set whether or not something was lost.  (Both
-// hold while fp32 does not underflow; it does for bf16 results below 2^-126 only.)  16 prompts in and out 117 us, with
-// products to nearest 115, from remainders 135.
-__device__ __forceinline__ uint32_t odd_bit(float g) { return (__float_as_uint(g) & 63u) != 0u; }
+// Another g has 19 bits or more and ends within 6 of its last place, as the product does: too low for it to be a
+// border itself, and off a border the bit may be set whether or not something was lost.  (Subnormal g below 2^18
+// units have at most 18 bits wherever they end.  All of it holds while the product does not underflow in fp32; it does
+// for bf16 results below 2^-126 only.)  16 prompts in and out 117 us, with products to nearest 115, from remainders 135.
+__device__ __forceinline__ uint32_t odd_bit(float g) { return (__float_as_uint(g) & 63u) != 0u && g >= 0x1p-131f; }
 __device__ __forceinline__ float product_to_odd(float f, float g, uint32_t last)
 {
     return __uint_as_float(__float_as_uint(__fmul_rz(f, g)) | last);

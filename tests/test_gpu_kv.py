@@ -900,6 +900,11 @@ def test_gather_rounds_once(dtype):
                         g[200:240] * np.float32(2.0 ** 118), np.exp2(rng.integers(-149, 128, 40)).astype(np.float32),
                         np.float32([1.401298464324817e-45, 1.1754942106924411e-38, 1.1754943508222875e-38, 3.4028234663852886e38])])
     g = np.maximum(g, np.float32(1.401298464324817e-45))
+    check_gather(g, dtype)
+
+
+def check_gather(g, dtype):
+    """Every code under every scale byte and the head scales g, against the nearest value of the type."""
     H = len(g)
     c = kv.KVCache.empty(1, 2, H, 64, 16, 1, 2, DEV, scales=np.stack([g, g[::-1]])[None])
     kv.resize(c, i32([32]))
@@ -920,6 +925,13 @@ def test_gather_rounds_once(dtype):
         # bf16 below its normal numbers goes through fp32: off by half a step, 2^-134, and half an fp32 step more
         low = (np.abs(true) < 2.0 ** -126) & (dtype == torch.bfloat16)
         assert np.array_equal(got[~low], want[~low]) and (np.abs(got - true)[low] <= 2.0 ** -134 + 2.0 ** -149).all()
+
+
+def test_gather_rounds_once_under_subnormal_scales():
+    """Products of short subnormal scales that lie exactly between two bf16 values go to the even one."""
+    rng = np.random.default_rng(106)
+    n = np.concatenate([(1 << 13) + 32 + 64 * np.arange(100), 32 * rng.integers(1, 1 << 18, 100), rng.integers(1, 1 << 23, 100)])
+    check_gather((n * 2.0 ** -149).astype(np.float32), torch.bfloat16)
 
 
 # ------------------------------------------------------------------------------------- extreme rows of q
