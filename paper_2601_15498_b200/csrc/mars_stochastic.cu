@@ -26,6 +26,7 @@
 // A template flag of the tail covers chains whose drafts were sampled from a drafter's
 // distribution Q (Eq. 1 in its general form): the test carries Q(x) and the residual is
 // max(0, P - Q), read from the target's and the drafter's row of the rejected position.
+#include "mars_fp32.cuh"
 #include "mars_top2_stream.cuh"
 
 #include <cooperative_groups.h>
@@ -42,13 +43,6 @@ struct __align__(16) SRec {
     float sum;   // SUM of those weights over the slice
     int pad0, pad1;
 };
-
-__device__ __forceinline__ float ex2f(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // (ref, sum) of the union of two disjoint element sets.
 __device__ __forceinline__ void soft_merge(float &ref, float &sum, float ref_b, float sum_b)
@@ -69,24 +63,6 @@ __device__ __forceinline__ void soft_add_scalar(float &ref, float &sum, float x,
         const float t = fmaf(x, c, -ref);
         sum += (t == t) ? ex2f(t) : INFINITY;
     }
-}
-
-// ---- packed fp32 pairs (one instruction for two lanes of work) ----------------------------
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("{ .reg .b64 ra, rb, rc, rd; mov.b64 ra, {%2,%3}; mov.b64 rb, {%4,%5}; mov.b64 rc, {%6,%7};\n"
-        "fma.rn.f32x2 rd, ra, rb, rc; mov.b64 {%0,%1}, rd; }"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 d;
-    asm("{ .reg .b64 ra, rb, rd; mov.b64 ra, {%2,%3}; mov.b64 rb, {%4,%5};\n"
-        "add.rn.f32x2 rd, ra, rb; mov.b64 {%0,%1}, rd; }"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
 }
 
 // Rare path of soft_batch: the batch's sum of weights came out NaN, i.e. the batch holds a NaN
