@@ -129,6 +129,10 @@ def lib() -> ctypes.CDLL:
             L.mars_kv_resize.restype = i32
             L.mars_kv_gather.argtypes = [vp, i32, i32, i32, vp, vp, i32, vp, vp, i32, vp]
             L.mars_kv_gather.restype = i32
+            L.mars_token_logprobs.argtypes = [vp, i64, i32, i64, vp, i64, i32, f32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+            L.mars_token_logprobs.restype = i32
+            L.mars_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i32, f32, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+            L.mars_token_logprobs_backward.restype = i32
             _lib = L
     return _lib
 
