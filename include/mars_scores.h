@@ -1,6 +1,6 @@
 /*
- * mars_scores.h -- the target model's output side of libmars: log probabilities of tokens with entropy and
- * best alternatives, and their gradient.
+ * mars_scores.h -- the target model's output side of libmars: the output projection in 8-bit integers, log
+ * probabilities of tokens with entropy and best alternatives, and their gradient.
  *
  * Verification (mars.h) decides on the target's logits rows; these calls give what a program reports and
  * trains with beside the decision: softmax probabilities P (Eq. 3 of the paper, at a temperature T) of the
@@ -22,6 +22,45 @@ extern "C" {
 
 #define MARS_SCORES_MAX_TOKENS 1024 /* cap on J, tokens per row        */
 #define MARS_SCORES_MAX_TOP 32      /* cap on k, alternatives per row  */
+
+/*
+ * Rows as signed 8-bit codes with one scale each: with a = max |x| of a row,
+ *   scale = a / 127,  code = rint(x * (127 * (1 / a))),
+ * every operation one fp32 IEEE operation, rint to nearest even.  A row whose a is below 2^-119 gets scale 0
+ * and zero codes; one that holds a NaN or an infinity gets scale NaN and zero codes, so that whatever is
+ * computed from it is NaN.
+ *   x        [rows, ldx] of `dt` (MARS_BF16, MARS_FP32, or MARS_FP16 of mars_kv.h), K columns of each row are
+ *            read; rows that start on 16-byte boundaries are read in 16-byte steps.
+ *   q        int8 [rows, ldq], 16-byte aligned, ldq a multiple of 16; columns 0 .. K-1 are written.
+ *   scale    float [rows].      K <= 2^17.
+ */
+mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t rows, int K, void *q, int64_t ldq,
+                                 float *scale, void *cuda_stream);
+
+/*
+ * Output projection (Eq. 2 of the paper: z = W_o h + b_o) in 8-bit integers:
+ *   out[m, v] = (sum_k xq[m, k] wq[v, k]) * x_scale[m] * w_scale[v] + bias[v].
+ * The sum is exact; the rest is fp32, in that order, the second product and the bias as one fused operation,
+ * and the result is rounded to `dt`.  Products run on the tensor cores (tcgen05, kind::i8).
+ *   xq       int8 [M, ldx], the tokens' codes (mars_quantize_rows); x_scale float [M].
+ *   wq       int8 [V, ldw], the weights' codes, quantised once; w_scale float [V].  Codes are -127 .. 127.
+ *   bias     float [V] or NULL.
+ *            Both matrices start on 16-byte boundaries, ldx and ldw are multiples of 16; K <= 2^17 is any.
+ *   out      `dt` (MARS_BF16 or MARS_FP32) [M, ldo], any alignment; columns 0 .. V-1 are written.
+ *   flags    MARS_COUNTERS_ZERO: the caller vouches that `workspace` was zeroed once and used by completed
+ *            calls of this function only since; otherwise the call clears its counters.
+ *   workspace  mars_project_int8_workspace_bytes() bytes (0 for unsupported sizes), 256-byte aligned; two
+ *            calls that may overlap on the GPU need separate workspaces.
+ *   The first call on a device sets function attributes: make it outside any stream capture.
+ *   If a bounded device-side wait gives up (a fault in the pipeline, not a property of the data), logits
+ *   that were not computed are NaN and the first uint32 of the workspace is MARS_SEQ_TIMEOUT; it is 0
+ *   otherwise.  A workspace after such a call has to be zeroed before MARS_COUNTERS_ZERO is used again.
+ */
+size_t mars_project_int8_workspace_bytes(int64_t M, int V, int K);
+mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scale, const void *wq, int64_t ldw,
+                                const float *w_scale, const float *bias, int64_t M, int V, int K, void *out,
+                                int64_t ldo, mars_dtype_t dt, uint32_t flags, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream);
 
 /*
  * Log probabilities of tokens.  For every row z of V logits, with p = softmax(z / T):

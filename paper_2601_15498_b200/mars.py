@@ -133,6 +133,12 @@ def lib() -> ctypes.CDLL:
             L.mars_token_logprobs.restype = i32
             L.mars_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i32, f32, vp, i32, vp, vp, vp, vp, vp, i64, vp]
             L.mars_token_logprobs_backward.restype = i32
+            L.mars_quantize_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp]
+            L.mars_quantize_rows.restype = i32
+            L.mars_project_int8_workspace_bytes.argtypes = [i64, i32, i32]
+            L.mars_project_int8_workspace_bytes.restype = sz
+            L.mars_project_int8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i32, i32, vp, i64, i32, u32, vp, sz, vp]
+            L.mars_project_int8.restype = i32
             _lib = L
     return _lib
 

@@ -1,5 +1,11 @@
 """ctypes binding of the output side of libmars (mars_scores.h; argument marshalling only).
 
+The output projection with weights in 8 bits, quantised once::
+
+    wq, ws = scores.quantize_rows(w_vocab)
+    work = scores.project_workspace(tokens, V, K, device)
+    logits = scores.project_int8(*scores.quantize_rows(hidden), wq, ws, workspace=work)      # [tokens, V]
+
 After a verification, the log probabilities, entropies and alternatives of what it emitted::
 
     out = mars.verify_tree(logits, tok, parent, theta=0.9)
@@ -18,9 +24,11 @@ from __future__ import annotations
 import torch
 
 from . import mars
-from .mars import MarsError, _check, _dev_f32, _dev_i32, _logits_args, lib
+from .mars import MarsError, _check, _dev_f32, _dev_i32, _dtype_code, _logits_args, lib
 
 MAX_TOKENS, MAX_TOP = 1024, 32
+
+_ROW_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: 2}
 
 
 def _call(fn, device, *args) -> None:
@@ -52,6 +60,75 @@ def _into(out, name: str, shape, dtype, device):
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise MarsError(f"out[{name!r}] must be a contiguous {dtype} tensor {list(shape)} on {device}")
     return t
+
+
+def quantize_rows(x: torch.Tensor, out=None):
+    """mars_quantize_rows on the current stream: x [rows, K] (bfloat16, float16 or float32, unit inner stride) as
+    (codes int8 [rows, K] in rows of a multiple of 16 bytes, scales float32 [rows]); `out` = such a pair."""
+    if not x.is_cuda or x.dim() != 2 or x.stride(1) != 1 or x.dtype not in _ROW_DTYPES:
+        raise MarsError("x must be [rows, K] of bfloat16, float16 or float32 with unit inner stride in device memory")
+    R, K = x.shape
+    if out is None:
+        out = (torch.empty((R, -(-K // 16) * 16), dtype=torch.int8, device=x.device)[:, :K],
+               torch.empty((R,), dtype=torch.float32, device=x.device))
+    q, scale = out
+    _codes(q, scale, "out")
+    if q.shape != x.shape or q.device != x.device:
+        raise MarsError("out must have the shape and device of x")
+    _call(lib().mars_quantize_rows, x.device, x.data_ptr(), x.stride(0), _ROW_DTYPES[x.dtype], R, K, q.data_ptr(), q.stride(0),
+          scale.data_ptr())
+    return q, scale
+
+
+def _codes(q, scale, name: str) -> None:
+    if q.dim() != 2 or q.dtype != torch.int8 or q.stride(1) != 1 or not q.is_cuda:
+        raise MarsError(f"{name}: codes must be int8 [rows, K] with unit inner stride in device memory")
+    if scale.dtype != torch.float32 or tuple(scale.shape) != q.shape[:1] or not scale.is_contiguous() or scale.device != q.device:
+        raise MarsError(f"{name}: scales must be contiguous float32, one a row, beside the codes")
+
+
+def project_workspace(tokens: int, V: int, K: int, device) -> torch.Tensor:
+    """A zeroed workspace for project_int8 calls of these sizes; it serves any number of calls that do not
+    overlap."""
+    need = int(lib().mars_project_int8_workspace_bytes(tokens, V, K))
+    if need == 0:
+        raise MarsError("unsupported sizes")
+    return torch.zeros((need,), dtype=torch.uint8, device=device)
+
+
+def project_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias=None,
+                 dtype=torch.bfloat16, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """mars_project_int8 on the current stream: logits [tokens, V] of codes xq [tokens, K] and wq [V, K] with
+    their scales (quantize_rows of the hidden states, and once of the weights).  `out` [tokens, >= V] (its dtype
+    is used).  `workspace` comes from project_workspace and is used by these calls only; without one, a call
+    allocates and clears its own."""
+    dev = xq.device
+    _codes(xq, x_scale, "xq")
+    _codes(wq, w_scale, "wq")
+    (M, K), V = xq.shape, wq.shape[0]
+    if wq.shape[1] != K or wq.device != dev:
+        raise MarsError("xq and wq must have the same number of columns and device")
+    if bias is not None:
+        bias = _dev_f32(bias, dev)
+        if tuple(bias.shape) != (V,):
+            raise MarsError(f"bias must be [{V}]")
+    if out is None:
+        out = torch.empty((M, V), dtype=dtype, device=dev)
+    if out.dim() != 2 or out.shape[0] != M or out.shape[1] < V or out.stride(1) != 1 or out.device != dev:
+        raise MarsError(f"out must be [{M}, >= {V}] with unit inner stride beside the codes")
+    flags = mars.COUNTERS_ZERO
+    if workspace is None:
+        flags = 0
+        need = int(lib().mars_project_int8_workspace_bytes(M, V, K))
+        if need == 0:
+            raise MarsError("unsupported sizes")
+        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise MarsError("workspace must be a contiguous tensor beside the codes")
+    _call(lib().mars_project_int8, dev, xq.data_ptr(), xq.stride(0), x_scale.data_ptr(), wq.data_ptr(), wq.stride(0),
+          w_scale.data_ptr(), _ptr(bias), M, V, K, out.data_ptr(), out.stride(0), _dtype_code(out), flags,
+          workspace.data_ptr(), workspace.nbytes)
+    return out
 
 
 def token_logprobs(logits: torch.Tensor, tok=None, temperature: float = 1.0, k: int = 0, rows=None,

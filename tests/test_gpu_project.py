@@ -1,0 +1,196 @@
+"""The 8-bit output projection on the device.  Codes, sums and every rounding of the call are defined, so all
+comparisons are bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+import hookctl as hooks
+import scores_checks as sc
+from paper_2601_15498_b200 import mars, scores
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def codes(R, K, seed, shift=0, full=False):
+    """[R, K] codes in rows of a multiple of 16 bytes between guard values, scales of both signs of exponent."""
+    wide = torch.full((R + 2, -(-K // 16) * 16 + 16 * shift), 99, dtype=torch.int8, device=DEV)
+    q = wide[1:R + 1, :K]
+    q.copy_(torch.randint(-127, 128, (R, K), generator=gen(seed), device=DEV) if not full else
+            torch.full((R, K), 127, device=DEV) * (1 - 2 * (torch.arange(R, device=DEV) % 2))[:, None])
+    return q, torch.exp2(torch.randn((R,), generator=gen(seed + 1), device=DEV) * 3) * 1e-3
+
+
+def plain(q, s, w, u, bias, dtype):
+    y = (q.double() @ w.double().T).float() * s[:, None]
+    # a product of two fp32 numbers is exact in 64 bits: with the bias, one rounding in all
+    y = (y.double() * u[None] + (0.0 if bias is None else bias.double()[None])).float()
+    return y.to(dtype)
+
+
+@pytest.mark.parametrize("M,V,K", [(1, 1, 1), (1, 300, 64), (2, 256, 128), (3, 257, 129), (31, 1000, 1000), (33, 640, 4096),
+                                   (100, 77, 31), (255, 513, 200), (256, 4096, 512), (257, 700, 384), (333, 3001, 5000),
+                                   (513, 2049, 130), (700, 256, 16), (1, 151936, 256), (64, 20000, 2048), (1025, 130, 8192)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_product(M, V, K, dtype):
+    (q, s), (w, u) = codes(M, K, M + K, shift=1), codes(V, K, V + 7, shift=M % 2)
+    bias = torch.randn((V,), generator=gen(3), device=DEV) if M % 2 else None
+    wide = torch.full((M + 1, V + 5), -777.0, dtype=dtype, device=DEV)
+    out = wide[:M, 2:2 + V] if V % 2 else wide[:M, :V]
+    got = scores.project_int8(q, s, w, u, bias=bias, out=out)
+    assert got is out and torch.equal(out, plain(q, s, w, u, bias, dtype))
+    at = 2 if V % 2 else 0
+    assert (wide[M] == -777).all() and (wide[:, :at] == -777).all() and (wide[:, at + V:] == -777).all()
+
+
+def test_largest_sums_are_exact():
+    """127 * 127 * 2^17 stays below 2^31, and a float that is halfway goes to the even one."""
+    K = 1 << 17
+    (q, s), (w, u) = codes(3, K, 1, full=True), codes(300, K, 2, full=True)
+    q[2] = torch.randint(-127, 128, (K,), generator=gen(5), device=DEV).to(torch.int8)
+    got = scores.project_int8(q, s, w, u, dtype=FP32)
+    assert torch.equal(got, plain(q, s, w, u, None, FP32))
+    assert float(got[0, 0] / (s[0] * u[0])) == pytest.approx(127 * 127 * K, rel=2 ** -21)
+
+
+def test_workspace_serves_calls_of_one_size_after_another():
+    """A workspace zeroed once: split tiles (few weight rows, long K) leave it as they found it."""
+    M, V, K = 40, 900, 6000
+    (w, u) = codes(V, K, 3)
+    work = scores.project_workspace(M, V, K, DEV)
+    for i in range(5):
+        q, s = codes(M, K, 10 + i)
+        assert torch.equal(scores.project_int8(q, s, w, u, dtype=FP32, workspace=work), plain(q, s, w, u, None, FP32))
+        assert int(work[:4].view(torch.int32)) == 0
+    small = codes(7, 640, 4)
+    (w2, u2) = codes(5000, 640, 5)
+    assert torch.equal(scores.project_int8(*small, w2, u2, workspace=work), plain(*small, w2, u2, None, BF16))
+
+
+def test_streams_and_graph():
+    M, V, K = 70, 5003, 1500
+    (q, s), (w, u) = codes(M, K, 1), codes(V, K, 2)
+    want = plain(q, s, w, u, None, BF16)
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    works = [scores.project_workspace(M, V, K, DEV) for _ in side]
+    torch.cuda.synchronize()
+    many = []
+    for i in range(8):
+        with torch.cuda.stream(side[i % 2]):
+            many.append(scores.project_int8(q, s, w, u, workspace=works[i % 2]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in many)
+    x = torch.randn((M, K), generator=gen(3), device=DEV).to(BF16)
+    out = torch.empty((M, V), dtype=BF16, device=DEV)
+    pair = scores.quantize_rows(x)
+    graphs = []
+    for _ in range(2):                                 # two graphs, one workspace
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            scores.project_int8(*scores.quantize_rows(x, out=pair), w, u, out=out, workspace=works[0])
+        graphs.append(graph)
+    for i in range(4):
+        x.copy_(torch.randn((M, K), generator=gen(30 + i), device=DEV).to(BF16))
+        out.zero_()
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, plain(*scores.quantize_rows(x), w, u, None, BF16))
+
+
+def quantised(x):
+    x = x.float()
+    a = x.abs().amax(1)
+    a = torch.where(torch.isnan(x).any(1), float("nan"), a)
+    bad, zero = ~torch.isfinite(a), a < 2.0 ** -119
+    r = torch.where(bad | zero, 0.0, a.reciprocal() * 127)
+    q = torch.where(bad[:, None], 0.0, torch.round(x * r[:, None]))
+    return q.to(torch.int8), torch.where(bad, float("nan"), torch.where(zero, 0.0, a / torch.full_like(a, 127)))     # (a number as divisor would become a product)
+
+
+@pytest.mark.parametrize("R,K", [(1, 1), (3, 7), (5, 100), (2, 4096), (9, 5000), (1, 8191), (2, 20001), (4, 70000), (600, 64)])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_quantise(R, K, dtype):
+    for shift in (0, 1, 8):
+        wide = (torch.randn((R, K + 24), generator=gen(K), device=DEV) * torch.exp2(torch.randint(-9, 6, (R, 1), generator=gen(1), device=DEV).float())).to(dtype)
+        x = wide[:, shift:shift + K]
+        want = quantised(x)
+        buf = torch.full((R + 1, -(-K // 16) * 16 + 16), 99, dtype=torch.int8, device=DEV)
+        q, s = scores.quantize_rows(x, out=(buf[:R, :K], torch.empty((R,), device=DEV)))
+        assert torch.equal(q, want[0]) and torch.equal(s, want[1])
+        assert (buf[R] == 99).all() and (buf[:, K:] == 99).all()
+        # a code is off by half a step at most, and by what x r and the scale round: 2^-24 of 127 each, thrice
+        assert ((q.double() * s.double()[:, None] - x.double()).abs() <= s.double()[:, None] * (0.5 + 3 * 127 * 2.0 ** -24)).all()
+        assert (q.abs().amax(1) == 127).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_quantise_special_rows(dtype):
+    x = torch.randn((8, 333), generator=gen(1), device=DEV).to(dtype)
+    x[0] = 0.0
+    x[1, 100] = float("nan")
+    x[2, 332] = float("inf")
+    x[3, 0] = float("-inf"); x[3, 1] = float("nan")
+    x[4] = torch.finfo(dtype).max
+    x[5] = torch.finfo(dtype).tiny
+    x[6] = -0.0
+    x[7] = 0.0; x[7, 7] = -1.0
+    q, s = scores.quantize_rows(x)
+    want = quantised(x)
+    assert torch.equal(q, want[0]) and torch.equal(torch.nan_to_num(s, nan=-1.0), torch.nan_to_num(want[1], nan=-1.0))
+    assert torch.isnan(s[1:4]).all() and (s[[0, 6]] == 0).all() and q[7, 7] == -127
+    w, u = codes(40, 333, 2)
+    y = scores.project_int8(q, s, w, u, dtype=FP32)
+    # (row 4: the sum times the scale, a step of the definition, passes fp32's largest number: 127 * 2^15 * 2^121)
+    assert torch.isnan(y[1:4]).all() and (y[0] == 0).all() and torch.isfinite(y[[0, 5, 6, 7]]).all()
+    assert torch.equal(y[[0, 4, 5, 6, 7]], plain(q, s, w, u, None, FP32)[[0, 4, 5, 6, 7]])
+
+
+def test_hidden_states_to_verified_tokens_and_their_log_probabilities():
+    """The run of a decode step: quantise, project, verify, report; and the gradient of what was reported."""
+    B, N, V, K = 3, 12, 5000, 512
+    hidden = torch.randn((B * N, K), generator=gen(1), device=DEV).to(BF16)
+    w = torch.randn((V, K), generator=gen(2), device=DEV).to(BF16) * 0.1
+    wq, ws = scores.quantize_rows(w)
+    logits = scores.project_int8(*scores.quantize_rows(hidden), wq, ws, dtype=FP32)
+    # a row of codes is off by half a step of 1/127 of its largest: products of K such pairs
+    step = hidden.float().abs().amax(1)[:, None] * w.float().abs().amax(1)[None] / 127
+    far = step * (w.float().abs().sum(1) / w.float().abs().amax(1) + (hidden.float().abs().sum(1) / hidden.float().abs().amax(1))[:, None] + K / 127) * 0.51
+    assert ((logits - hidden.float() @ w.float().T).abs() <= far).all()
+    tok = logits.argmax(1).view(B, N)
+    parent = torch.arange(-1, N - 1, device=DEV).expand(B, N)
+    tok = torch.cat([tok[:, :1], tok[:, :-1]], 1)                   # every draft is the best token of its parent's row
+    out = mars.verify_tree(logits, tok, parent, theta=0.9)
+    assert (out["accept_len"] == N - 1).all()
+    got = scores.emitted_logprobs(logits, out, k=3)
+    ref = sc.reference(logits)
+    want = ref["logp"].gather(1, logits.argmax(1)[:, None]).view(B, N)
+    assert (got["logprob"].double() - want).abs().max() <= sc.UNIT * (sc.SUM + 200)
+    assert torch.equal(got["top_id"][:, :, 0].long(), logits.argmax(1).view(B, N))
+    z = logits.clone().requires_grad_()
+    lp, _ = scores.logprobs(z, logits.argmax(1))
+    lp.sum().backward()
+    sc.check_grad(logits, z.grad, ref, logits.argmax(1)[:, None].int(), torch.ones((B * N, 1), device=DEV), None, 1.0)
+
+
+def test_refusals_of_the_binding():
+    (q, s), (w, u) = codes(4, 64, 1), codes(10, 64, 2)
+    good = scores.project_workspace(4, 10, 64, DEV)
+    for bad in (lambda: scores.project_int8(q, s[:3], w, u), lambda: scores.project_int8(q.float(), s, w, u),
+                lambda: scores.project_int8(q, s.double(), w, u), lambda: scores.project_int8(q[:, :32], s, w, u),
+                lambda: scores.project_int8(q, s, w, u, dtype=FP16), lambda: scores.project_int8(q, s, w, u, bias=torch.zeros(9, device=DEV)),
+                lambda: scores.project_int8(q, s, w, u, out=torch.empty((4, 9), device=DEV)),
+                lambda: scores.project_int8(q, s, w, u, workspace=good[:100]),
+                lambda: scores.project_int8(q, s, w, u, workspace=good[1:]),
+                lambda: scores.project_int8(q[:, 1:17], s, w[:, :16], u), lambda: scores.project_int8(q.cpu(), s.cpu(), w, u),
+                lambda: scores.quantize_rows(q), lambda: scores.quantize_rows(s), lambda: scores.quantize_rows(torch.zeros((2, 64))),
+                lambda: scores.quantize_rows(torch.zeros((2, 20), device=DEV), out=(torch.empty((2, 20), dtype=torch.int8, device=DEV), torch.empty(2, device=DEV))),
+                lambda: scores.project_workspace(0, 10, 64, DEV)):
+        with pytest.raises(mars.MarsError):
+            bad()

@@ -49,3 +49,37 @@ def test_gradient_refusals(lib):
     for k, bad in (("dt", 2), ("J", 1025), ("T", 1e-45)):
         assert f(**{k: bad}) == UNSUPPORTED, (k, bad)
     assert f(rows=1 << 27, V=1 << 20, ld=1 << 20, ld_grad=1 << 20) == UNSUPPORTED
+
+
+def test_quantise_refusals(lib):
+    d = dict(x=P, ldx=100, dt=mars.BF16, rows=4, K=100, q=Q, ldq=112, scale=P, stream=N)
+    f = lambda **k: call(lib.mars_quantize_rows, d, **k)  # noqa: E731
+    for k in ("x", "q", "scale"):
+        assert f(**{k: N}) == INVALID, k
+    for k, bad in (("ldx", 99), ("ldq", 96), ("ldq", 104), ("rows", 0), ("K", 0), ("q", ctypes.c_void_p(8200)), ("x", ctypes.c_void_p(4097))):
+        assert f(**{k: bad}) == INVALID, (k, bad)
+    assert f(dt=mars.FP32, x=ctypes.c_void_p(4098)) == INVALID
+    for k, bad in (("dt", 3), ("rows", 1 << 31)):
+        assert f(**{k: bad}) == UNSUPPORTED, (k, bad)
+    assert f(K=(1 << 17) + 1, ldx=1 << 18, ldq=1 << 18) == UNSUPPORTED
+
+
+def test_project_refusals_and_workspace(lib):
+    size = lib.mars_project_int8_workspace_bytes
+    need = size(40, 1000, 512)
+    assert need % 256 == 0 and need > 0
+    assert size(1, 1000, 512) <= need <= size(256, 1000, 512) and size(3840, 151936, 4096) == size(256, 1000, 512)
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, (1 << 17) + 1), (1, (1 << 28) + 1, 1), ((1 << 24) + 1, 1, 1), (1 << 24, 1 << 28, 1)):
+        assert size(*bad) == 0, bad
+    d = dict(xq=P, ldx=512, xs=P, wq=P, ldw=512, ws=P, bias=N, M=40, V=1000, K=500, out=P, ldo=1000, dt=mars.BF16, flags=0,
+             work=Q, bytes=need, stream=N)
+    f = lambda **k: call(lib.mars_project_int8, d, **k)  # noqa: E731
+    for k in ("xq", "xs", "wq", "ws", "out"):
+        assert f(**{k: N}) == INVALID, k
+    for k, bad in (("ldx", 496), ("ldx", 520), ("ldw", 496), ("ldw", 520), ("ldo", 999), ("M", 0), ("V", 0), ("K", 0),
+                   ("xq", ctypes.c_void_p(4104)), ("wq", ctypes.c_void_p(4104)), ("out", ctypes.c_void_p(4097))):
+        assert f(**{k: bad}) == INVALID, (k, bad)
+    for k, bad in (("dt", 2), ("flags", 1), ("flags", 128)):
+        assert f(**{k: bad}) == UNSUPPORTED, (k, bad)
+    for k, bad in (("work", N), ("work", ctypes.c_void_p(8192 + 128)), ("bytes", need - 1)):
+        assert f(**{k: bad}) == WORKSPACE, (k, bad)
