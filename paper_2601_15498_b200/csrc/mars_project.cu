@@ -147,7 +147,8 @@ constexpr int kPjStride = kPjGroup * kPjWarps / 4;
 constexpr int kPjThreads = 64 + 32 * kPjWarps;
 constexpr int kPjMaxStages = 10;
 constexpr int kPjPairs = 74;                // pairs of blocks that fill a B200
-constexpr int kPjHolders = 4;               // parts that a cut tile of many tokens goes to
+constexpr int kPjHolders = 4;               // parts that a cut tile goes to (or one more)
+constexpr int kPjFewTokens = 64;
 constexpr uint32_t kPjABytes = kPjRows * kPjBK;
 constexpr uint32_t kPjTmemCols = 512;
 constexpr size_t kPjRing = 200 * 1024;
@@ -279,6 +280,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     ProjectWalk walk(p);
     ProjectSegment s;
 
+    pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 2 * kPjWarps); }
@@ -296,6 +298,8 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
     volatile int *abort_flag = &s_abort;
+    pdl_wait();                    // the set-up above lies under the predecessor's end
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;      // (a wait gives up after a second at the earliest)
 
     if (warp == 0) {
         if (lane == 0) {
@@ -555,20 +559,24 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
         return MARS_ERR_CUDA;
     int pairs = project_pairs();
     if (pairs < 1) return MARS_ERR_CUDA;
-    p.rounds = p.n_tiles / pairs;
+    // Few tokens: every weight tile is read once whoever takes it, the sums of a cut tile are small, and one
+    // contiguous range of the weights for each pair streams faster than tiles dealt round by round.
+    p.rounds = p.n_ttiles == 1 && p.tokens <= kPjFewTokens ? 0 : p.n_tiles / pairs;
     const int n_cut = p.n_tiles - p.rounds * pairs;
     const long long cut = (long long)n_cut * p.kblocks;
-    // Even shares, but a tile of many tokens goes to a few pairs only: each of them writes its sums, and one reads all.
+    // Even shares, but a tile goes to a few pairs only: each of them writes its sums, and one reads all.
     p.per = (cut + pairs - 1) / pairs;
-    const int least = p.tokens > 64 ? (p.kblocks + kPjHolders - 1) / kPjHolders : 1;
+    const int least = (p.kblocks + kPjHolders - 1) / kPjHolders;
     if (p.per < least) p.per = least;
     if (p.rounds == 0) pairs = (int)((cut + p.per - 1) / p.per);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(workspace, 0, (flags & MARS_COUNTERS_ZERO) ? 4 : kPjHead, st) != cudaSuccess)
-        return MARS_ERR_CUDA;
-    if (dt == MARS_BF16) project_kernel<MARS_BF16><<<2 * pairs, kPjThreads, kPjSmemBytes, st>>>(map_w, map_x, p);
-    else project_kernel<MARS_FP32><<<2 * pairs, kPjThreads, kPjSmemBytes, st>>>(map_w, map_x, p);
-    return cudaGetLastError() == cudaSuccess ? MARS_OK : MARS_ERR_CUDA;
+    if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kPjHead, st) != cudaSuccess) return MARS_ERR_CUDA;
+    void (*kernel)(const CUtensorMap, const CUtensorMap, const ProjectParams) =
+        dt == MARS_BF16 ? project_kernel<MARS_BF16> : project_kernel<MARS_FP32>;
+    const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, kernel, dim3(2 * pairs), dim3(kPjThreads), kPjSmemBytes, st,
+                                     map_w, map_x, p);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
+    return MARS_OK;
 }
 
 }  // extern "C"
