@@ -3,8 +3,8 @@
 // With m the row's largest logit, c = log2(e) / T and x_v = (z_v - m) c:
 //   s = sum 2^x,  u = sum 2^x x,  ln p_v = (z_v - m) / T - ln s,  entropy = ln s - ln2 u / s,
 // so one pass suffices: every thread keeps (m, s, u) of what it has seen and rescales them when its
-// maximum rises by d (in units of x): s 2^d, (u + s d) 2^d.  Differences are taken before the scaling,
-// so logits of any size keep their exact distances.  The gradient of g = sum_j grad_logprob_j and
+// maximum rises by d (in units of x): s 2^d, (u + s d) 2^d.  Maxima are kept unscaled and differences of them
+// taken before the scaling, so logits of any size keep their distances.  The gradient of g = sum_j grad_logprob_j and
 // h = grad_entropy is, without the tokens' own terms,
 //   -p (g + h (ln p + entropy)) / T = 2^x (a + b x),  a = -(g + h (entropy - ln s)) / (T s),  b = -h ln2 / (T s).
 #include "mars_fp32.cuh"
@@ -24,6 +24,18 @@ namespace mars {
 
 namespace cg = cooperative_groups;
 
+#ifndef LP_DB
+#define LP_DB 0
+#endif
+#ifndef LP_U
+#define LP_U 8
+#define LP_B 4
+#endif
+#ifndef LP_TU
+#define LP_TU 8
+#define LP_TB 4
+#endif
+
 constexpr int kScMaxSplit = 8;                  // blocks per row = blocks per cluster
 constexpr int kScTargetBlocks = 148 * 4;        // resident blocks of the forward kernel
 constexpr int kScMinSliceBytes = 24 * 1024;     // three quarters of a batch of one block
@@ -35,6 +47,7 @@ struct LogprobParams {
     const int32_t *row_ids;     // or null
     int V, S, L;                // blocks per row, columns per block
     float temperature, c;       // c = log2(e) / temperature
+    float reach;                // 200 / c
     const int32_t *tok;
     int J, k;
     float *logprob, *entropy, *stats;
@@ -80,20 +93,17 @@ __device__ __forceinline__ Soft soft_shfl_xor(const Soft &a, int m)
     return o;
 }
 
-// Logits this far below the reference have 2^x = 0 (x <= -200) and are raised to it, so that -inf and NaN
-// need no test of their own: 2^x x is then 0 and not 0 * infinity.  Where a reference is so large, or c so
-// extreme, that no such level exists in fp32, `ok` is false and the elements are taken one by one.
-struct SoftFloor {
-    float z;
-    bool ok;
+// The fast form of x: one fma with R = fl(ref c), which gives x + d with d = ref c - R exactly (below 2^-4); a
+// thread's sums are kept with that offset and freed of it at the end.  Logits far below the reference are raised
+// to a floor where 2^x = 0 (x <= -199), so that -inf and NaN need no test of their own: 2^x x is then 0 and not
+// 0 * infinity.  Where |ref c| passes 2^20, or no such floor exists in fp32, `fast` is false, d = 0, and the
+// elements are taken one by one, their differences before the scaling.
+struct SoftState {
+    Soft a;
+    float R, d;
+    uint32_t floor;          // packed as the logits are
+    bool fast;
 };
-__device__ __forceinline__ SoftFloor soft_floor(float ref, float c)
-{
-    SoftFloor f;
-    f.z = ref - fmaxf(200.0f / c, fabsf(ref) * 0x1p-6f);
-    f.ok = f.z > -3e38f && fabsf(ref) * c < 1e38f;
-    return f;
-}
 
 // max(z, floor) of a packed word; the floor as a bf16 pair is rounded down.
 template <int DT>
@@ -104,6 +114,18 @@ __device__ __forceinline__ uint32_t soft_floor_word(float z)
     const uint32_t h = (b >> 31 ? b + 0xffffu : b) >> 16;
     return h | h << 16;
 }
+
+template <int DT>
+__device__ __forceinline__ void soft_reference(SoftState &t, float ref, float c, float reach)
+{
+    const float floor = ref - fmaxf(reach, fabsf(ref) * 0x1p-6f);
+    t.a.ref = ref;
+    t.R = ref * c;
+    t.fast = floor > -3e38f && fabsf(t.R) <= 0x1p20f;
+    t.d = t.fast ? fmaf(ref, c, -t.R) : 0.0f;
+    t.floor = soft_floor_word<DT>(floor);
+}
+
 template <int DT>
 __device__ __forceinline__ uint4 soft_clamp(uint4 v, uint32_t w)
 {
@@ -122,12 +144,6 @@ __device__ __forceinline__ void soft_term(float z, float ref, float c, float &su
     dot = fmaf(e, x, dot);
 }
 
-__device__ __forceinline__ void soft_add(Soft &a, float z, float c)
-{
-    if (z > a.ref) { soft_move(a, soft_distance(a.ref, z, c)); a.ref = z; }
-    soft_term(z, a.ref, c, a.sum, a.dot);
-}
-
 // The elements of a batch one by one, read again; kept out of the fast path's registers.
 template <int DT>
 __device__ __noinline__ float2 soft_batch_slow(const uint4 *vbase, int v0, int nvec, int U, float ref, float c)
@@ -141,29 +157,55 @@ __device__ __noinline__ float2 soft_batch_slow(const uint4 *vbase, int v0, int n
     return make_float2(sum, dot);
 }
 
+// Something with the maximum m joins: the reference moves up to it.
+template <int DT>
+__device__ __forceinline__ void soft_rise(SoftState &t, float m, float c, float reach)
+{
+    if (!(m > t.a.ref)) return;
+    const float move = soft_distance(t.a.ref, m, c), d = t.d;
+    soft_reference<DT>(t, m, c, reach);
+    soft_move(t.a, move + (t.d - d));
+}
+
+template <int DT>
+__device__ __forceinline__ void soft_single(SoftState &t, float z, float c, float reach)
+{
+    soft_rise<DT>(t, z, c, reach);
+    if (!(z > -INFINITY)) return;
+    const float x = soft_distance(z, t.a.ref, c) + t.d, e = ex2f(x);
+    t.a.sum += e;
+    t.a.dot = fmaf(e, x, t.a.dot);
+}
+
+// The state's sums without the offset.
+__device__ __forceinline__ Soft soft_free(SoftState t)
+{
+    soft_move(t.a, -t.d);
+    return t.a;
+}
+
 // A batch with the maximum bm joins.
 template <int DT, int U>
-__device__ __forceinline__ void soft_batch(Soft &a, const uint4 (&v)[U], float bm, float c, const uint4 *vbase, int v0, int nvec)
+__device__ __forceinline__ void soft_batch(SoftState &t, const uint4 (&v)[U], float bm, float c, float reach, const uint4 *vbase,
+                                           int v0, int nvec)
 {
     typedef Elem<DT> E;
-    if (bm > a.ref) { soft_move(a, soft_distance(a.ref, bm, c)); a.ref = bm; }
-    if (!(fabsf(a.ref) < INFINITY)) return;          // nothing above -inf so far, or no softmax
-    const SoftFloor f = soft_floor(a.ref, c);
-    if (!f.ok) {
-        const float2 t = soft_batch_slow<DT>(vbase, v0, nvec, U, a.ref, c);
-        a.sum += t.x;
-        a.dot += t.y;
+    soft_rise<DT>(t, bm, c, reach);
+    if (!t.fast) {
+        if (!(fabsf(t.a.ref) < INFINITY)) return;          // nothing above -inf so far, or no softmax
+        const float2 s = soft_batch_slow<DT>(vbase, v0, nvec, U, t.a.ref, c);
+        t.a.sum += s.x;
+        t.a.dot += s.y;
         return;
     }
-    const uint32_t w = soft_floor_word<DT>(f.z);
-    const float2 nref = make_float2(-a.ref, -a.ref), c2 = make_float2(c, c);
+    const float2 nr = make_float2(-t.R, -t.R), c2 = make_float2(c, c);
     float2 s0 = make_float2(0.0f, 0.0f), d0 = s0, s1 = s0, d1 = s0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint4 t = soft_clamp<DT>(v[u], w);
+        const uint4 w = soft_clamp<DT>(v[u], t.floor);
 #pragma unroll
         for (int e = 0; e < E::kVec; e += 2) {
-            const float2 x = mul2(add2(make_float2(E::elem(t, e), E::elem(t, e + 1)), nref), c2);
+            const float2 x = fma2(make_float2(E::elem(w, e), E::elem(w, e + 1)), c2, nr);
             const float2 y = make_float2(ex2f(x.x), ex2f(x.y));
             if (e & 2) { s1 = add2(s1, y); d1 = fma2(y, x, d1); }
             else { s0 = add2(s0, y); d0 = fma2(y, x, d0); }
@@ -171,9 +213,109 @@ __device__ __forceinline__ void soft_batch(Soft &a, const uint4 (&v)[U], float b
     }
     s0 = add2(s0, s1);
     d0 = add2(d0, d1);
-    a.sum += s0.x + s0.y;
-    a.dot += d0.x + d0.y;
+    t.a.sum += s0.x + s0.y;
+    t.a.dot += d0.x + d0.y;
 }
+
+// A batch of vectors (-inf where there is none), and its maximum.
+template <int DT, int U>
+__device__ __forceinline__ void load_raw(const uint4 *vbase, int bi, int nvec, uint4 (&v)[U])
+{
+    const int v0 = bi * kTkThreads * U + threadIdx.x;
+    if ((bi + 1) * kTkThreads * U <= nvec) {          // a full batch (the same for all threads) needs no guards
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = ld_stream(vbase + v0 + u * kTkThreads);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = v0 + u * kTkThreads < nvec ? ld_stream(vbase + v0 + u * kTkThreads) : Elem<DT>::neg_inf();
+    }
+}
+template <int DT, int U>
+__device__ __forceinline__ float batch_maximum(const uint4 (&v)[U])
+{
+    typedef Elem<DT> E;
+    typename E::packed_t m = E::vred(v[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u) m = E::pmax(m, E::vred(v[u]));
+    return E::to_float(m);
+}
+
+// The slice's best k.  While the slice streams by, a thread keeps the largest element that it has seen and nothing
+// else.  The k-th largest of the threads' maxima is a floor under the slice's k-th best, and what reaches it lies with
+// the threads whose maximum does, k of them where values differ: warps read those threads' elements once more (1/256
+// of the slice each), and what reaches the floor, some more than k elements, is ranked.  Order does not matter to it;
+// slices in which very many elements tie at the floor are selected again by topk_slice_exact.
+struct TopSelect {
+    __align__(8) Cand cand[kTkCap];
+    __align__(8) Cand xlist[kTkWarps * kTkMaxK];    // exact fallback only
+    int xqn[kTkWarps];
+    unsigned xfloor;
+    unsigned top[kTkWarps * kTkMaxK];               // tk_enc of the warps' largest maxima
+    unsigned floor;
+    int n, hits;
+    int hit[kTkThreads];
+
+    __device__ __forceinline__ void append(float z, int id)
+    {
+        const int at = atomicAdd(&n, 1);
+        if (at < kTkCap) { cand[at].z = z; cand[at].id = id; }
+    }
+
+    // All threads, `best` the thread's maximum; list[0 .. k-1] gets the slice's best, unused entries {-inf, kNoId}.
+    template <int DT>
+    __device__ __forceinline__ void finish(int k, float best, const char *rowp, int lo, int hi, int vlo, int nvec, Cand *list)
+    {
+        typedef Elem<DT> E;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        // a table of each warp's m largest maxima: its k-th largest never exceeds theirs, and falls short of it
+        // only where one warp holds more than m of the block's k largest
+        const int m = min(k, 4 + (k >> 2)), nt = kTkWarps * m;
+        const unsigned mine = best > -INFINITY ? tk_enc(best) : 0u;
+        unsigned left = mine;
+        for (int i = 0; i < m; ++i) {
+            const unsigned most = __reduce_max_sync(0xffffffffu, left);
+            const unsigned who = __ballot_sync(0xffffffffu, left == most);
+            if (lane == __ffs(who) - 1) { top[warp * m + i] = most; left = 0u; }
+        }
+        if (tid == 0) { floor = 1u; hits = 0; }
+        if (tid < k) { list[tid].z = -INFINITY; list[tid].id = kNoId; }
+        __syncthreads();
+        for (int i = tid; i < nt; i += kTkThreads) {
+            const unsigned t = top[i];
+            int ahead = 0;
+            for (int j = 0; j < nt; ++j) ahead += (top[j] > t || (top[j] == t && j < i)) ? 1 : 0;
+            if (ahead == k - 1 && t > 1u) floor = t;
+        }
+        __syncthreads();
+        if (mine >= floor) hit[atomicAdd(&hits, 1)] = tid;
+        __syncthreads();
+        const uint4 *vbase = (const uint4 *)(rowp + (size_t)vlo * E::kBytes);
+        const float f = floor > 1u ? tk_dec(floor) : -INFINITY;
+        for (int h = warp; h < hits; h += kTkWarps) {
+            for (int vi = hit[h] + lane * kTkThreads; vi < nvec; vi += 32 * kTkThreads) {
+                const uint4 v = ld_stream(vbase + vi);
+                if (!(E::to_float(E::vred(v)) >= f)) continue;
+#pragma unroll
+                for (int e = 0; e < E::kVec; ++e) {
+                    const float x = E::elem(v, e);
+                    if (x >= f && x > -INFINITY) append(x, vlo + vi * E::kVec + e);
+                }
+            }
+        }
+        __syncthreads();
+        const int found = n;
+        if (found > kTkCap) {
+            topk_slice_exact<DT>(rowp, lo, hi, k, list, cand, xlist, xqn, &xfloor);
+            return;
+        }
+        for (int i = tid; i < found; i += kTkThreads) {
+            const Cand c = cand[i];
+            int ahead = 0;
+            for (int j = 0; j < found; ++j) ahead += beats(cand[j].z, cand[j].id, c.z, c.id) ? 1 : 0;
+            if (ahead < k) list[ahead] = c;
+        }
+    }
+};
 
 // What a row comes to.
 struct RowScore {
@@ -192,7 +334,7 @@ template <int DT, int U, int MINB, bool TOP>
 __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const LogprobParams p)
 {
     typedef Elem<DT> E;
-    struct Select { TopkSelect s; };
+    struct Select { TopSelect s; };
     struct None {};
     __shared__ typename std::conditional<TOP, Select, None>::type s_sel;
     __shared__ Soft s_soft[kTkThreads / 32];
@@ -230,13 +372,10 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
     const int ntail = hi - tlo;
     const uint4 *vbase = (const uint4 *)(rowp + (size_t)vlo * E::kBytes);
     constexpr int kBatchVecs = kTkThreads * U;
-    const int nfull = nvec / kBatchVecs;
     const float c = p.c;
 
     uint4 v[U];
-    typename E::packed_t q[U];
-    float bm = (nfull > 0) ? load_batch<DT, U, false>(vbase, tid, nvec, v, q)
-                           : load_batch<DT, U, true>(vbase, tid, nvec, v, q);
+    load_raw<DT, U>(vbase, 0, nvec, v);
     // the first tokens' logits are fetched beside the stream
     float zt = -INFINITY;
     bool inside = false;
@@ -245,36 +384,47 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         inside = t >= 0 && t < p.V;
         if (inside) zt = E::scalar(rowp, t);
     }
-    Soft a;
-    a.ref = -INFINITY; a.sum = 0.0f; a.dot = 0.0f;
+    const float reach = p.reach;
+    SoftState t;
+    t.a.ref = -INFINITY; t.a.sum = 0.0f; t.a.dot = 0.0f; t.d = 0.0f; t.fast = false;
+    float best = -INFINITY;
     if constexpr (TOP) {
-        s_sel.s.clear();
+        if (tid == 0) s_sel.s.n = 0;
         __syncthreads();
     }
     auto single = [&](int at) {
         const float z = E::scalar(rowp, at);
-        soft_add(a, z, c);
+        soft_single<DT>(t, z, c, reach);
         if constexpr (TOP) { if (z > -INFINITY) s_sel.s.append(z, at); }
     };
     if (tid < nhead) single(lo + tid);
     if (tid < ntail) single(tlo + tid);
-    if constexpr (TOP) s_sel.s.first_floor(k, bm);
-
-    auto batch = [&](int v0) {
-        if constexpr (TOP) s_sel.s.template scan<DT, U>(k, v, q, bm, vlo + v0 * E::kVec);
-        soft_batch<DT, U>(a, v, bm, c, vbase, v0, nvec);
+    const int nbatch = (nvec + kBatchVecs - 1) / kBatchVecs;
+    auto batch = [&](const uint4 (&x)[U], int bi) {
+        const float bm = batch_maximum<DT, U>(x);
+        if constexpr (TOP) best = fmaxf(best, bm);
+        soft_batch<DT, U>(t, x, bm, c, reach, vbase, bi * kBatchVecs + tid, nvec);
     };
-    batch(tid);
-    for (int bi = 1; bi < nfull; ++bi) {
-        bm = load_batch<DT, U, false>(vbase, bi * kBatchVecs + tid, nvec, v, q);
-        batch(bi * kBatchVecs + tid);
+#if LP_DB
+    uint4 w[U];
+    if (nbatch > 1) load_raw<DT, U>(vbase, 1, nvec, w);
+    // two buffers: a batch is on its way while the one before it is worked on
+    for (int bi = 0; bi < nbatch; bi += 2) {
+        batch(v, bi);
+        if (bi + 1 >= nbatch) break;
+        if (bi + 2 < nbatch) load_raw<DT, U>(vbase, bi + 2, nvec, v);
+        batch(w, bi + 1);
+        if (bi + 3 < nbatch) load_raw<DT, U>(vbase, bi + 3, nvec, w);
     }
-    if (nfull > 0 && nfull * kBatchVecs < nvec) {
-        bm = load_batch<DT, U, true>(vbase, nfull * kBatchVecs + tid, nvec, v, q);
-        batch(nfull * kBatchVecs + tid);
+#else
+    for (int bi = 0; bi < nbatch; ++bi) {
+        if (bi) load_raw<DT, U>(vbase, bi, nvec, v);
+        batch(v, bi);
     }
+#endif
 
     // ---- the block's (m, s, u) and list ----
+    Soft a = soft_free(t);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) a = soft_union(a, soft_shfl_xor(a, m), c);
     if (lane == 0) s_soft[warp] = a;
@@ -286,15 +436,7 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         for (int m = kTkThreads / 64; m > 0; m >>= 1) a = soft_union(a, soft_shfl_xor(a, m), c);
         if (lane == 0) s_block = a;
     }
-    if constexpr (TOP) {
-        if (s_sel.s.overflow) {
-            topk_slice_exact<DT>(rowp, lo, hi, k, s_list, s_sel.s.cand, s_sel.s.xlist, s_sel.s.xqn, &s_sel.s.floor);
-        } else if (warp == 0) {
-            s_sel.s.drain(k, true);
-            __syncwarp();
-            s_list[lane] = s_sel.s.list[lane];
-        }
-    }
+    if constexpr (TOP) s_sel.s.template finish<DT>(k, best, rowp, lo, hi, vlo, nvec, s_list);
 
     // ---- the row's ----
     int n_all = k;
@@ -370,7 +512,7 @@ struct GradParams {
     void *grad;
     long long ld, ld_grad;
     int V, S, L;                // blocks per row, columns per block
-    float temperature, c;
+    float temperature, c, reach;
     const int32_t *tok;
     int J;
     const float *stats, *entropy, *g, *h;
@@ -385,12 +527,22 @@ __device__ __forceinline__ void store_scalar(void *row, int at, float x)
     else ((float *)row)[at] = x;
 }
 
-// Gradient of one logit without the tokens' own terms.
-__device__ __forceinline__ float grad_term(float z, float m, float c, float a, float b)
+// Gradient of one logit without the tokens' own terms, by the arithmetic of the vector form where there is one, so
+// that a result does not depend on where its row begins.
+struct GradLine {
+    SoftState f;
+    float m, c, a, b, fa, fb;        // a + b x, and the same line in x + d times 2^-d
+};
+template <int DT>
+__device__ __forceinline__ float grad_term(float z, const GradLine &l)
 {
+    if (l.f.fast) {
+        const float x = fmaf(fmaxf(z, DT == MARS_BF16 ? __uint_as_float(l.f.floor & 0xffff0000u) : __uint_as_float(l.f.floor)), l.c, -l.f.R);
+        return ex2f(x) * fmaf(l.fb, x, l.fa);
+    }
     if (!(z > -INFINITY)) return 0.0f;
-    const float x = soft_distance(z, m, c);
-    return ex2f(x) * fmaf(b, x, a);
+    const float x = soft_distance(z, l.m, l.c);
+    return ex2f(x) * fmaf(l.b, x, l.a);
 }
 
 // Backward: a block takes a contiguous piece of one row.
@@ -402,8 +554,9 @@ __global__ void __launch_bounds__(kTkThreads) logprob_grad_kernel(const GradPara
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31;
-    const long long row = blockIdx.x / p.S;
-    const int lo = min((int)(blockIdx.x - row * p.S) * p.L, p.V), hi = min(p.V, lo + p.L);
+    // the last rows first: a forward pass that came just before has left them in L2
+    const long long block = (long long)gridDim.x - 1 - blockIdx.x, row = block / p.S;
+    const int lo = min((int)(block - row * p.S) * p.L, p.V), hi = min(p.V, lo + p.L);
     const char *zrow = (const char *)p.logits + (size_t)row * (size_t)p.ld * E::kBytes;
     char *grow = (char *)p.grad + (size_t)row * (size_t)p.ld_grad * E::kBytes;
     const int32_t *tok = p.tok + row * p.J;
@@ -432,49 +585,51 @@ __global__ void __launch_bounds__(kTkThreads) logprob_grad_kernel(const GradPara
     }
     hit = __syncthreads_or(hit);
 
-    const SoftFloor f = soft_floor(m, c);
+    GradLine line;
+    soft_reference<DT>(line.f, m, c, p.reach);
+    const SoftState &f = line.f;
+    const float fd = ex2f(-f.d);
+    line.m = m; line.c = c; line.a = a; line.b = b;
+    line.fa = fd * fmaf(-b, f.d, a); line.fb = fd * b;
     const uintptr_t a0 = (uintptr_t)(zrow + (size_t)lo * E::kBytes), b0 = (uintptr_t)(grow + (size_t)lo * E::kBytes);
-    if (((a0 ^ b0) & 15) || !ok || !f.ok) {
+    if (((a0 ^ b0) & 15) || !ok || !f.fast) {
         // rows that lie differently on 16-byte boundaries, and rows without fast form: one by one
         for (int i = lo + tid; i < hi; i += kTkThreads)
-            store_scalar<DT>(grow, i, ok ? grad_term(E::scalar(zrow, i), m, c, a, b) : 0.0f);
+            store_scalar<DT>(grow, i, ok ? grad_term<DT>(E::scalar(zrow, i), line) : 0.0f);
     } else {
         const int nhead = min((int)(((16 - (a0 & 15)) & 15) / E::kBytes), hi - lo);
         const int vlo = lo + nhead, nvec = (hi - vlo) / E::kVec, tlo = vlo + nvec * E::kVec, ntail = hi - tlo;
-        if (tid < nhead) store_scalar<DT>(grow, lo + tid, grad_term(E::scalar(zrow, lo + tid), m, c, a, b));
-        if (tid < ntail) store_scalar<DT>(grow, tlo + tid, grad_term(E::scalar(zrow, tlo + tid), m, c, a, b));
+        if (tid < nhead) store_scalar<DT>(grow, lo + tid, grad_term<DT>(E::scalar(zrow, lo + tid), line));
+        if (tid < ntail) store_scalar<DT>(grow, tlo + tid, grad_term<DT>(E::scalar(zrow, tlo + tid), line));
         const uint4 *src = (const uint4 *)(zrow + (size_t)vlo * E::kBytes);
         uint4 *dst = (uint4 *)(grow + (size_t)vlo * E::kBytes);
-        const uint32_t w = soft_floor_word<DT>(f.z);
-        const float2 nm = make_float2(-m, -m), c2 = make_float2(c, c), a2 = make_float2(a, a), b2 = make_float2(b, b);
-        for (int v0 = tid; v0 < nvec; v0 += kTkThreads * kGrU) {
+        const float2 nr = make_float2(-f.R, -f.R), c2 = make_float2(c, c), a2 = make_float2(line.fa, line.fa), b2 = make_float2(line.fb, line.fb);
+        auto one = [&](const uint4 &v) {
+            const uint4 t = soft_clamp<DT>(v, f.floor);
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < E::kVec; e += 2) {
+                const float2 x = fma2(make_float2(E::elem(t, e), E::elem(t, e + 1)), c2, nr);
+                const float2 y = mul2(make_float2(ex2f(x.x), ex2f(x.y)), fma2(b2, x, a2));
+                if constexpr (DT == MARS_BF16) {
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[e / 2]) : "f"(y.y), "f"(y.x));
+                } else {
+                    o[e] = __float_as_uint(y.x);
+                    o[e + 1] = __float_as_uint(y.y);
+                }
+            }
+            return make_uint4(o[0], o[1], o[2], o[3]);
+        };
+        int v0 = tid;
+        // (plain loads: the gradient may overwrite the logits; stores that leave L2 to them)
+        for (; v0 + (kGrU - 1) * kTkThreads < nvec; v0 += kGrU * kTkThreads) {
             uint4 v[kGrU];
 #pragma unroll
-            for (int u = 0; u < kGrU; ++u)
-                if (v0 + u * kTkThreads < nvec) v[u] = src[v0 + u * kTkThreads];   // (plain loads: the gradient may overwrite)
+            for (int u = 0; u < kGrU; ++u) v[u] = src[v0 + u * kTkThreads];
 #pragma unroll
-            for (int u = 0; u < kGrU; ++u) {
-                if (v0 + u * kTkThreads >= nvec) break;
-                const uint4 t = soft_clamp<DT>(v[u], w);
-                float y[E::kVec];
-#pragma unroll
-                for (int e = 0; e < E::kVec; e += 2) {
-                    const float2 x = mul2(add2(make_float2(E::elem(t, e), E::elem(t, e + 1)), nm), c2);
-                    const float2 r = mul2(make_float2(ex2f(x.x), ex2f(x.y)), fma2(b2, x, a2));
-                    y[e] = r.x; y[e + 1] = r.y;
-                }
-                uint4 o;
-                if constexpr (DT == MARS_BF16) {
-                    uint32_t q[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
-                    o = make_uint4(q[0], q[1], q[2], q[3]);
-                } else {
-                    o = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-                }
-                dst[v0 + u * kTkThreads] = o;
-            }
+            for (int u = 0; u < kGrU; ++u) __stcs(dst + v0 + u * kTkThreads, one(v[u]));
         }
+        for (; v0 < nvec; v0 += kTkThreads) __stcs(dst + v0, one(src[v0]));
     }
     if (!hit) return;
     __syncthreads();
@@ -487,7 +642,7 @@ __global__ void __launch_bounds__(kTkThreads) logprob_grad_kernel(const GradPara
         if (!first) continue;
         float own = 0.0f;
         for (int i = j; i < p.J; ++i) own += tok[i] == t ? gj[i] : 0.0f;
-        store_scalar<DT>(grow, t, grad_term(s_z[j], m, c, a, b) + own / p.temperature);
+        store_scalar<DT>(grow, t, grad_term<DT>(s_z[j], line) + own / p.temperature);
     }
 }
 
@@ -513,7 +668,7 @@ static int slice_columns(int V, int S)
 template <int DT>
 static cudaError_t logprob_launch(const LogprobParams &p, unsigned rows, cudaStream_t st)
 {
-    void (*kernel)(const LogprobParams) = p.k ? logprob_kernel<DT, kTkU, 3, true> : logprob_kernel<DT, kTkU, 4, false>;
+    void (*kernel)(const LogprobParams) = p.k ? logprob_kernel<DT, LP_TU, LP_TB, true> : logprob_kernel<DT, LP_U, LP_B, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(rows * (unsigned)p.S); cfg.blockDim = dim3(kTkThreads); cfg.stream = st;
     cudaLaunchAttribute at[2];
@@ -551,6 +706,7 @@ mars_status_t mars_token_logprobs(const void *logits, int64_t ld, mars_dtype_t d
     p.temperature = temperature;
     p.c = (float)(1.4426950408889634 / (double)temperature);
     if (!(p.c > 0.0f) || p.c > 3.40282347e38f) return MARS_ERR_UNSUPPORTED;
+    p.reach = 200.0f / p.c;
     p.tok = tok; p.J = J; p.k = k;
     p.logprob = logprob; p.entropy = entropy; p.stats = stats; p.top_id = top_id; p.top_logprob = top_logprob;
     cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -576,13 +732,18 @@ mars_status_t mars_token_logprobs_backward(const void *logits, int64_t ld, mars_
     if (grad == logits && ld_grad != ld) return MARS_ERR_INVALID_ARG;
     GradParams p;
     p.logits = logits; p.grad = grad; p.ld = ld; p.ld_grad = ld_grad; p.V = V;
-    const int piece = kTkThreads * kGrU * 16 / es;       // columns that a block holds in registers at once
-    p.S = (V + piece - 1) / piece;
+    // Batches per block: each block spends about 300 instructions a thread before its first logit, so as many as leave
+    // the GPU full, up to eight.
+    const int64_t batch = kTkThreads * kGrU * 16 / es, batches = (V + batch - 1) / batch;
+    int64_t each = rows * batches / (148 * 8);
+    each = each < 1 ? 1 : each > 8 ? 8 : each;
+    p.S = (int)((batches + each - 1) / each);
     p.L = slice_columns(V, p.S);
     if (rows * p.S > 0x7fffffffll) return MARS_ERR_UNSUPPORTED;
     p.temperature = temperature;
     p.c = (float)(1.4426950408889634 / (double)temperature);
     if (!(p.c > 0.0f) || p.c > 3.40282347e38f) return MARS_ERR_UNSUPPORTED;
+    p.reach = 200.0f / p.c;
     p.tok = tok; p.J = J; p.stats = stats; p.entropy = entropy; p.g = grad_logprob; p.h = grad_entropy;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool overlap = hook(kHookNoOverlap) == 0;

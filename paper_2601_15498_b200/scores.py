@@ -31,11 +31,19 @@ MAX_TOKENS, MAX_TOP = 1024, 32
 _ROW_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: 2}
 
 
-def _call(fn, device, *args) -> None:
-    """fn(*args, stream) with `device` current; raises on a refusal."""
-    with torch.cuda.device(device):
-        code = fn(*args, torch.cuda.current_stream(device).cuda_stream)
-    _check(code, fn.__name__)
+# The calls below run once a decode step or more, so their host time counts: devices are compared by index, the
+# stream is taken as a raw handle, and the current device is only changed where it has to be.
+
+def _call(fn, index: int, *args) -> None:
+    """fn(*args, stream) with device `index` current; raises on a refusal."""
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
+        code = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args, stream)
+    if code:
+        _check(code, fn.__name__)
 
 
 def _ptr(t):
@@ -57,7 +65,7 @@ def _into(out, name: str, shape, dtype, device):
     t = None if out is None else out.get(name)
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
         raise MarsError(f"out[{name!r}] must be a contiguous {dtype} tensor {list(shape)} on {device}")
     return t
 
@@ -75,7 +83,7 @@ def quantize_rows(x: torch.Tensor, out=None):
     _codes(q, scale, "out")
     if q.shape != x.shape or q.device != x.device:
         raise MarsError("out must have the shape and device of x")
-    _call(lib().mars_quantize_rows, x.device, x.data_ptr(), x.stride(0), _ROW_DTYPES[x.dtype], R, K, q.data_ptr(), q.stride(0),
+    _call(lib().mars_quantize_rows, x.get_device(), x.data_ptr(), x.stride(0), _ROW_DTYPES[x.dtype], R, K, q.data_ptr(), q.stride(0),
           scale.data_ptr())
     return q, scale
 
@@ -125,7 +133,7 @@ def project_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_sc
         workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise MarsError("workspace must be a contiguous tensor beside the codes")
-    _call(lib().mars_project_int8, dev, xq.data_ptr(), xq.stride(0), x_scale.data_ptr(), wq.data_ptr(), wq.stride(0),
+    _call(lib().mars_project_int8, xq.get_device(), xq.data_ptr(), xq.stride(0), x_scale.data_ptr(), wq.data_ptr(), wq.stride(0),
           w_scale.data_ptr(), _ptr(bias), M, V, K, out.data_ptr(), out.stride(0), _dtype_code(out), flags,
           workspace.data_ptr(), workspace.nbytes)
     return out
@@ -149,7 +157,7 @@ def token_logprobs(logits: torch.Tensor, tok=None, temperature: float = 1.0, k: 
     if k:
         got["top_id"] = _into(out, "top_id", (R, k), torch.int32, dev)
         got["top_logprob"] = _into(out, "top_logprob", (R, k), torch.float32, dev)
-    _call(lib().mars_token_logprobs, dev, logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, float(temperature), _ptr(tok), J,
+    _call(lib().mars_token_logprobs, logits.get_device(), logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, float(temperature), _ptr(tok), J,
           int(k), _ptr(got.get("logprob")), got["entropy"].data_ptr(), got["stats"].data_ptr(), _ptr(got.get("top_id")),
           _ptr(got.get("top_logprob")))
     return got
@@ -176,7 +184,7 @@ def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logpr
         out = torch.empty((R, V), dtype=logits.dtype, device=dev)
     elif out.dim() != 2 or out.shape[0] != R or out.shape[1] < V or out.stride(1) != 1 or out.dtype != logits.dtype or out.device != dev:
         raise MarsError("out must be [rows, >= V] of the logits' dtype with unit inner stride")
-    _call(lib().mars_token_logprobs_backward, dev, logits.data_ptr(), ld, dt, R, V, float(temperature), tok.data_ptr(), J,
+    _call(lib().mars_token_logprobs_backward, logits.get_device(), logits.data_ptr(), ld, dt, R, V, float(temperature), tok.data_ptr(), J,
           stats.data_ptr(), _ptr(entropy), g.data_ptr(), _ptr(h), out.data_ptr(), out.stride(0))
     return out
 
