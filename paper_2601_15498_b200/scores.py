@@ -24,15 +24,18 @@ from __future__ import annotations
 import torch
 
 from . import mars
-from .mars import MarsError, _check, _dev_f32, _dev_i32, _dtype_code, _logits_args, lib
+from .mars import MarsError, _check, _dev_f32, _dev_i32, lib
 
 MAX_TOKENS, MAX_TOP = 1024, 32
 
+_LOGIT_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32}
 _ROW_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: 2}
 
 
-# The calls below run once a decode step or more, so their host time counts: devices are compared by index, the
-# stream is taken as a raw handle, and the current device is only changed where it has to be.
+_I32, _F32, _I8 = torch.int32, torch.float32, torch.int8
+
+# The calls below run once a decode step or more, so their host time counts: attributes are read once, devices
+# compared by index, the stream is taken as a raw handle, outputs come from the cheapest allocating call.
 
 def _call(fn, index: int, *args) -> None:
     """fn(*args, stream) with device `index` current; raises on a refusal."""
@@ -50,54 +53,94 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _tokens(tok, rows: int, device):
-    """(int32 [rows, J] on `device`, J) of tok [rows], [rows, J] or None."""
+def _logits(logits, V):
+    """(dtype code, rows, row stride, V, device index)."""
+    index, dtype = logits.get_device(), logits.dtype
+    if index < 0 or logits.dim() != 2 or dtype not in _LOGIT_DTYPES:
+        raise MarsError("logits must be [rows, >= V] of bfloat16 or float32 in device memory")
+    rows, width = logits.shape
+    ld, inner = logits.stride()
+    if inner != 1 and width != 1:
+        raise MarsError("logits must have unit inner stride")
+    V = width if V is None else int(V)
+    # a single row has no second one to be apart from
+    return _LOGIT_DTYPES[dtype], rows, max(ld, V) if rows == 1 else ld, V, index
+
+
+def _tokens(tok, rows: int, logits):
+    """(int32 [rows, J] beside the logits, J) of tok [rows], [rows, J] or None."""
     if tok is None:
         return None, 0
-    tok = _dev_i32(tok, device)
-    if tok.dim() not in (1, 2) or tok.shape[0] != rows:
-        raise MarsError(f"tok must be [{rows}] or [{rows}, J], got {list(tok.shape)}")
-    return tok, 1 if tok.dim() == 1 else tok.shape[1]
+    if type(tok) is not torch.Tensor or tok.dtype is not _I32 or tok.get_device() != logits.get_device() or not tok.is_contiguous():
+        tok = _dev_i32(tok, logits.device)
+    shape = tok.shape
+    if len(shape) not in (1, 2) or shape[0] != rows:
+        raise MarsError(f"tok must be [{rows}] or [{rows}, J], got {list(shape)}")
+    return tok, 1 if len(shape) == 1 else shape[1]
 
 
-def _into(out, name: str, shape, dtype, device):
-    """out[name], checked, or a new tensor."""
+def _out1(out, name: str, n: int, dtype, device, index: int):
+    """out[name] of n entries, checked, or a new tensor."""
     t = None if out is None else out.get(name)
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        raise MarsError(f"out[{name!r}] must be a contiguous {dtype} tensor {list(shape)} on {device}")
+        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+    return _checked(t, name, (n,), dtype, index)
+
+
+def _out2(out, name: str, n: int, m: int, dtype, device, index: int):
+    """The same for [n, m]."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return torch.empty_strided((n, m), (m, 1), dtype=dtype, device=device)
+    return _checked(t, name, (n, m), dtype, index)
+
+
+def _checked(t, name: str, shape, dtype, index: int):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise MarsError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on device {index}")
     return t
+
+
+def _codes(q, scale, name: str):
+    """(rows, K, row stride, device index) of a pair of codes and scales."""
+    index = q.get_device()
+    if index < 0 or q.dim() != 2 or q.dtype is not _I8:
+        raise MarsError(f"{name}: codes must be int8 [rows, K] in device memory")
+    rows, K = q.shape
+    ld, inner = q.stride()
+    if inner != 1 and K != 1:
+        raise MarsError(f"{name}: codes must have unit inner stride")
+    if scale.dtype is not _F32 or scale.shape != (rows,) or not scale.is_contiguous() or scale.get_device() != index:
+        raise MarsError(f"{name}: scales must be contiguous float32, one a row, beside the codes")
+    return rows, K, ld if rows > 1 else max(ld, -(-K // 16) * 16), index
 
 
 def quantize_rows(x: torch.Tensor, out=None):
     """mars_quantize_rows on the current stream: x [rows, K] (bfloat16, float16 or float32, unit inner stride) as
     (codes int8 [rows, K] in rows of a multiple of 16 bytes, scales float32 [rows]); `out` = such a pair."""
-    if not x.is_cuda or x.dim() != 2 or x.stride(1) != 1 or x.dtype not in _ROW_DTYPES:
+    index, dt = x.get_device(), _ROW_DTYPES.get(x.dtype)
+    if index < 0 or dt is None or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] != 1):
         raise MarsError("x must be [rows, K] of bfloat16, float16 or float32 with unit inner stride in device memory")
     R, K = x.shape
     if out is None:
-        out = (torch.empty((R, -(-K // 16) * 16), dtype=torch.int8, device=x.device)[:, :K],
-               torch.empty((R,), dtype=torch.float32, device=x.device))
-    q, scale = out
-    _codes(q, scale, "out")
-    if q.shape != x.shape or q.device != x.device:
-        raise MarsError("out must have the shape and device of x")
-    _call(lib().mars_quantize_rows, x.get_device(), x.data_ptr(), x.stride(0), _ROW_DTYPES[x.dtype], R, K, q.data_ptr(), q.stride(0),
-          scale.data_ptr())
+        ldq = -(-K // 16) * 16
+        q = torch.empty_strided((R, ldq), (ldq, 1), dtype=_I8, device=x.device)
+        if ldq != K:
+            q = q[:, :K]
+        scale = torch.empty_strided((R,), (1,), dtype=_F32, device=x.device)
+    else:
+        q, scale = out
+        r, k, ldq, i = _codes(q, scale, "out")
+        if (r, k, i) != (R, K, index):
+            raise MarsError("out must have the shape and device of x")
+    ldx = x.stride(0)
+    _call(lib().mars_quantize_rows, index, x.data_ptr(), max(ldx, K) if R == 1 else ldx, dt, R, K, q.data_ptr(), ldq, scale.data_ptr())
     return q, scale
 
 
-def _codes(q, scale, name: str) -> None:
-    if q.dim() != 2 or q.dtype != torch.int8 or q.stride(1) != 1 or not q.is_cuda:
-        raise MarsError(f"{name}: codes must be int8 [rows, K] with unit inner stride in device memory")
-    if scale.dtype != torch.float32 or tuple(scale.shape) != q.shape[:1] or not scale.is_contiguous() or scale.device != q.device:
-        raise MarsError(f"{name}: scales must be contiguous float32, one a row, beside the codes")
-
-
 def project_workspace(tokens: int, V: int, K: int, device) -> torch.Tensor:
-    """A zeroed workspace for project_int8 calls of these sizes; it serves any number of calls that do not
-    overlap."""
+    """A zeroed workspace for project_int8 calls of up to so many tokens, V and K of any size; it serves any
+    number of calls that do not overlap."""
     need = int(lib().mars_project_int8_workspace_bytes(tokens, V, K))
     if need == 0:
         raise MarsError("unsupported sizes")
@@ -110,32 +153,30 @@ def project_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_sc
     their scales (quantize_rows of the hidden states, and once of the weights).  `out` [tokens, >= V] (its dtype
     is used).  `workspace` comes from project_workspace and is used by these calls only; without one, a call
     allocates and clears its own."""
-    dev = xq.device
-    _codes(xq, x_scale, "xq")
-    _codes(wq, w_scale, "wq")
-    (M, K), V = xq.shape, wq.shape[0]
-    if wq.shape[1] != K or wq.device != dev:
+    M, K, ldx, index = _codes(xq, x_scale, "xq")
+    V, wk, ldw, wi = _codes(wq, w_scale, "wq")
+    if wk != K or wi != index:
         raise MarsError("xq and wq must have the same number of columns and device")
     if bias is not None:
-        bias = _dev_f32(bias, dev)
-        if tuple(bias.shape) != (V,):
-            raise MarsError(f"bias must be [{V}]")
+        bias = _checked(_dev_f32(bias, xq.device), "bias", (V,), _F32, index)
     if out is None:
-        out = torch.empty((M, V), dtype=dtype, device=dev)
-    if out.dim() != 2 or out.shape[0] != M or out.shape[1] < V or out.stride(1) != 1 or out.device != dev:
-        raise MarsError(f"out must be [{M}, >= {V}] with unit inner stride beside the codes")
+        if dtype not in _LOGIT_DTYPES:
+            raise MarsError("logits are bfloat16 or float32")
+        out = torch.empty_strided((M, V), (V, 1), dtype=dtype, device=xq.device)
+    dt, rows, ldo, width, oi = _logits(out, None)
+    if rows != M or width < V or oi != index:
+        raise MarsError(f"out must be [{M}, >= {V}] beside the codes")
     flags = mars.COUNTERS_ZERO
     if workspace is None:
         flags = 0
         need = int(lib().mars_project_int8_workspace_bytes(M, V, K))
         if need == 0:
             raise MarsError("unsupported sizes")
-        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
-    elif workspace.device != dev or not workspace.is_contiguous():
+        workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=xq.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
         raise MarsError("workspace must be a contiguous tensor beside the codes")
-    _call(lib().mars_project_int8, xq.get_device(), xq.data_ptr(), xq.stride(0), x_scale.data_ptr(), wq.data_ptr(), wq.stride(0),
-          w_scale.data_ptr(), _ptr(bias), M, V, K, out.data_ptr(), out.stride(0), _dtype_code(out), flags,
-          workspace.data_ptr(), workspace.nbytes)
+    _call(lib().mars_project_int8, index, xq.data_ptr(), ldx, x_scale.data_ptr(), wq.data_ptr(), ldw, w_scale.data_ptr(),
+          _ptr(bias), M, V, K, out.data_ptr(), ldo, dt, flags, workspace.data_ptr(), workspace.nbytes)
     return out
 
 
@@ -145,21 +186,25 @@ def token_logprobs(logits: torch.Tensor, tok=None, temperature: float = 1.0, k: 
     tok [rows, J], [rows] or None, `rows` int32 [rows] (logits row of each output row, -1 for none) or None
     (all).  Returns {"logprob" (shape of tok), "entropy" [rows], "stats" [rows, 2], and with k > 0 "top_id",
     "top_logprob" [rows, k]}, in the tensors of `out` where it has them."""
+    dt, n, ld, V, index = _logits(logits, V)
     dev = logits.device
-    dt, ld, V = _logits_args(logits, logits.shape[0], V)
-    n = logits.shape[0]
-    rows = None if rows is None else _dev_i32(rows, dev)
-    R = n if rows is None else rows.numel()
-    tok, J = _tokens(tok, R, dev)
-    got = {"entropy": _into(out, "entropy", (R,), torch.float32, dev), "stats": _into(out, "stats", (R, 2), torch.float32, dev)}
+    R = n
+    if rows is not None:
+        rows = _dev_i32(rows, dev)
+        R = rows.numel()
+    tok, J = _tokens(tok, R, logits)
+    entropy, stats = _out1(out, "entropy", R, _F32, dev, index), _out2(out, "stats", R, 2, _F32, dev, index)
+    got = {"entropy": entropy, "stats": stats}
+    logprob = top_id = top_logprob = None
     if tok is not None:
-        got["logprob"] = _into(out, "logprob", tok.shape, torch.float32, dev)
-    if k:
-        got["top_id"] = _into(out, "top_id", (R, k), torch.int32, dev)
-        got["top_logprob"] = _into(out, "top_logprob", (R, k), torch.float32, dev)
-    _call(lib().mars_token_logprobs, logits.get_device(), logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, float(temperature), _ptr(tok), J,
-          int(k), _ptr(got.get("logprob")), got["entropy"].data_ptr(), got["stats"].data_ptr(), _ptr(got.get("top_id")),
-          _ptr(got.get("top_logprob")))
+        logprob = (_out1(out, "logprob", R, _F32, dev, index) if tok.dim() == 1 else
+                   _out2(out, "logprob", R, J, _F32, dev, index))
+        got["logprob"] = logprob
+    if k > 0:
+        top_id, top_logprob = _out2(out, "top_id", R, k, _I32, dev, index), _out2(out, "top_logprob", R, k, _F32, dev, index)
+        got["top_id"], got["top_logprob"] = top_id, top_logprob
+    _call(lib().mars_token_logprobs, index, logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, temperature, _ptr(tok), J, k,
+          _ptr(logprob), entropy.data_ptr(), stats.data_ptr(), _ptr(top_id), _ptr(top_logprob))
     return got
 
 
@@ -168,24 +213,22 @@ def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logpr
     """mars_token_logprobs_backward on the current stream: the gradient by `logits` (columns 0 .. V-1, dtype of
     the logits; a new [rows, V] tensor, or `out`, which may be the logits).  `forward` is what token_logprobs
     returned for these logits; grad_logprob has the shape of tok, grad_entropy [rows] or None."""
-    dev = logits.device
-    dt, ld, V = _logits_args(logits, logits.shape[0], V)
-    R = logits.shape[0]
-    tok, J = _tokens(tok, R, dev)
-    g = _dev_f32(grad_logprob, dev)
-    h = None if grad_entropy is None else _dev_f32(grad_entropy, dev)
-    stats, entropy = forward["stats"], forward.get("entropy")
+    dt, R, ld, V, index = _logits(logits, V)
+    tok, J = _tokens(tok, R, logits)
+    g = _dev_f32(grad_logprob, logits.device)
+    h = None if grad_entropy is None else _dev_f32(grad_entropy, logits.device)
+    stats, entropy = _checked(forward["stats"], "forward['stats']", (R, 2), _F32, index), forward.get("entropy")
     if tok is None or g.numel() != R * J or (h is not None and (h.numel() != R or entropy is None)):
         raise MarsError("grad_logprob must have the shape of tok, grad_entropy one value a row")
-    for t, shape in ((stats, (R, 2)), (entropy, (R,))):
-        if t is not None and (tuple(t.shape) != shape or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous()):
-            raise MarsError("forward is not the result of token_logprobs on these logits")
+    if entropy is not None:
+        _checked(entropy, "forward['entropy']", (R,), _F32, index)
     if out is None:
-        out = torch.empty((R, V), dtype=logits.dtype, device=dev)
-    elif out.dim() != 2 or out.shape[0] != R or out.shape[1] < V or out.stride(1) != 1 or out.dtype != logits.dtype or out.device != dev:
-        raise MarsError("out must be [rows, >= V] of the logits' dtype with unit inner stride")
-    _call(lib().mars_token_logprobs_backward, logits.get_device(), logits.data_ptr(), ld, dt, R, V, float(temperature), tok.data_ptr(), J,
-          stats.data_ptr(), _ptr(entropy), g.data_ptr(), _ptr(h), out.data_ptr(), out.stride(0))
+        out = torch.empty_strided((R, V), (V, 1), dtype=logits.dtype, device=logits.device)
+    gdt, rows, ld_grad, width, gi = _logits(out, None)
+    if gdt != dt or rows != R or width < V or gi != index:
+        raise MarsError("out must be [rows, >= V] of the logits' dtype beside them")
+    _call(lib().mars_token_logprobs_backward, index, logits.data_ptr(), ld, dt, R, V, temperature, tok.data_ptr(), J,
+          stats.data_ptr(), _ptr(entropy), g.data_ptr(), _ptr(h), out.data_ptr(), ld_grad)
     return out
 
 
