@@ -37,8 +37,6 @@ namespace cg = cooperative_groups;
 #endif
 
 constexpr int kScMaxSplit = 8;                  // blocks per row = blocks per cluster
-constexpr int kScTargetBlocks = 148 * 4;        // resident blocks of the forward kernel
-constexpr int kScMinSliceBytes = 24 * 1024;     // three quarters of a batch of one block
 constexpr float kLn2 = 0.693147180559945309f;
 
 struct LogprobParams {
@@ -74,23 +72,18 @@ __device__ __forceinline__ float soft_distance(float from, float to, float c)
     return from == to ? 0.0f : fmaxf((from - to) * c, -1000.0f);
 }
 
-__device__ __forceinline__ Soft soft_union(Soft a, Soft b, float c)
+// The union of a warp's 32 sets, in all lanes: everybody moves to the largest reference, then plain sums.
+__device__ __forceinline__ Soft soft_warp(Soft a, float c)
 {
-    const float r = fmaxf(a.ref, b.ref);
+    const float r = tk_dec(__reduce_max_sync(0xffffffffu, tk_enc(a.ref)));
     soft_move(a, soft_distance(a.ref, r, c));
-    soft_move(b, soft_distance(b.ref, r, c));
-    Soft o;
-    o.ref = r; o.sum = a.sum + b.sum; o.dot = a.dot + b.dot;
-    return o;
-}
-
-__device__ __forceinline__ Soft soft_shfl_xor(const Soft &a, int m)
-{
-    Soft o;
-    o.ref = __shfl_xor_sync(0xffffffffu, a.ref, m);
-    o.sum = __shfl_xor_sync(0xffffffffu, a.sum, m);
-    o.dot = __shfl_xor_sync(0xffffffffu, a.dot, m);
-    return o;
+    a.ref = r;
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) {
+        a.sum += __shfl_xor_sync(0xffffffffu, a.sum, m);
+        a.dot += __shfl_xor_sync(0xffffffffu, a.dot, m);
+    }
+    return a;
 }
 
 // The fast form of x: one fma with R = fl(ref c), which gives x + d with d = ref c - R exactly (below 2^-4); a
@@ -245,6 +238,18 @@ __device__ __forceinline__ float batch_maximum(const uint4 (&v)[U])
 // the threads whose maximum does, k of them where values differ: warps read those threads' elements once more (1/256
 // of the slice each), and what reaches the floor, some more than k elements, is ranked.  Order does not matter to it;
 // slices in which very many elements tie at the floor are selected again by topk_slice_exact.
+
+// The k best of n candidates, in order; empty ones (kNoId) lose against every other.
+__device__ __forceinline__ void select_rank(const Cand *from, int n, int k, Cand *list)
+{
+    for (int i = threadIdx.x; i < n; i += kTkThreads) {
+        const Cand c = from[i];
+        int ahead = 0;
+        for (int j = 0; j < n; ++j) ahead += beats(from[j].z, from[j].id, c.z, c.id) ? 1 : 0;
+        if (ahead < k && c.id != kNoId) list[ahead] = c;
+    }
+}
+
 struct TopSelect {
     __align__(8) Cand cand[kTkCap];
     __align__(8) Cand xlist[kTkWarps * kTkMaxK];    // exact fallback only
@@ -261,25 +266,29 @@ struct TopSelect {
         if (at < kTkCap) { cand[at].z = z; cand[at].id = id; }
     }
 
-    // All threads, `best` the thread's maximum; list[0 .. k-1] gets the slice's best, unused entries {-inf, kNoId}.
-    template <int DT>
-    __device__ __forceinline__ void finish(int k, float best, const char *rowp, int lo, int hi, int vlo, int nvec, Cand *list)
+    // A table of each warp's m largest maxima: its k-th largest never exceeds theirs, and falls short of it only
+    // where one warp holds more than m of the block's k largest.  All threads, `best` the thread's maximum; the
+    // caller synchronises before finish().
+    __device__ __forceinline__ void table(int k, float best, Cand *list)
     {
-        typedef Elem<DT> E;
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-        // a table of each warp's m largest maxima: its k-th largest never exceeds theirs, and falls short of it
-        // only where one warp holds more than m of the block's k largest
-        const int m = min(k, 4 + (k >> 2)), nt = kTkWarps * m;
-        const unsigned mine = best > -INFINITY ? tk_enc(best) : 0u;
-        unsigned left = mine;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, m = min(k, 4 + (k >> 2));
+        unsigned left = best > -INFINITY ? tk_enc(best) : 0u;
         for (int i = 0; i < m; ++i) {
             const unsigned most = __reduce_max_sync(0xffffffffu, left);
             const unsigned who = __ballot_sync(0xffffffffu, left == most);
             if (lane == __ffs(who) - 1) { top[warp * m + i] = most; left = 0u; }
         }
         if (tid == 0) { floor = 1u; hits = 0; }
-        if (tid < k) { list[tid].z = -INFINITY; list[tid].id = kNoId; }
-        __syncthreads();
+        if (tid < kTkMaxK) { list[tid].z = -INFINITY; list[tid].id = kNoId; }
+    }
+
+    // All threads, after table(); list gets the slice's best k in order (the caller synchronises).
+    template <int DT>
+    __device__ __forceinline__ void finish(int k, float best, const char *rowp, int lo, int hi, int vlo, int nvec, Cand *list)
+    {
+        typedef Elem<DT> E;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = kTkWarps * min(k, 4 + (k >> 2));
+        const unsigned mine = best > -INFINITY ? tk_enc(best) : 0u;
         for (int i = tid; i < nt; i += kTkThreads) {
             const unsigned t = top[i];
             int ahead = 0;
@@ -308,12 +317,7 @@ struct TopSelect {
             topk_slice_exact<DT>(rowp, lo, hi, k, list, cand, xlist, xqn, &xfloor);
             return;
         }
-        for (int i = tid; i < found; i += kTkThreads) {
-            const Cand c = cand[i];
-            int ahead = 0;
-            for (int j = 0; j < found; ++j) ahead += beats(cand[j].z, cand[j].id, c.z, c.id) ? 1 : 0;
-            if (ahead < k) list[ahead] = c;
-        }
+        select_rank(cand, found, k, list);
     }
 };
 
@@ -339,10 +343,8 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
     __shared__ typename std::conditional<TOP, Select, None>::type s_sel;
     __shared__ Soft s_soft[kTkThreads / 32];
     __shared__ Soft s_block;
-    __shared__ RowScore s_row;
-    __shared__ Cand s_list[TOP ? kTkMaxK : 1];
+    __shared__ Cand s_list[kTkMaxK];
     __shared__ Cand s_all[TOP ? kTkMaxK * kScMaxSplit : 1];
-    __shared__ int s_found;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = p.k;
     const long long out_row = blockIdx.x / p.S;
@@ -424,56 +426,49 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
 #endif
 
     // ---- the block's (m, s, u) and list ----
-    Soft a = soft_free(t);
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) a = soft_union(a, soft_shfl_xor(a, m), c);
+    Soft a = soft_warp(soft_free(t), c);
     if (lane == 0) s_soft[warp] = a;
+    if constexpr (TOP) s_sel.s.table(k, best, s_list);
     __syncthreads();
-    if (warp == 0) {
+    if (warp == kTkWarps - 1) {
         a.ref = -INFINITY; a.sum = 0.0f; a.dot = 0.0f;
-        if (lane < kTkThreads / 32) a = s_soft[lane];
-#pragma unroll
-        for (int m = kTkThreads / 64; m > 0; m >>= 1) a = soft_union(a, soft_shfl_xor(a, m), c);
+        if (lane < kTkWarps) a = s_soft[lane];
+        a = soft_warp(a, c);
         if (lane == 0) s_block = a;
     }
     if constexpr (TOP) s_sel.s.template finish<DT>(k, best, rowp, lo, hi, vlo, nvec, s_list);
 
     // ---- the row's ----
-    int n_all = k;
     if (p.S > 1) {
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         if (rank == 0) {
-            if (warp == 0) {
+            if (warp == kTkWarps - 1) {
                 a.ref = -INFINITY; a.sum = 0.0f; a.dot = 0.0f;
                 if (lane < p.S) a = *cluster.map_shared_rank(&s_block, lane);
-#pragma unroll
-                for (int m = kScMaxSplit / 2; m > 0; m >>= 1) a = soft_union(a, soft_shfl_xor(a, m), c);
+                a = soft_warp(a, c);
                 if (lane == 0) s_block = a;
             }
-            n_all = p.S * k;
             if constexpr (TOP)
-                if (tid < n_all) s_all[tid] = *(cluster.map_shared_rank(s_list, tid / k) + tid % k);
+                if (tid < p.S * k) s_all[tid] = *(cluster.map_shared_rank(s_list, tid / k) + tid % k);
         }
         cluster.sync();          // the other blocks' shared memory was read
         if (rank != 0) return;
-    } else {
-        __syncthreads();
-        if constexpr (TOP) { if (tid < k) s_all[tid] = s_list[tid]; }
-    }
-    if (tid == 0) {
-        const Soft t = s_block;
-        RowScore r;
-        r.m = t.ref;
-        r.ok = fabsf(t.ref) < INFINITY;
-        r.ln_s = logf(t.sum);
-        s_row = r;
-        s_found = 0;
-        if (p.entropy) p.entropy[out_row] = r.ok ? r.ln_s - kLn2 * (t.dot / t.sum) : NAN;
-        if (p.stats) { p.stats[2 * out_row] = t.ref; p.stats[2 * out_row + 1] = r.ok ? t.sum : NAN; }
+        if constexpr (TOP) {
+            if (tid < k) { s_list[tid].z = -INFINITY; s_list[tid].id = kNoId; }
+            __syncthreads();
+            select_rank(s_all, p.S * k, k, s_list);
+        }
     }
     __syncthreads();
-    const RowScore r = s_row;
+    RowScore r;
+    r.m = s_block.ref;
+    r.ok = fabsf(r.m) < INFINITY;
+    r.ln_s = logf(s_block.sum);
+    if (tid == 0) {
+        if (p.entropy) p.entropy[out_row] = r.ok ? r.ln_s - kLn2 * (s_block.dot / s_block.sum) : NAN;
+        if (p.stats) { p.stats[2 * out_row] = r.m; p.stats[2 * out_row + 1] = r.ok ? s_block.sum : NAN; }
+    }
     for (int j = tid; j < p.J; j += kTkThreads) {
         if (j >= kTkThreads) {
             const int t = p.tok[out_row * p.J + j];
@@ -483,26 +478,19 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         p.logprob[out_row * p.J + j] = inside ? row_logprob(r, zt, p.temperature) : 0.0f;
     }
     if constexpr (TOP) {
-        float *ov = p.top_logprob + out_row * k;
-        int32_t *oi = p.top_id + out_row * k;
-        if (tid < n_all) {
-            const Cand mine = s_all[tid];
-            if (mine.id != kNoId) {
-                int ahead = 0;
-                for (int j = 0; j < n_all; ++j) ahead += beats(s_all[j].z, s_all[j].id, mine.z, mine.id) ? 1 : 0;
-                if (ahead < k) {
-                    ov[ahead] = row_logprob(r, mine.z, p.temperature);
-                    oi[ahead] = mine.id;
-                    atomicAdd(&s_found, 1);
-                }
+        if (warp == kTkWarps - 1) {
+            float *ov = p.top_logprob + out_row * k;
+            int32_t *oi = p.top_id + out_row * k;
+            const Cand mine = s_list[lane];              // ordered; entries from `found` on are empty
+            const bool real = lane < k && mine.id != kNoId;
+            if (real) { ov[lane] = row_logprob(r, mine.z, p.temperature); oi[lane] = mine.id; }
+            const int found = __popc(__ballot_sync(0xffffffffu, real));
+            __syncwarp();
+            if (lane == 0 && found < k) {
+                complete_row(ov, oi, found, k);
+                if (!r.ok)
+                    for (int j = found; j < k; ++j) ov[j] = NAN;
             }
-        }
-        __syncthreads();
-        if (tid == 0 && s_found < k) {
-            const int found = s_found;
-            complete_row(ov, oi, found, k);
-            if (!r.ok)
-                for (int j = found; j < k; ++j) ov[j] = NAN;
         }
     }
 }
@@ -648,14 +636,20 @@ __global__ void __launch_bounds__(kTkThreads) logprob_grad_kernel(const GradPara
 
 static bool scores_sizes_ok(int64_t rows, int V) { return rows <= (1ll << 27) && V <= (1 << 30); }
 
-// Blocks per row: as many as fill the GPU, while a slice is worth a block.
+// Blocks per row: rows are split while the GPU is not full.  How full it has to be depends on what is left of a slice,
+// since a block also takes some microseconds whatever its slice.  us split into 1 / 2 / 4 / 8 (bf16): 8 rows of 151936
+// 12.9 / 8.5 / 6.4 / 5.5, 120 rows 21.0 / 19.7 / 18.1 / 24.6, 300 rows 31.5 / 26.5 / 28.6 / 37.3, 700 rows 48.6 / 45.9 /
+// 56.0 / 78.8, 1000 rows 57.5 / 61.6; 200 rows of 32000 7.9 / 8.4 / 10.8 / 17.3.
 static int logprob_split(int64_t rows, int V, int es)
 {
     const int force = hook(kHookForceSplit);
     int S = 1;
-    while (S < kScMaxSplit && (force >= 1 ? 2 * S <= force
-                                          : rows * S * 2 <= kScTargetBlocks && (int64_t)V * es >= (int64_t)2 * S * kScMinSliceBytes))
-        S *= 2;
+    for (; S < kScMaxSplit; S *= 2) {
+        const int64_t blocks = rows * S * 2, slice = (int64_t)V * es / (S * 2);
+        const bool more = force >= 1 ? 2 * S <= force
+                                     : slice >= 24 * 1024 && blocks <= 148 * (slice >= 128 * 1024 ? 8 : slice >= 64 * 1024 ? 4 : 2);
+        if (!more) break;
+    }
     return S;
 }
 
