@@ -24,18 +24,7 @@ namespace mars {
 
 namespace cg = cooperative_groups;
 
-#ifndef LP_DB
-#define LP_DB 0
-#endif
-#ifndef LP_U
-#define LP_U 8
-#define LP_B 4
-#endif
-#ifndef LP_TU
-#define LP_TU 8
-#define LP_TB 4
-#endif
-
+constexpr int kScWarps = kTkThreads / 32;
 constexpr int kScMaxSplit = 8;                  // blocks per row = blocks per cluster
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -252,10 +241,10 @@ __device__ __forceinline__ void select_rank(const Cand *from, int n, int k, Cand
 
 struct TopSelect {
     __align__(8) Cand cand[kTkCap];
-    __align__(8) Cand xlist[kTkWarps * kTkMaxK];    // exact fallback only
-    int xqn[kTkWarps];
+    __align__(8) Cand xlist[kScWarps * kTkMaxK];    // exact fallback only
+    int xqn[kScWarps];
     unsigned xfloor;
-    unsigned top[kTkWarps * kTkMaxK];               // tk_enc of the warps' largest maxima
+    unsigned top[kScWarps * kTkMaxK];               // tk_enc of the warps' largest maxima
     unsigned floor;
     int n, hits;
     int hit[kTkThreads];
@@ -287,7 +276,7 @@ struct TopSelect {
     __device__ __forceinline__ void finish(int k, float best, const char *rowp, int lo, int hi, int vlo, int nvec, Cand *list)
     {
         typedef Elem<DT> E;
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = kTkWarps * min(k, 4 + (k >> 2));
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = kScWarps * min(k, 4 + (k >> 2));
         const unsigned mine = best > -INFINITY ? tk_enc(best) : 0u;
         for (int i = tid; i < nt; i += kTkThreads) {
             const unsigned t = top[i];
@@ -300,7 +289,7 @@ struct TopSelect {
         __syncthreads();
         const uint4 *vbase = (const uint4 *)(rowp + (size_t)vlo * E::kBytes);
         const float f = floor > 1u ? tk_dec(floor) : -INFINITY;
-        for (int h = warp; h < hits; h += kTkWarps) {
+        for (int h = warp; h < hits; h += kScWarps) {
             for (int vi = hit[h] + lane * kTkThreads; vi < nvec; vi += 32 * kTkThreads) {
                 const uint4 v = ld_stream(vbase + vi);
                 if (!(E::to_float(E::vred(v)) >= f)) continue;
@@ -334,10 +323,11 @@ __device__ __forceinline__ float row_logprob(const RowScore &r, float z, float t
 
 // Forward: a cluster of S blocks (S = 1: a block) streams one row, each block a contiguous slice; the
 // block of rank 0 joins the slices' (m, s, u) and lists through distributed shared memory and writes.
-template <int DT, int U, int MINB, bool TOP>
-__global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const LogprobParams p)
+template <int DT, bool TOP>
+__global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobParams p)
 {
     typedef Elem<DT> E;
+    constexpr int U = kTkU;
     struct Select { TopSelect s; };
     struct None {};
     __shared__ typename std::conditional<TOP, Select, None>::type s_sel;
@@ -407,32 +397,19 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         if constexpr (TOP) best = fmaxf(best, bm);
         soft_batch<DT, U>(t, x, bm, c, reach, vbase, bi * kBatchVecs + tid, nvec);
     };
-#if LP_DB
-    uint4 w[U];
-    if (nbatch > 1) load_raw<DT, U>(vbase, 1, nvec, w);
-    // two buffers: a batch is on its way while the one before it is worked on
-    for (int bi = 0; bi < nbatch; bi += 2) {
-        batch(v, bi);
-        if (bi + 1 >= nbatch) break;
-        if (bi + 2 < nbatch) load_raw<DT, U>(vbase, bi + 2, nvec, v);
-        batch(w, bi + 1);
-        if (bi + 3 < nbatch) load_raw<DT, U>(vbase, bi + 3, nvec, w);
-    }
-#else
     for (int bi = 0; bi < nbatch; ++bi) {
         if (bi) load_raw<DT, U>(vbase, bi, nvec, v);
         batch(v, bi);
     }
-#endif
 
     // ---- the block's (m, s, u) and list ----
     Soft a = soft_warp(soft_free(t), c);
     if (lane == 0) s_soft[warp] = a;
     if constexpr (TOP) s_sel.s.table(k, best, s_list);
     __syncthreads();
-    if (warp == kTkWarps - 1) {
+    if (warp == kScWarps - 1) {
         a.ref = -INFINITY; a.sum = 0.0f; a.dot = 0.0f;
-        if (lane < kTkWarps) a = s_soft[lane];
+        if (lane < kScWarps) a = s_soft[lane];
         a = soft_warp(a, c);
         if (lane == 0) s_block = a;
     }
@@ -443,7 +420,7 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         if (rank == 0) {
-            if (warp == kTkWarps - 1) {
+            if (warp == kScWarps - 1) {
                 a.ref = -INFINITY; a.sum = 0.0f; a.dot = 0.0f;
                 if (lane < p.S) a = *cluster.map_shared_rank(&s_block, lane);
                 a = soft_warp(a, c);
@@ -478,7 +455,7 @@ __global__ void __launch_bounds__(kTkThreads, MINB) logprob_kernel(const Logprob
         p.logprob[out_row * p.J + j] = inside ? row_logprob(r, zt, p.temperature) : 0.0f;
     }
     if constexpr (TOP) {
-        if (warp == kTkWarps - 1) {
+        if (warp == kScWarps - 1) {
             float *ov = p.top_logprob + out_row * k;
             int32_t *oi = p.top_id + out_row * k;
             const Cand mine = s_list[lane];              // ordered; entries from `found` on are empty
@@ -506,7 +483,9 @@ struct GradParams {
     const float *stats, *entropy, *g, *h;
 };
 
-constexpr int kGrU = 4;
+// Vectors per thread at a time, blocks per SM.  2048 rows of 151936 (bf16), us: 2 at 6 blocks 205, at 5 209, at 7 216;
+// 4 at 6 blocks 210, at 5 (47 registers) 217; 1 at 6 blocks 234, at 8 224.  Stores that stay in L2 228.
+constexpr int kGrU = 2, kGrBlocks = 6;
 
 template <int DT>
 __device__ __forceinline__ void store_scalar(void *row, int at, float x)
@@ -535,7 +514,7 @@ __device__ __forceinline__ float grad_term(float z, const GradLine &l)
 
 // Backward: a block takes a contiguous piece of one row.
 template <int DT>
-__global__ void __launch_bounds__(kTkThreads) logprob_grad_kernel(const GradParams p)
+__global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(const GradParams p)
 {
     typedef Elem<DT> E;
     __shared__ float s_z[MARS_SCORES_MAX_TOKENS];
@@ -662,7 +641,7 @@ static int slice_columns(int V, int S)
 template <int DT>
 static cudaError_t logprob_launch(const LogprobParams &p, unsigned rows, cudaStream_t st)
 {
-    void (*kernel)(const LogprobParams) = p.k ? logprob_kernel<DT, LP_TU, LP_TB, true> : logprob_kernel<DT, LP_U, LP_B, false>;
+    void (*kernel)(const LogprobParams) = p.k ? logprob_kernel<DT, true> : logprob_kernel<DT, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(rows * (unsigned)p.S); cfg.blockDim = dim3(kTkThreads); cfg.stream = st;
     cudaLaunchAttribute at[2];

@@ -38,12 +38,35 @@ struct TopkParams {
     int32_t *out_id;     // [R, k] final token ids
 };
 
-// Streams one slice with the selection of mars_topk_select.cuh.
+// Slice selection.  A block streams its slice once, like the top-2 kernel (batches of 8 vectors
+// per thread reduced with packed max instructions).  A batch is looked at more closely only if
+// its maximum reaches the floor, a lower bound on the slice's k-th value:
+//   - the floor starts as the k-th largest of the threads' first-batch maxima (values of distinct
+//     elements): every warp orders its lanes' maxima, the k best of each warp go to a small
+//     table, and the table's k-th entry is found by rank counting;
+//   - a thread whose batch reaches the floor appends the elements that do to a queue in shared
+//     memory (one atomicAdd each), nothing more;
+//   - the slice's k best so far live in one ordered list in shared memory.  After appending, a
+//     warp TRIES to take the list (one compare-and-swap, no waiting): if it gets it, it holds
+//     the list in its lanes (lane i = entry i), feeds the queued elements into it one by one (a
+//     ballot and a shuffle each), stores it back and publishes the k-th entry's value as the new
+//     floor; if another warp has it, that warp or a later one will pick the elements up.
+// So nobody ever waits, the floor trails the stream by at most a few elements, about
+// k (1 + ln(batches)) elements reach the queue on unordered data, and the list is the result.
+// If the queue fills up (adversarially ordered rows), the block redoes its slice with
+// topk_slice_exact.
 template <int DT, int U, int MINB>
 __global__ void __launch_bounds__(kTkThreads, MINB) topk_slice_kernel(const TopkParams p)
 {
     typedef Elem<DT> E;
-    __shared__ TopkSelect sel;
+    constexpr int kWarps = kTkThreads / 32;
+    __shared__ __align__(8) Cand s_cand[kTkCap];
+    __shared__ __align__(8) Cand s_list[kTkMaxK];
+    __shared__ __align__(8) Cand s_xlist[kWarps * kTkMaxK];    // exact fallback only
+    __shared__ float s_top[kWarps * kTkMaxK];
+    __shared__ unsigned s_floor;
+    __shared__ int s_tail, s_head, s_lock, s_overflow;
+    __shared__ int s_xqn[kWarps];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = p.k;
     const long long blk = blockIdx.x;
@@ -70,44 +93,158 @@ __global__ void __launch_bounds__(kTkThreads, MINB) topk_slice_kernel(const Topk
     // batch 0: issue its loads first, so that the set-up below overlaps their latency
     float bm = (nfull > 0) ? load_batch<DT, U, false>(vbase, tid, nvec, v, q)
                            : load_batch<DT, U, true>(vbase, tid, nvec, v, q);
-    sel.clear();
+    {   // empty slots carry kNoId so that a reader can tell a reserved slot from a written one
+        Cand e; e.z = -INFINITY; e.id = kNoId;
+        for (int i = tid; i < kTkCap; i += kTkThreads) s_cand[i] = e;
+        if (tid < kTkMaxK) s_list[tid] = e;
+    }
+    if (tid == 0) { s_floor = tk_enc(-INFINITY); s_tail = 0; s_head = 0; s_lock = 0; s_overflow = 0; }
     __syncthreads();
-    if (tid < nhead) { float x = E::scalar(rowp, lo + tid); if (x > -INFINITY) sel.append(x, lo + tid); }
-    if (tid < ntail) { float x = E::scalar(rowp, tlo + tid); if (x > -INFINITY) sel.append(x, tlo + tid); }
-    sel.first_floor(k, bm);
 
-    sel.scan<DT, U>(k, v, q, bm, vlo + tid * E::kVec);
+    auto append = [&](float x, int idx) {
+        const int pos = atomicAdd(&s_tail, 1);
+        if (pos < kTkCap) {
+            Cand e; e.z = x; e.id = idx;     // one 8-byte store: value and id become visible together
+            *reinterpret_cast<volatile unsigned long long *>(&s_cand[pos]) = *reinterpret_cast<unsigned long long *>(&e);
+        } else {
+            s_overflow = 1;
+        }
+    };
+    // Feed the queued elements into the list.  Called by whole warps; `force` skips the
+    // compare-and-swap (used once at the end, when no other warp can be in here).
+    auto drain = [&](bool force) {
+        int got = 1;
+        if (!force) {
+            if (lane == 0) got = atomicCAS(&s_lock, 0, 1) == 0 ? 1 : 0;
+            got = __shfl_sync(0xffffffffu, got, 0);
+        }
+        if (!got) return;
+        __threadfence_block();
+        // one lane reads the queue's bounds for all: the tail moves while other warps append
+        int i = 0, tail = 0;
+        if (lane == 0) { i = *(volatile int *)&s_head; tail = min(*(volatile int *)&s_tail, kTkCap); }
+        i = __shfl_sync(0xffffffffu, i, 0);
+        tail = __shfl_sync(0xffffffffu, tail, 0);
+        unsigned long long raw = *reinterpret_cast<volatile unsigned long long *>(&s_list[lane]);
+        Cand mine = *reinterpret_cast<Cand *>(&raw);
+        // 32 slots at a time, one per lane.  Lanes do not read at the same instant, so what is
+        // "written" is settled by a ballot: every decision below is the same in all lanes.
+        while (i < tail) {
+            Cand c; c.z = -INFINITY; c.id = kNoId;
+            if (i + lane < tail) {
+                raw = *reinterpret_cast<volatile unsigned long long *>(&s_cand[i + lane]);
+                c = *reinterpret_cast<Cand *>(&raw);
+            }
+            const unsigned written = __ballot_sync(0xffffffffu, c.id != kNoId);
+            const int n = written == 0xffffffffu ? 32 : __ffs(~written) - 1;    // leading written slots
+            for (int t = 0; t < n; ++t) {
+                const float cz = __shfl_sync(0xffffffffu, c.z, t);
+                const int cid = __shfl_sync(0xffffffffu, c.id, t);
+                warp_list_insert(mine.z, mine.id, lane, k, cz, cid);
+            }
+            i += n;
+            if (n < 32) break;       // a slot that is reserved but not written yet: a later round takes it
+        }
+        *reinterpret_cast<volatile unsigned long long *>(&s_list[lane]) = *reinterpret_cast<unsigned long long *>(&mine);
+        if (lane == k - 1 && mine.id != kNoId) atomicMax(&s_floor, tk_enc(mine.z));
+        __syncwarp();
+        if (lane == 0) {
+            *(volatile int *)&s_head = i;
+            __threadfence_block();
+            if (!force) atomicExch(&s_lock, 0);
+        }
+    };
+
+    if (tid < nhead) { float x = E::scalar(rowp, lo + tid); if (x > -INFINITY) append(x, lo + tid); }
+    if (tid < ntail) { float x = E::scalar(rowp, tlo + tid); if (x > -INFINITY) append(x, tlo + tid); }
+
+    // First floor: the k-th largest of the threads' first-batch maxima, or a value just below it.
+    // Each warp enters its m = min(k, 4 + k/4) largest maxima, ordered, into a table and the
+    // k-th largest table entry is taken: the table is a subset of the maxima (8 m >= k entries),
+    // so its k-th largest never exceeds theirs, and it falls short of it only when one warp
+    // holds more than m of the block's k largest (k = 32: 12 of 32 in one of 8 warps).
+    {
+        const int m = min(k, 4 + (k >> 2));
+        const float mine = (bm == bm) ? bm : -INFINITY;
+        int wrank = 0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float o = __shfl_sync(0xffffffffu, mine, j);
+            wrank += (o > mine || (o == mine && j < lane)) ? 1 : 0;
+        }
+        if (wrank < m) s_top[warp * m + wrank] = mine;
+        __syncthreads();
+        const int nt = kWarps * m;
+        if (tid < nt) {
+            const float t = s_top[tid];
+            int rank = 0;
+            for (int j = 0; j < nt; ++j) {
+                const float o = s_top[j];
+                rank += (o > t || (o == t && j < tid)) ? 1 : 0;
+            }
+            if (rank == k - 1 && t > -INFINITY) atomicMax(&s_floor, tk_enc(t));
+        }
+        __syncthreads();
+    }
+
+    auto scan = [&](int v0) {
+        const float floor_v = tk_dec(*(volatile unsigned *)&s_floor);
+        bool appended = false;
+        if (bm >= floor_v) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (E::to_float(q[u]) >= floor_v) {
+                    unsigned em = 0;
+#pragma unroll
+                    for (int e = 0; e < E::kVec; ++e) {
+                        const float x = E::elem(v[u], e);
+                        em |= (x >= floor_v && x > -INFINITY) ? (1u << e) : 0u;
+                    }
+                    const int base = vlo + (v0 + u * kTkThreads) * E::kVec;
+                    while (em) {
+                        const int e = __ffs(em) - 1;
+                        em &= em - 1;
+                        append(E::elem(v[u], e), base + e);
+                        appended = true;
+                    }
+                }
+            }
+        }
+        if (__any_sync(0xffffffffu, appended)) drain(false);
+    };
+
+    scan(tid);
     for (int bi = 1; bi < nfull; ++bi) {
         bm = load_batch<DT, U, false>(vbase, bi * kBatchVecs + tid, nvec, v, q);
-        sel.scan<DT, U>(k, v, q, bm, vlo + (bi * kBatchVecs + tid) * E::kVec);
+        scan(bi * kBatchVecs + tid);
     }
     if (nfull > 0 && nfull * kBatchVecs < nvec) {
         bm = load_batch<DT, U, true>(vbase, nfull * kBatchVecs + tid, nvec, v, q);
-        sel.scan<DT, U>(k, v, q, bm, vlo + (nfull * kBatchVecs + tid) * E::kVec);
+        scan(nfull * kBatchVecs + tid);
     }
     __syncthreads();
-    if (sel.overflow) {
+    if (s_overflow) {
         // The queue ran out of room (adversarially ordered data): redo the slice with the exact
         // per-warp lists, which leave the slice's ordered list in the workspace.
         const long long xrow = (long long)blockIdx.x / p.S;
         const int xlo = (int)((long long)blockIdx.x - xrow * p.S) * p.L;
         topk_slice_exact<DT>((const char *)p.logits + (size_t)xrow * (size_t)p.ld * E::kBytes, xlo,
-                             min(p.V, xlo + p.L), p.k, p.partial + (size_t)blockIdx.x * p.k, sel.cand,
-                             sel.xlist, sel.xqn, &sel.floor);
+                             min(p.V, xlo + p.L), p.k, p.partial + (size_t)blockIdx.x * p.k, s_cand,
+                             s_xlist, s_xqn, &s_floor);
         __threadfence_block();
         __syncthreads();
     }
     if (warp == 0) {
         Cand c; c.z = -INFINITY; c.id = kNoId;   // ordered; unused entries are {-inf, kNoId}
-        if (sel.overflow) {
+        if (s_overflow) {
             if (lane < k) c = p.partial[(size_t)blk * k + lane];
         } else {
-            sel.drain(k, true);                  // whatever is still queued
+            drain(true);                         // whatever is still queued
             __syncwarp();
-            c = sel.list[lane];
+            c = s_list[lane];
         }
         if (p.S > 1) {
-            if (!sel.overflow && lane < k) p.partial[(size_t)blk * k + lane] = c;
+            if (!s_overflow && lane < k) p.partial[(size_t)blk * k + lane] = c;
         } else {
             // a whole row: the list is the row's result, write it out here
             float *ov = p.out_val + (size_t)row * k;

@@ -1,5 +1,5 @@
-// Exact top-k (k <= 32) of a slice of a logits row while a block streams it: the selection shared by
-// mars_topk_rows and the calls that report alternatives beside other results of the same pass.
+// Pieces shared by the kernels that select the best k <= 32 of a logits row: candidates, ordered lists held
+// by warps, the exact selection of a slice, and the completion of rows with fewer than k entries above -inf.
 #pragma once
 
 #include "mars_common.cuh"
@@ -10,9 +10,8 @@ namespace mars {
 constexpr int kTkThreads = 256;
 constexpr int kTkU = 8;
 constexpr int kTkMaxK = 32;
-constexpr int kTkWarps = kTkThreads / 32;
-constexpr int kTkCap = kTkThreads * 8;   // slots of the slice's queue of elements at or above the floor
-                                         // (the exact fallback reuses them: one vector step per thread)
+constexpr int kTkCap = kTkThreads * 8;   // slots of a slice's queue of candidates (the exact selection reuses
+                                         // them: one vector step per thread)
 
 struct Cand {
     float z;
@@ -45,7 +44,7 @@ __device__ __forceinline__ void warp_list_insert(float &wz, int &wid, int lane, 
     }
 }
 
-// Exact slice selection with per-warp lists; always correct, used when the streaming kernel below
+// Exact slice selection with per-warp lists; always correct, used when a streaming kernel's queue
 // runs out of room.  Called by all threads of the block.  The caller lends its shared memory:
 //   queue_mem  kTkThreads * 8 candidates (per warp: the candidates of one vector step)
 //   s_list     (kTkThreads / 32) * kTkMaxK candidates (the warps' lists for the final ranking)
@@ -195,163 +194,5 @@ __device__ inline void complete_row(float *ov, int32_t *oi, int found, int k)
         ++next;
     }
 }
-
-// Slice selection.  A block streams its slice once, like the top-2 kernel (batches of 8 vectors
-// per thread reduced with packed max instructions).  A batch is looked at more closely only if
-// its maximum reaches the floor, a lower bound on the slice's k-th value:
-//   - the floor starts as the k-th largest of the threads' first-batch maxima (values of distinct
-//     elements): every warp orders its lanes' maxima, the k best of each warp go to a small
-//     table, and the table's k-th entry is found by rank counting;
-//   - a thread whose batch reaches the floor appends the elements that do to a queue in shared
-//     memory (one atomicAdd each), nothing more;
-//   - the slice's k best so far live in one ordered list in shared memory.  After appending, a
-//     warp TRIES to take the list (one compare-and-swap, no waiting): if it gets it, it holds
-//     the list in its lanes (lane i = entry i), feeds the queued elements into it one by one (a
-//     ballot and a shuffle each), stores it back and publishes the k-th entry's value as the new
-//     floor; if another warp has it, that warp or a later one will pick the elements up.
-// So nobody ever waits, the floor trails the stream by at most a few elements, about
-// k (1 + ln(batches)) elements reach the queue on unordered data, and the list is the result.
-// If the queue fills up (adversarially ordered rows), the block redoes its slice with
-// topk_slice_exact.
-struct TopkSelect {
-    __align__(8) Cand cand[kTkCap];
-    __align__(8) Cand list[kTkMaxK];
-    __align__(8) Cand xlist[kTkWarps * kTkMaxK];    // exact fallback only
-    float top[kTkWarps * kTkMaxK];
-    unsigned floor;
-    int tail, head, lock, overflow;
-    int xqn[kTkWarps];
-
-    // Empty queue and list (all threads; the caller synchronises before the first append).
-    __device__ __forceinline__ void clear()
-    {
-        // empty slots carry kNoId so that a reader can tell a reserved slot from a written one
-        Cand e; e.z = -INFINITY; e.id = kNoId;
-        for (int i = threadIdx.x; i < kTkCap; i += kTkThreads) cand[i] = e;
-        if (threadIdx.x < kTkMaxK) list[threadIdx.x] = e;
-        if (threadIdx.x == 0) { floor = tk_enc(-INFINITY); tail = 0; head = 0; lock = 0; overflow = 0; }
-    }
-
-    __device__ __forceinline__ void append(float x, int idx)
-    {
-        const int pos = atomicAdd(&tail, 1);
-        if (pos < kTkCap) {
-            Cand e; e.z = x; e.id = idx;     // one 8-byte store: value and id become visible together
-            *reinterpret_cast<volatile unsigned long long *>(&cand[pos]) = *reinterpret_cast<unsigned long long *>(&e);
-        } else {
-            overflow = 1;
-        }
-    }
-
-    // Feed the queued elements into the list.  Called by whole warps; `force` skips the
-    // compare-and-swap (used once at the end, when no other warp can be in here).
-    __device__ __forceinline__ void drain(int k, bool force)
-    {
-        const int lane = threadIdx.x & 31;
-        int got = 1;
-        if (!force) {
-            if (lane == 0) got = atomicCAS(&lock, 0, 1) == 0 ? 1 : 0;
-            got = __shfl_sync(0xffffffffu, got, 0);
-        }
-        if (!got) return;
-        __threadfence_block();
-        // one lane reads the queue's bounds for all: the tail moves while other warps append
-        int i = 0, end = 0;
-        if (lane == 0) { i = *(volatile int *)&head; end = min(*(volatile int *)&tail, kTkCap); }
-        i = __shfl_sync(0xffffffffu, i, 0);
-        end = __shfl_sync(0xffffffffu, end, 0);
-        unsigned long long raw = *reinterpret_cast<volatile unsigned long long *>(&list[lane]);
-        Cand mine = *reinterpret_cast<Cand *>(&raw);
-        // 32 slots at a time, one per lane.  Lanes do not read at the same instant, so what is
-        // "written" is settled by a ballot: every decision below is the same in all lanes.
-        while (i < end) {
-            Cand c; c.z = -INFINITY; c.id = kNoId;
-            if (i + lane < end) {
-                raw = *reinterpret_cast<volatile unsigned long long *>(&cand[i + lane]);
-                c = *reinterpret_cast<Cand *>(&raw);
-            }
-            const unsigned written = __ballot_sync(0xffffffffu, c.id != kNoId);
-            const int n = written == 0xffffffffu ? 32 : __ffs(~written) - 1;    // leading written slots
-            for (int t = 0; t < n; ++t) {
-                const float cz = __shfl_sync(0xffffffffu, c.z, t);
-                const int cid = __shfl_sync(0xffffffffu, c.id, t);
-                warp_list_insert(mine.z, mine.id, lane, k, cz, cid);
-            }
-            i += n;
-            if (n < 32) break;       // a slot that is reserved but not written yet: a later round takes it
-        }
-        *reinterpret_cast<volatile unsigned long long *>(&list[lane]) = *reinterpret_cast<unsigned long long *>(&mine);
-        if (lane == k - 1 && mine.id != kNoId) atomicMax(&floor, tk_enc(mine.z));
-        __syncwarp();
-        if (lane == 0) {
-            *(volatile int *)&head = i;
-            __threadfence_block();
-            if (!force) atomicExch(&lock, 0);
-        }
-    }
-
-    // First floor: the k-th largest of the threads' first-batch maxima, or a value just below it.
-    // Each warp enters its m = min(k, 4 + k/4) largest maxima, ordered, into a table and the
-    // k-th largest table entry is taken: the table is a subset of the maxima (8 m >= k entries),
-    // so its k-th largest never exceeds theirs, and it falls short of it only when one warp
-    // holds more than m of the block's k largest (k = 32: 12 of 32 in one of 8 warps).
-    __device__ __forceinline__ void first_floor(int k, float bm)
-    {
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-        const int m = min(k, 4 + (k >> 2));
-        const float mine = (bm == bm) ? bm : -INFINITY;
-        int wrank = 0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float o = __shfl_sync(0xffffffffu, mine, j);
-            wrank += (o > mine || (o == mine && j < lane)) ? 1 : 0;
-        }
-        if (wrank < m) top[warp * m + wrank] = mine;
-        __syncthreads();
-        const int nt = kTkWarps * m;
-        if (tid < nt) {
-            const float t = top[tid];
-            int rank = 0;
-            for (int j = 0; j < nt; ++j) {
-                const float o = top[j];
-                rank += (o > t || (o == t && j < tid)) ? 1 : 0;
-            }
-            if (rank == k - 1 && t > -INFINITY) atomicMax(&floor, tk_enc(t));
-        }
-        __syncthreads();
-    }
-
-    // One batch of the thread (its vectors, their maxima and the batch's): element e of vector u has
-    // the id base0 + u * kTkThreads * kVec + e.
-    template <int DT, int U>
-    __device__ __forceinline__ void scan(int k, const uint4 (&v)[U], const typename Elem<DT>::packed_t (&q)[U],
-                                         float bm, int base0)
-    {
-        typedef Elem<DT> E;
-        const float floor_v = tk_dec(*(volatile unsigned *)&floor);
-        bool appended = false;
-        if (bm >= floor_v) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (E::to_float(q[u]) >= floor_v) {
-                    unsigned em = 0;
-#pragma unroll
-                    for (int e = 0; e < E::kVec; ++e) {
-                        const float x = E::elem(v[u], e);
-                        em |= (x >= floor_v && x > -INFINITY) ? (1u << e) : 0u;
-                    }
-                    const int base = base0 + u * kTkThreads * E::kVec;
-                    while (em) {
-                        const int e = __ffs(em) - 1;
-                        em &= em - 1;
-                        append(E::elem(v[u], e), base + e);
-                        appended = true;
-                    }
-                }
-            }
-        }
-        if (__any_sync(0xffffffffu, appended)) drain(k, false);
-    }
-};
 
 }  // namespace mars
