@@ -544,7 +544,8 @@ mars_status_t mars_device_check(int *sm_count, int *sm_tuned);
  * Process-wide, takes effect from the next call, also changes the matching *_workspace_bytes
  * results.  The library never reads the environment: unless this function is called, behaviour
  * depends on the arguments of each call alone.
- *   which 0: slices per logits row (mars_verify_*, mars_top2_shard, mars_topk_rows, stochastic calls)
+ *   which 0: slices per logits row (mars_verify_*, mars_top2_shard, mars_topk_rows, stochastic calls; mars_token_logprobs:
+ *            the largest power of two up to it and to 8)
  *         1: value 1 selects the single-block MMA kernel of mars_lmhead_verify / _top2_shard
  *         2: blocks per cluster of the stochastic tail kernel (1, 2, 4 or 8)
  *         3: value 1 launches every kernel in plain stream order (no programmatic overlap of

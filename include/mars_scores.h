@@ -49,8 +49,8 @@ mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t row
  *   out      `dt` (MARS_BF16 or MARS_FP32) [M, ldo], any alignment; columns 0 .. V-1 are written.
  *   flags    MARS_COUNTERS_ZERO: the caller vouches that `workspace` was zeroed once and used by completed
  *            calls of this function only since; otherwise the call clears its counters.
- *   workspace  mars_project_int8_workspace_bytes() bytes (0 for unsupported sizes), 256-byte aligned; two
- *            calls that may overlap on the GPU need separate workspaces.
+ *   workspace  mars_project_int8_workspace_bytes() bytes (0 for unsupported sizes; never less for a larger M,
+ *            whatever V and K), 256-byte aligned; two calls that may overlap on the GPU need separate ones.
  *   The first call on a device sets function attributes: make it outside any stream capture.
  *   If a bounded device-side wait gives up (a fault in the pipeline, not a property of the data), logits
  *   that were not computed are NaN and the first uint32 of the workspace is MARS_SEQ_TIMEOUT; it is 0

@@ -25,6 +25,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <mutex>
 
 #include "mars_scores.h"
@@ -148,7 +149,6 @@ constexpr int kPjThreads = 64 + 32 * kPjWarps;
 constexpr int kPjMaxStages = 10;
 constexpr int kPjPairs = 74;                // pairs of blocks that fill a B200
 constexpr int kPjHolders = 4;               // parts that a cut tile goes to (or one more)
-constexpr int kPjFewTokens = 64;
 constexpr uint32_t kPjABytes = kPjRows * kPjBK;
 constexpr uint32_t kPjTmemCols = 512;
 constexpr size_t kPjRing = 200 * 1024;
@@ -457,11 +457,51 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
 }
 
-// Tiles of equal width, as many as 256 tokens each need.
-static int project_tile_tokens(int64_t M)
+// How a product is cut up.  `tokens` per tile; `rounds` whole tiles for each of `pairs`; the remaining tiles are dealt in
+// shares of `per` K blocks, which may end inside a tile, or (per = kblocks) as whole tiles to the first pairs.
+struct ProjectPlan {
+    int tokens, rounds, pairs;
+    long long per;
+};
+
+static int project_widest(int64_t M) { return M < kPjMaxTokens ? (int)((M + 31) / 32 * 32) : kPjMaxTokens; }
+
+// The plan of least time by this estimate, in us: a K block of a tile takes what its bytes take from L2, 43 a clock and
+// SM (measured: 0.43 us at 256 tokens, 0.35 at 192, 12 TB/s in all; the MMA's own 2 clocks a token lie below), the whole
+// no less than the weights take from HBM; a tile's epilogue 1 us and 1 us for 64 tokens; a cut tile 2 us and 1 us for 24
+// tokens more, for the sums that its holders exchange.  Narrower tiles than the widest are tried where tiles are few.
+static ProjectPlan project_plan(int64_t M, int V, int K, int pairs)
 {
-    const int64_t tiles = (M + kPjMaxTokens - 1) / kPjMaxTokens;
-    return (int)(((M + tiles - 1) / tiles + 31) / 32 * 32);
+    const int kb = (K + kPjBK - 1) / kPjBK;
+    const int64_t rows = (V + 2 * kPjRows - 1) / (2 * kPjRows), fewest = (M + kPjMaxTokens - 1) / kPjMaxTokens;
+    const int64_t most = rows * fewest >= 4 * pairs ? fewest : (M + 31) / 32 < 8 * fewest ? (M + 31) / 32 : 8 * fewest;
+    const double hbm = (double)V * K / 6.3e6;
+    ProjectPlan best = {};
+    double least = 0;
+    for (int64_t t = fewest; t <= most; ++t) {
+        const int n = (int)(((M + t - 1) / t + 31) / 32 * 32), used = M < n ? (int)M : n;
+        const int64_t tiles = rows * ((M + n - 1) / n);
+        const double unit = fmax(2.0 * n, (kPjABytes + 64.0 * n) / 43) / 1900, edge = 1 + n / 64.0, join = 2 + used / 24.0;
+        for (int how = 0; how < 3; ++how) {
+            // 0: whole tiles only; 1: the rest of the tiles cut; 2: one contiguous range of all tiles for each pair, which
+            // streams the weights fastest where nobody shares them
+            if (how == 2 && t > 1) continue;
+            ProjectPlan p;
+            p.tokens = n;
+            p.rounds = how == 2 ? 0 : (int)(tiles / pairs);
+            const int64_t rest = tiles - (int64_t)p.rounds * pairs, units = rest * kb;
+            if (how == 1 && rest == 0) continue;
+            p.per = how == 0 ? kb : (units + pairs - 1) / pairs;
+            if (p.per < (kb + kPjHolders - 1) / kPjHolders) p.per = (kb + kPjHolders - 1) / kPjHolders;
+            p.pairs = p.rounds ? pairs : (int)((units + p.per - 1) / p.per);
+            const double work = ((double)p.rounds * kb + (rest ? (double)p.per : 0)) * unit;
+            // in the last, ragged round few pairs pull
+            const double stream = how == 2 ? hbm : hbm * p.rounds * pairs / tiles + (rest ? p.per * 0.2 : 0);
+            const double us = fmax(work, stream) + edge + (how == 0 ? 0 : join);
+            if (least == 0 || us < least) { least = us; best = p; }
+        }
+    }
+    return best;
 }
 
 static bool project_supported(int64_t M, int64_t V, int64_t K)
@@ -524,7 +564,7 @@ mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t row
 size_t mars_project_int8_workspace_bytes(int64_t M, int V, int K)
 {
     if (!mars::project_supported(M, V, K)) return 0;
-    return mars::kPjHead + (size_t)mars::kPjPairs * 2 * mars::project_tile_tokens(M) * (2 * mars::kPjRows) * sizeof(int);
+    return mars::kPjHead + (size_t)mars::kPjPairs * 2 * mars::project_widest(M) * (2 * mars::kPjRows) * sizeof(int);
 }
 
 mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scale, const void *wq, int64_t ldw,
@@ -543,9 +583,14 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
     ProjectParams p;
     p.M = (int)M; p.V = V;
     p.kblocks = (K + kPjBK - 1) / kPjBK;
-    p.tokens = project_tile_tokens(M);
+    const int resident = project_pairs();
+    if (resident < 1) return MARS_ERR_CUDA;
+    const ProjectPlan plan = project_plan(M, V, K, resident);
+    p.tokens = plan.tokens;
     p.n_ttiles = (int)((M + p.tokens - 1) / p.tokens);
     p.n_tiles = p.n_ttiles * ((V + 2 * kPjRows - 1) / (2 * kPjRows));
+    p.rounds = plan.rounds;
+    p.per = plan.per;
     const size_t stage = kPjABytes + (size_t)(p.tokens / 2) * kPjBK;
     p.stages = (int)(kPjRing / stage < (size_t)kPjMaxStages ? kPjRing / stage : kPjMaxStages);
     p.xs = x_scale; p.ws = w_scale; p.bias = bias; p.out = out; p.ldo = ldo;
@@ -557,23 +602,11 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
     if (!tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, wq, (uint64_t)V, (uint64_t)K, (uint64_t)ldw, kPjRows, kPjBK) ||
         !tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, xq, (uint64_t)M, (uint64_t)K, (uint64_t)ldx, (uint32_t)p.tokens / 2, kPjBK))
         return MARS_ERR_CUDA;
-    int pairs = project_pairs();
-    if (pairs < 1) return MARS_ERR_CUDA;
-    // Few tokens: every weight tile is read once whoever takes it, the sums of a cut tile are small, and one
-    // contiguous range of the weights for each pair streams faster than tiles dealt round by round.
-    p.rounds = p.n_ttiles == 1 && p.tokens <= kPjFewTokens ? 0 : p.n_tiles / pairs;
-    const int n_cut = p.n_tiles - p.rounds * pairs;
-    const long long cut = (long long)n_cut * p.kblocks;
-    // Even shares, but a tile goes to a few pairs only: each of them writes its sums, and one reads all.
-    p.per = (cut + pairs - 1) / pairs;
-    const int least = (p.kblocks + kPjHolders - 1) / kPjHolders;
-    if (p.per < least) p.per = least;
-    if (p.rounds == 0) pairs = (int)((cut + p.per - 1) / p.per);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kPjHead, st) != cudaSuccess) return MARS_ERR_CUDA;
     void (*kernel)(const CUtensorMap, const CUtensorMap, const ProjectParams) =
         dt == MARS_BF16 ? project_kernel<MARS_BF16> : project_kernel<MARS_FP32>;
-    const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, kernel, dim3(2 * pairs), dim3(kPjThreads), kPjSmemBytes, st,
+    const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, kernel, dim3(2 * plan.pairs), dim3(kPjThreads), kPjSmemBytes, st,
                                      map_w, map_x, p);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     return MARS_OK;

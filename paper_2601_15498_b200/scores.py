@@ -139,8 +139,8 @@ def quantize_rows(x: torch.Tensor, out=None):
 
 
 def project_workspace(tokens: int, V: int, K: int, device) -> torch.Tensor:
-    """A zeroed workspace for project_int8 calls of up to so many tokens, V and K of any size; it serves any
-    number of calls that do not overlap."""
+    """A zeroed workspace for project_int8 calls of up to so many tokens (V and K do not matter to its size); it
+    serves any number of calls that do not overlap."""
     need = int(lib().mars_project_int8_workspace_bytes(tokens, V, K))
     if need == 0:
         raise MarsError("unsupported sizes")
@@ -203,7 +203,7 @@ def token_logprobs(logits: torch.Tensor, tok=None, temperature: float = 1.0, k: 
     if k > 0:
         top_id, top_logprob = _out2(out, "top_id", R, k, _I32, dev, index), _out2(out, "top_logprob", R, k, _F32, dev, index)
         got["top_id"], got["top_logprob"] = top_id, top_logprob
-    _call(lib().mars_token_logprobs, index, logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, temperature, _ptr(tok), J, k,
+    _call(lib().mars_token_logprobs, index, logits.data_ptr(), ld, dt, n, _ptr(rows), R, V, float(temperature), _ptr(tok), J, int(k),
           _ptr(logprob), entropy.data_ptr(), stats.data_ptr(), _ptr(top_id), _ptr(top_logprob))
     return got
 
@@ -227,7 +227,7 @@ def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logpr
     gdt, rows, ld_grad, width, gi = _logits(out, None)
     if gdt != dt or rows != R or width < V or gi != index:
         raise MarsError("out must be [rows, >= V] of the logits' dtype beside them")
-    _call(lib().mars_token_logprobs_backward, index, logits.data_ptr(), ld, dt, R, V, temperature, tok.data_ptr(), J,
+    _call(lib().mars_token_logprobs_backward, index, logits.data_ptr(), ld, dt, R, V, float(temperature), tok.data_ptr(), J,
           stats.data_ptr(), _ptr(entropy), g.data_ptr(), _ptr(h), out.data_ptr(), ld_grad)
     return out
 
@@ -254,14 +254,23 @@ def logprobs(logits: torch.Tensor, tok, temperature: float = 1.0):
     return _Logprobs.apply(logits, _dev_i32(tok, logits.device), float(temperature))
 
 
-def emitted_logprobs(logits: torch.Tensor, verified: dict, temperature: float = 1.0, k: int = 0, V: int | None = None) -> dict:
-    """token_logprobs of the tokens that a tree verification emitted, from its logits [B*N, ld] and its result:
-    out_tokens[b, i] was judged by, or drawn from, the row of node path_nodes[b, i].  Results are
-    [B, Dcap + 1] (and [B, Dcap + 1, k]); places behind a sequence's out_len hold no token."""
-    path, tok = verified["path_nodes"], verified["out_tokens"]
-    B, W = path.shape
+def emitted_logprobs(logits: torch.Tensor, verified: dict, temperature: float = 1.0, k: int = 0, V: int | None = None,
+                     chain: bool = False) -> dict:
+    """token_logprobs of the tokens that a verification emitted, from its logits [B*N, ld] and its result:
+    out_tokens[b, i] was judged by, or drawn from, the row of node path_nodes[b, i] (with `chain`, for the
+    results of the chain calls, which have no path: of row i).  Results are [B, W] (and [B, W, k]) for
+    out_tokens [B, W]; places behind a sequence's out_len hold no token."""
+    tok = verified["out_tokens"]
+    B, W = tok.shape
     if logits.shape[0] % B:
         raise MarsError("logits must hold N rows for each sequence of the verification")
-    first = torch.arange(0, logits.shape[0], logits.shape[0] // B, device=path.device, dtype=torch.int32)[:, None]
-    got = token_logprobs(logits, tok.reshape(-1), temperature, k, rows=torch.where(path < 0, -1, path + first).view(-1), V=V)
+    N = logits.shape[0] // B
+    first = torch.arange(0, B * N, N, device=tok.device, dtype=_I32)[:, None]
+    if chain:
+        node = torch.arange(W, device=tok.device, dtype=_I32)[None]
+        rows = torch.where(node < verified["out_len"][:, None], node + first, -1)
+    else:
+        path = verified["path_nodes"]
+        rows = torch.where(path < 0, -1, path + first)
+    got = token_logprobs(logits, tok.reshape(-1), temperature, k, rows=rows.view(-1), V=V)
     return {name: t.view(B, W, *t.shape[1:]) for name, t in got.items()}

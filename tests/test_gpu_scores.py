@@ -287,6 +287,30 @@ def test_emitted_tokens_of_a_verified_batch():
     assert torch.isfinite(again["logprob"]).all() and (again["logprob"] <= 0).all()
 
 
+def test_emitted_tokens_of_verified_chains():
+    w = synth.cfg2(DEV, B=6)
+    B, K = w.draft.shape[0], w.draft.shape[1] + 1
+    out = mars.verify_chain(w.logits, w.draft, w.theta)
+    got = scores.emitted_logprobs(w.logits, out, chain=True)
+    ref = sc.reference(w.logits)["logp"].view(B, K, -1)
+    tok, n = out["out_tokens"].long(), out["out_len"]
+    live = torch.arange(K, device=DEV)[None] < n[:, None]
+    want = torch.where(live, ref.gather(2, tok.clamp(min=0)[:, :, None])[:, :, 0], 0.0)
+    assert (got["logprob"].double() - want).abs().max() <= 1e-4 and int(n.max()) > 1
+    assert (got["stats"][:, :, 1][~live] == 0).all()
+
+
+def test_numbers_of_other_kinds_as_arguments():
+    z, tok = rows_of(3, 500, FP32, 1), tokens(3, 2, 500, 1)
+    a = scores.token_logprobs(z, tok, temperature=np.float32(2), k=np.int64(3))
+    b = scores.token_logprobs(z, tok.cpu().long().numpy(), temperature=torch.tensor(2.0), k=3)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    c = scores.token_logprobs(z[:, :400], tok % 400, V=300)
+    sc.check_forward(z[:, :300], c, tok % 400, 1.0, 0)
+    one = scores.token_logprobs(z[:1], tok[:1, :0])
+    assert one["logprob"].shape == (1, 0) and torch.isfinite(one["entropy"]).all()
+
+
 def test_refusals_of_the_binding():
     z = torch.zeros((4, 100), device=DEV)
     tok = torch.zeros((4, 2), dtype=torch.int32, device=DEV)
