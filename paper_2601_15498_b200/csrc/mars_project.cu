@@ -70,17 +70,20 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 
 __device__ __forceinline__ int quantise(float x, float r) { return __float2int_rn(x * r); }
 
-// One block per row.
-template <int DT>
-__global__ void __launch_bounds__(kQzThreads) quantize_rows_kernel(const void *x, long long ldx, int K, int8_t *q,
+// kGroup threads (a warp or the block) per row: one pass for the largest magnitude, one for the codes, the first
+// kQzKeep vectors of a thread read once.  Bound by memory: 3840 rows of 4096 (bf16) 10 us, 4.7 TB/s; 20000 rows of 512
+// 26.6 us by blocks, 8.0 us by warps.
+template <int DT, int kGroup>
+__global__ void __launch_bounds__(kQzThreads) quantize_rows_kernel(const void *x, long long ldx, long long rows, int K, int8_t *q,
                                                                    long long ldq, float *scale)
 {
     typedef QzElem<DT> E;
     __shared__ uint32_t s_max[kQzThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
-    const int tid = threadIdx.x;
-    const long long row = blockIdx.x;
+    const int tid = threadIdx.x % kGroup;
+    const long long row = (long long)blockIdx.x * (kQzThreads / kGroup) + threadIdx.x / kGroup;
+    if (row >= rows) return;             // the same for a whole group
     const typename E::raw_t *src = (const typename E::raw_t *)x + row * ldx;
     int8_t *dst = q + row * ldq;
     const bool wide = ((uintptr_t)src & 15) == 0;        // the codes' rows always are 16-byte aligned
@@ -91,24 +94,26 @@ __global__ void __launch_bounds__(kQzThreads) quantize_rows_kernel(const void *x
     int n = 0;
 #pragma unroll
     for (int u = 0; u < kQzKeep; ++u)
-        if (tid + u * kQzThreads < nvec) keep[u].v = vsrc[tid + u * kQzThreads];
+        if (tid + u * kGroup < nvec) keep[u].v = vsrc[tid + u * kGroup];
 #pragma unroll
     for (int u = 0; u < kQzKeep; ++u)
-        if (tid + u * kQzThreads < nvec)
+        if (tid + u * kGroup < nvec)
 #pragma unroll
             for (int e = 0; e < E::kVec; ++e) m = max(m, magnitude(E::value(keep[u].e[e])));
-    for (n = tid + kQzKeep * kQzThreads; n < nvec; n += kQzThreads) {
+    for (n = tid + kQzKeep * kGroup; n < nvec; n += kGroup) {
         QzVec<DT> t;
         t.v = vsrc[n];
 #pragma unroll
         for (int e = 0; e < E::kVec; ++e) m = max(m, magnitude(E::value(t.e[e])));
     }
-    for (int i = nvec * E::kVec + tid; i < K; i += kQzThreads) m = max(m, magnitude(E::value(src[i])));
+    for (int i = nvec * E::kVec + tid; i < K; i += kGroup) m = max(m, magnitude(E::value(src[i])));
     m = __reduce_max_sync(0xffffffffu, m);
-    if ((tid & 31) == 0) s_max[tid >> 5] = m;
-    __syncthreads();
+    if constexpr (kGroup > 32) {
+        if ((tid & 31) == 0) s_max[tid >> 5] = m;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kQzThreads / 32; ++w) m = max(m, s_max[w]);
+        for (int w = 0; w < kQzThreads / 32; ++w) m = max(m, s_max[w]);
+    }
     const float a = __uint_as_float(m);
     const bool zero = a < kQzLeast, bad = !(a < INFINITY);
     const float r = zero || bad ? 0.0f : 127.0f * __frcp_rn(a);
@@ -128,13 +133,13 @@ __global__ void __launch_bounds__(kQzThreads) quantize_rows_kernel(const void *x
     };
 #pragma unroll
     for (int u = 0; u < kQzKeep; ++u)
-        if (tid + u * kQzThreads < nvec) put(tid + u * kQzThreads, keep[u]);
-    for (n = tid + kQzKeep * kQzThreads; n < nvec; n += kQzThreads) {
+        if (tid + u * kGroup < nvec) put(tid + u * kGroup, keep[u]);
+    for (n = tid + kQzKeep * kGroup; n < nvec; n += kGroup) {
         QzVec<DT> t;
         t.v = vsrc[n];
         put(n, t);
     }
-    for (int i = nvec * E::kVec + tid; i < K; i += kQzThreads) dst[i] = (int8_t)code(E::value(src[i]));
+    for (int i = nvec * E::kVec + tid; i < K; i += kGroup) dst[i] = (int8_t)code(E::value(src[i]));
 }
 
 // ------------------------------------------------------------------------------ product
@@ -552,11 +557,15 @@ mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t row
     if ((uintptr_t)x % (dt == MARS_FP32 ? 4 : 2)) return MARS_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool overlap = hook(kHookNoOverlap) == 0;
-    void (*kernel)(const void *, long long, int, int8_t *, long long, float *) =
-        dt == MARS_BF16 ? quantize_rows_kernel<MARS_BF16> : dt == MARS_FP32 ? quantize_rows_kernel<MARS_FP32>
-                                                                            : quantize_rows_kernel<kPjFp16>;
-    const cudaError_t e = launch_pdl(overlap, kernel, dim3((unsigned)rows), dim3(kQzThreads), 0, st, x, (long long)ldx, K,
-                                     (int8_t *)q, (long long)ldq, scale);
+    // a warp holds rows of up to 32 * kQzKeep vectors in registers; longer ones get a block
+    const bool warps = (int64_t)K * (dt == MARS_FP32 ? 4 : 2) <= 32 * kQzKeep * 16;
+    void (*kernel)(const void *, long long, long long, int, int8_t *, long long, float *) =
+        dt == MARS_BF16   ? (warps ? quantize_rows_kernel<MARS_BF16, 32> : quantize_rows_kernel<MARS_BF16, kQzThreads>)
+        : dt == MARS_FP32 ? (warps ? quantize_rows_kernel<MARS_FP32, 32> : quantize_rows_kernel<MARS_FP32, kQzThreads>)
+                          : (warps ? quantize_rows_kernel<kPjFp16, 32> : quantize_rows_kernel<kPjFp16, kQzThreads>);
+    const int64_t blocks = warps ? (rows + kQzThreads / 32 - 1) / (kQzThreads / 32) : rows;
+    const cudaError_t e = launch_pdl(overlap, kernel, dim3((unsigned)blocks), dim3(kQzThreads), 0, st, x, (long long)ldx,
+                                     (long long)rows, K, (int8_t *)q, (long long)ldq, scale);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     return MARS_OK;
 }
