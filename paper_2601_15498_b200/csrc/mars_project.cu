@@ -158,7 +158,7 @@ constexpr uint32_t kPjABytes = kPjRows * kPjBK;
 constexpr uint32_t kPjTmemCols = 512;
 constexpr size_t kPjRing = 200 * 1024;
 constexpr size_t kPjSmemBytes = kPjRing + 1024 /*align*/ + 256 /*barriers*/;
-constexpr size_t kPjHead = 16384;           // workspace: status word, then a counter per (pair, block, warp)
+constexpr size_t kPjHead = MARS_PROJECT_COUNTER_BYTES;   // workspace: status word, then a counter per (pair, block, warp)
 
 struct ProjectParams {
     int M, V, kblocks;
@@ -487,22 +487,19 @@ static ProjectPlan project_plan(int64_t M, int V, int K, int pairs)
         const int n = (int)(((M + t - 1) / t + 31) / 32 * 32), used = M < n ? (int)M : n;
         const int64_t tiles = rows * ((M + n - 1) / n);
         const double unit = fmax(2.0 * n, (kPjABytes + 64.0 * n) / 43) / 1900, edge = 1 + n / 64.0, join = 2 + used / 24.0;
-        for (int how = 0; how < 3; ++how) {
-            // 0: whole tiles only; 1: the rest of the tiles cut; 2: one contiguous range of all tiles for each pair, which
-            // streams the weights fastest where nobody shares them
-            if (how == 2 && t > 1) continue;
+        for (int cut = 0; cut < 2; ++cut) {
             ProjectPlan p;
             p.tokens = n;
-            p.rounds = how == 2 ? 0 : (int)(tiles / pairs);
+            p.rounds = (int)(tiles / pairs);
             const int64_t rest = tiles - (int64_t)p.rounds * pairs, units = rest * kb;
-            if (how == 1 && rest == 0) continue;
-            p.per = how == 0 ? kb : (units + pairs - 1) / pairs;
+            if (cut && rest == 0) continue;
+            p.per = cut ? (units + pairs - 1) / pairs : kb;
             if (p.per < (kb + kPjHolders - 1) / kPjHolders) p.per = (kb + kPjHolders - 1) / kPjHolders;
             p.pairs = p.rounds ? pairs : (int)((units + p.per - 1) / p.per);
             const double work = ((double)p.rounds * kb + (rest ? (double)p.per : 0)) * unit;
             // in the last, ragged round few pairs pull
-            const double stream = how == 2 ? hbm : hbm * p.rounds * pairs / tiles + (rest ? p.per * 0.2 : 0);
-            const double us = fmax(work, stream) + edge + (how == 0 ? 0 : join);
+            const double stream = hbm * p.rounds * pairs / tiles + (rest ? p.per * 0.2 : 0);
+            const double us = fmax(work, stream) + edge + (cut ? join : 0);
             if (least == 0 || us < least) { least = us; best = p; }
         }
     }

@@ -27,6 +27,7 @@ from . import mars
 from .mars import MarsError, _check, _dev_f32, _dev_i32, lib
 
 MAX_TOKENS, MAX_TOP = 1024, 32
+PROJECT_COUNTER_BYTES = 16384
 
 _LOGIT_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32}
 _ROW_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: 2}
@@ -139,12 +140,14 @@ def quantize_rows(x: torch.Tensor, out=None):
 
 
 def project_workspace(tokens: int, V: int, K: int, device) -> torch.Tensor:
-    """A zeroed workspace for project_int8 calls of up to so many tokens (V and K do not matter to its size); it
-    serves any number of calls that do not overlap."""
+    """A workspace for project_int8 calls of up to so many tokens (V and K do not matter to its size), its counters
+    zeroed; it serves any number of calls that do not overlap."""
     need = int(lib().mars_project_int8_workspace_bytes(tokens, V, K))
     if need == 0:
         raise MarsError("unsupported sizes")
-    return torch.zeros((need,), dtype=torch.uint8, device=device)
+    work = torch.empty((need,), dtype=torch.uint8, device=device)
+    work[:PROJECT_COUNTER_BYTES].zero_()
+    return work
 
 
 def project_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias=None,
