@@ -554,6 +554,7 @@ mars_status_t mars_device_check(int *sm_count, int *sm_tuned);
  *            batch and 6 blocks per SM, whatever the size
  *         6: mars_tree_attention with more than 32 query rows per KV head: blocks from number value - 1
  *            on give up at their first wait
+ *         7: mars_project_int8: pairs of blocks from number value - 1 on give up before their first product
  *   value 0 clears the hook.  Returns the previous value, or -1 for an unknown hook / negative value.
  */
 int mars_test_hook(int which, int value);

@@ -25,6 +25,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <climits>
 #include <cmath>
 #include <mutex>
 
@@ -173,6 +174,7 @@ struct ProjectParams {
     unsigned *status, *counters;
     int *partial;               // [pair][2][tokens][2 * kPjRows]
     int packed;                 // bf16 logits may be written two at a time
+    int give_up;                // pairs from this one on give up (test hook; the status is then cleared by the host)
 };
 
 // A pair's work: its part of the cut tiles first, so that what their holders wait for one another lies under
@@ -304,12 +306,16 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     const uint32_t tmem_base = s_tmem_base;
     volatile int *abort_flag = &s_abort;
     pdl_wait();                    // the set-up above lies under the predecessor's end
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;      // (a wait gives up after a second at the earliest)
+    const bool sound = walk.pair < p.give_up;
+    if (threadIdx.x == 0) {
+        if (blockIdx.x == 0 && p.give_up == INT_MAX) *p.status = 0;      // (a wait gives up after a second at the earliest)
+        if (!sound) atomicExch(p.status, (unsigned)MARS_SEQ_TIMEOUT);
+    }
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t stage = 0, phase = 0;
-            bool ok = true;
+            bool ok = sound;
             while (ok && project_next(p, walk, s)) {
                 const int w_row = (s.tile / p.n_ttiles) * 2 * kPjRows + (int)rank * kPjRows;
                 const int x_row = (s.tile % p.n_ttiles) * p.tokens + (int)rank * (p.tokens / 2);
@@ -334,7 +340,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(p.tokens >> 3) << 17) |
                                    ((uint32_t)((2 * kPjRows) >> 4) << 24);
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-            bool ok = true;
+            bool ok = sound;
             while (ok && project_next(p, walk, s)) {
                 if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
@@ -364,7 +370,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const long long slot = (long long)p.tokens * 2 * kPjRows;
         float *xs = s_xs[mine];
         uint32_t acc = 0, acc_phase = 0;
-        bool ok = true;
+        bool ok = sound;
         while (project_next(p, walk, s)) {
             const int v = (s.tile / p.n_ttiles) * 2 * kPjRows + in_tile;
             const int tok0 = (s.tile % p.n_ttiles) * p.tokens, n = min(p.tokens, p.M - tok0);
@@ -608,7 +614,10 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
     if (!tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, wq, (uint64_t)V, (uint64_t)K, (uint64_t)ldw, kPjRows, kPjBK) ||
         !tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, xq, (uint64_t)M, (uint64_t)K, (uint64_t)ldx, (uint32_t)p.tokens / 2, kPjBK))
         return MARS_ERR_CUDA;
+    const int give_up = hook(kHookProjectGiveUp);
+    p.give_up = give_up ? give_up - 1 : INT_MAX;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (give_up && cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return MARS_ERR_CUDA;
     if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kPjHead, st) != cudaSuccess) return MARS_ERR_CUDA;
     void (*kernel)(const CUtensorMap, const CUtensorMap, const ProjectParams) =
         dt == MARS_BF16 ? project_kernel<MARS_BF16> : project_kernel<MARS_FP32>;

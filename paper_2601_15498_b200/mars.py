@@ -144,7 +144,7 @@ def lib() -> ctypes.CDLL:
 
 
 HOOK_FORCE_SPLIT, HOOK_LMHEAD_SINGLE_BLOCK, HOOK_STOCH_TAIL_CLUSTER, HOOK_NO_OVERLAP, HOOK_TOPK_VARIANT = 0, 1, 2, 3, 4
-HOOK_ATTENTION_GIVE_UP = 6
+HOOK_ATTENTION_GIVE_UP, HOOK_PROJECT_GIVE_UP = 6, 7
 
 
 def test_hook(which: int, value: int) -> int:

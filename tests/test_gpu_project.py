@@ -179,6 +179,32 @@ def test_hidden_states_to_verified_tokens_and_their_log_probabilities():
     sc.check_grad(logits, z.grad, ref, logits.argmax(1)[:, None].int(), torch.ones((B * N, 1), device=DEV), None, 1.0)
 
 
+@pytest.mark.parametrize("M,V,K", [(40, 900, 6000), (300, 25000, 512)])
+def test_pairs_that_give_up_leave_nan_and_a_status(M, V, K):
+    """What a wait that runs out leaves behind (through the test hook): logits that were not computed are NaN, the
+    others right, the status says so, and zeroed counters make the workspace serve again."""
+    (q, s), (w, u) = codes(M, K, 1), codes(V, K, 2)
+    want = plain(q, s, w, u, None, FP32)
+    work = scores.project_workspace(M, V, K, DEV)
+    lost = []
+    try:
+        for first in (1, 2, 40, 75):
+            mars.test_hook(mars.HOOK_PROJECT_GIVE_UP, first)
+            got = scores.project_int8(q, s, w, u, dtype=FP32, workspace=work)
+            torch.cuda.synchronize()
+            gone = torch.isnan(got)
+            assert torch.equal(got[~gone], want[~gone])
+            lost.append(int(gone.sum()))
+            # a call that runs fewer pairs than `first` - 1 loses nothing and reports nothing
+            assert int(work[:4].view(torch.int32)) == (3 if lost[-1] else 0)
+            work[:scores.PROJECT_COUNTER_BYTES].zero_()
+    finally:
+        mars.test_hook(mars.HOOK_PROJECT_GIVE_UP, 0)
+    assert lost[0] == M * V and lost == sorted(lost, reverse=True) and lost[3] == 0 and lost[1] > 0
+    assert torch.equal(scores.project_int8(q, s, w, u, dtype=FP32, workspace=work), want)
+    assert int(work[:4].view(torch.int32)) == 0
+
+
 def test_refusals_of_the_binding():
     (q, s), (w, u) = codes(4, 64, 1), codes(10, 64, 2)
     good = scores.project_workspace(4, 10, 64, DEV)
