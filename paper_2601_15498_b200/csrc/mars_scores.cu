@@ -7,12 +7,18 @@
 // taken before the scaling, so logits of any size keep their distances.  The gradient of g = sum_j grad_logprob_j and
 // h = grad_entropy is, without the tokens' own terms,
 //   -p (g + h (ln p + entropy)) / T = 2^x (a + b x),  a = -(g + h (entropy - ln s)) / (T s),  b = -h ln2 / (T s).
+//
+// Forward: bound by reading the logits, with the exponential unit (one 2^x a logit, 16 a clock and SM) and instruction
+// issue (6.8 a logit, 1.6 more with alternatives) close behind: bf16 rows 6.1 TB/s (3840 of 151936 in 190 us), fp32 6.65
+// (2000 in 183 us); without half of the exponentials, the floor and the maxima together it would be 178 us.  Batches of 8
+// vectors a thread at 4 blocks per SM; also measured, us for 3840 rows / 512 rows: 4 vectors at 6 blocks 184 / 46, at 5
+// 199 / 43; two buffers of 4 vectors at 4 blocks 193 / 35, at 3 194 / 38; two of 8 at 2 blocks 210 / 37.
+// Gradient: bound by the copy, 6.1 TB/s (2048 rows of 151936 in 204 us).
 #include "mars_fp32.cuh"
 #include "mars_hooks.cuh"
 #include "mars_topk_select.cuh"
 
 #include <cooperative_groups.h>
-
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -352,7 +358,7 @@ __global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobPar
     struct Select { TopSelect s; };
     struct None {};
     __shared__ typename std::conditional<TOP, Select, None>::type s_sel;
-    __shared__ Soft s_soft[kTkThreads / 32];
+    __shared__ Soft s_soft[kScWarps];
     __shared__ Soft s_block;
     __shared__ Cand s_list[kTkMaxK];
     __shared__ Cand s_all[TOP ? kTkMaxK * kScMaxSplit : 1];
@@ -462,10 +468,12 @@ __global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobPar
     RowScore r;
     r.m = s_block.ref;
     r.ok = fabsf(r.m) < INFINITY;
-    r.ln_s = logf(s_block.sum);
+    // s holds the largest logit's 1: what rounding leaves below it would make probabilities above 1
+    const float s = fmaxf(s_block.sum, 1.0f);
+    r.ln_s = logf(s);
     if (tid == 0) {
-        if (p.entropy) p.entropy[out_row] = r.ok ? r.ln_s - kLn2 * (s_block.dot / s_block.sum) : NAN;
-        if (p.stats) { p.stats[2 * out_row] = r.m; p.stats[2 * out_row + 1] = r.ok ? s_block.sum : NAN; }
+        if (p.entropy) p.entropy[out_row] = r.ok ? fmaxf(r.ln_s - kLn2 * (s_block.dot / s), 0.0f) : NAN;
+        if (p.stats) { p.stats[2 * out_row] = r.m; p.stats[2 * out_row + 1] = r.ok ? s : NAN; }
     }
     for (int j = tid; j < p.J; j += kTkThreads) {
         if (j >= kTkThreads) {
