@@ -9,10 +9,10 @@
 //   -p (g + h (ln p + entropy)) / T = 2^x (a + b x),  a = -(g + h (entropy - ln s)) / (T s),  b = -h ln2 / (T s).
 //
 // Forward: bound by reading the logits, with the exponential unit (one 2^x a logit, 16 a clock and SM) and instruction
-// issue (6.8 a logit, 1.6 more with alternatives) close behind: bf16 rows 6.1 TB/s (3840 of 151936 in 190 us), fp32 6.65
-// (2000 in 183 us); without half of the exponentials, the floor and the maxima together it would be 178 us.  Batches of 8
-// vectors a thread at 4 blocks per SM; also measured, us for 3840 rows / 512 rows: 4 vectors at 6 blocks 184 / 46, at 5
-// 199 / 43; two buffers of 4 vectors at 4 blocks 193 / 35, at 3 194 / 38; two of 8 at 2 blocks 210 / 37.
+// issue close behind: bf16 rows 6.5 TB/s (3840 of 151936 in 180 us), fp32 6.8 (2000 in 179 us), with ten alternatives 205
+// to 213 us.  Batches of 8 vectors a thread at 4 blocks per SM; also measured (before the last step, at 190 us / 34 us), us
+// for 3840 rows / 512 rows: 4 vectors at 6 blocks 184 / 46, at 5 199 / 43; two buffers of 4 vectors at 4 blocks 193 / 35,
+// at 3 194 / 38; two of 8 at 2 blocks 210 / 37.
 // Gradient: bound by the copy, 6.1 TB/s (2048 rows of 151936 in 204 us).
 #include "mars_fp32.cuh"
 #include "mars_hooks.cuh"
@@ -172,10 +172,11 @@ __device__ __forceinline__ Soft soft_free(SoftState t)
     return t.a;
 }
 
-// A batch with the maximum bm joins.
+// A batch with the maximum bm joins; vectors from `live` on (the same for all threads) are empty.  Skipping those of the
+// last batch of 9.3 is worth 5 % of the time of rows of 151936 (bf16).
 template <int DT, int U>
 __device__ __forceinline__ void soft_batch(SoftState &t, const uint4 (&v)[U], float bm, float c, float reach, const uint4 *vbase,
-                                           int v0, int nvec)
+                                           int v0, int nvec, int live)
 {
     typedef Elem<DT> E;
     soft_rise<DT>(t, bm, c, reach);
@@ -190,6 +191,7 @@ __device__ __forceinline__ void soft_batch(SoftState &t, const uint4 (&v)[U], fl
     float2 s0 = make_float2(0.0f, 0.0f), d0 = s0, s1 = s0, d1 = s0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        if (u >= live) break;
         const uint4 w = soft_clamp<DT>(v[u], t.floor);
 #pragma unroll
         for (int e = 0; e < E::kVec; e += 2) {
@@ -422,7 +424,7 @@ __global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobPar
     auto batch = [&](const uint4 (&x)[U], int bi) {
         const float bm = batch_maximum<DT, U>(x);
         if constexpr (TOP) best.add(bm, bi);
-        soft_batch<DT, U>(t, x, bm, c, reach, vbase, bi * kBatchVecs + tid, nvec);
+        soft_batch<DT, U>(t, x, bm, c, reach, vbase, bi * kBatchVecs + tid, nvec, (nvec - bi * kBatchVecs + kTkThreads - 1) / kTkThreads);
     };
     for (int bi = 0; bi < nbatch; ++bi) {
         if (bi) load_raw<DT, U>(vbase, bi, nvec, v);
@@ -646,8 +648,8 @@ static bool scores_sizes_ok(int64_t rows, int V) { return rows <= (1ll << 27) &&
 
 // Blocks per row: rows are split while the GPU is not full.  How full it has to be depends on what is left of a slice,
 // since a block also takes some microseconds whatever its slice.  us split into 1 / 2 / 4 / 8 (bf16): 8 rows of 151936
-// 12.9 / 8.5 / 6.4 / 5.5, 120 rows 21.0 / 19.7 / 18.1 / 24.6, 300 rows 31.5 / 26.5 / 28.6 / 37.3, 700 rows 48.6 / 45.9 /
-// 56.0 / 78.8, 1000 rows 57.5 / 61.6; 200 rows of 32000 7.9 / 8.4 / 10.8 / 17.3.
+// 12.0 / 8.2 / 5.8 / 4.8, 60 rows 16.4 / 11.4 / 10.4 / 9.3, 120 rows 21.9 / 19.7 / 16.9 / 21.8, 300 rows 29.6 / 25.0 /
+// 25.1 / 30.6, 700 rows 44.8 / 42.8 / 48.2 / 63.2, 1000 rows 61.6 / 69.2; 200 rows of 32000 7.6 / 7.9 / 9.3 / 12.8.
 static int logprob_split(int64_t rows, int V, int es)
 {
     const int force = hook(kHookForceSplit);
@@ -655,7 +657,7 @@ static int logprob_split(int64_t rows, int V, int es)
     for (; S < kScMaxSplit; S *= 2) {
         const int64_t blocks = rows * S * 2, slice = (int64_t)V * es / (S * 2);
         const bool more = force >= 1 ? 2 * S <= force
-                                     : slice >= 24 * 1024 && blocks <= 148 * (slice >= 128 * 1024 ? 8 : slice >= 64 * 1024 ? 4 : 2);
+                                     : slice >= 24 * 1024 && blocks <= 148 * (slice >= 128 * 1024 ? 8 : 4);
         if (!more) break;
     }
     return S;
