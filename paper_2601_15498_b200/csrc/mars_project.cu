@@ -243,38 +243,58 @@ __device__ __forceinline__ void put_logit(void *out, long long at, float y)
 
 // Logits of a group of tokens (n of them exist) from the sums of one weight row per lane.
 template <int DT>
-__device__ __forceinline__ void project_emit(const ProjectParams &p, const int (&sum)[kPjGroup], const float *xs, float u, float b,
+__device__ __forceinline__ void project_emit(const ProjectParams &p, const int (&sum)[kPjGroup], const float4 *xs, float u, float b,
                                              int v, int tok, int n)
 {
     const float2 u2 = make_float2(u, u), b2 = make_float2(b, b);
     float y[kPjGroup];
 #pragma unroll
-    for (int j = 0; j < kPjGroup; j += 2) {
-        float2 t = mul2(make_float2((float)sum[j], (float)sum[j + 1]), make_float2(xs[j], xs[j + 1]));
+    for (int j = 0; j < kPjGroup; j += 4) {
+        const float4 x = xs[j / 4];
+        float2 t = mul2(make_float2((float)sum[j], (float)sum[j + 1]), make_float2(x.x, x.y));
+        float2 w = mul2(make_float2((float)sum[j + 2], (float)sum[j + 3]), make_float2(x.z, x.w));
         t = p.bias ? fma2(t, u2, b2) : mul2(t, u2);
-        y[j] = t.x;
-        y[j + 1] = t.y;
+        w = p.bias ? fma2(w, u2, b2) : mul2(w, u2);
+        y[j] = t.x; y[j + 1] = t.y; y[j + 2] = w.x; y[j + 3] = w.y;
     }
     if (DT == MARS_BF16 && p.packed) {
         // neighbouring lanes swap: the even one takes both rows of the even token, the odd one of the odd
         const int odd = threadIdx.x & 1;
-        uint32_t *dst = (uint32_t *)((__nv_bfloat16 *)p.out + (tok + odd) * p.ldo + (v - odd));
+        const uint32_t pick = odd ? 0x3276u : 0x5410u;
+        uint32_t w[kPjGroup / 2];
 #pragma unroll
-        for (int j = 0; j < kPjGroup; j += 2) {
-            const float got = __shfl_xor_sync(0xffffffffu, odd ? y[j] : y[j + 1], 1);
-            uint32_t w;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(odd ? y[j + 1] : got), "f"(odd ? got : y[j]));
-            if (v < p.V && j + odd < n) *dst = w;
-            dst += p.ldo;               // two tokens of two bytes
+        for (int j = 0; j < kPjGroup; j += 2) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j / 2]) : "f"(y[j + 1]), "f"(y[j]));
+#pragma unroll
+        for (int j = 0; j < kPjGroup / 2; ++j) w[j] = __byte_perm(w[j], __shfl_xor_sync(0xffffffffu, w[j], 1), pick);
+        if (v >= p.V) return;
+        // (two tokens of two bytes lie ldo words apart)
+        uint32_t *dst = (uint32_t *)((__nv_bfloat16 *)p.out + (tok + odd) * p.ldo + (v - odd));
+        if (n >= kPjGroup) {
+#pragma unroll
+            for (int j = 0; j < kPjGroup / 2; ++j) dst[j * p.ldo] = w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPjGroup / 2; ++j)
+                if (2 * j + odd < n) dst[j * p.ldo] = w[j];
         }
         return;
     }
     if (v >= p.V) return;
     const long long at = (long long)tok * p.ldo + v;
+    if (n >= kPjGroup) {
 #pragma unroll
-    for (int j = 0; j < kPjGroup; ++j)
-        if (j < n) put_logit<DT>(p.out, at + j * p.ldo, y[j]);
+        for (int j = 0; j < kPjGroup; ++j) put_logit<DT>(p.out, at + j * p.ldo, y[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPjGroup; ++j)
+            if (j < n) put_logit<DT>(p.out, at + j * p.ldo, y[j]);
+    }
 }
+
+// What a tile's epilogue needs besides its sums: this lane's weight row and two of the warp's tokens.
+struct ProjectScales {
+    float u, b, x0, x1;
+};
 
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPjThreads, 1)
@@ -379,15 +399,30 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         float *xs = s_xs[mine];
         uint32_t acc = 0, acc_phase = 0;
         bool ok = sound;
-        while (project_next(p, walk, s)) {
+        static_assert(kPjMaxTokens * 4 / kPjWarps == 64, "two scales of tokens per lane");
+        auto scales = [&](const ProjectSegment &g) {
+            const int v = (g.tile / p.n_ttiles) * 2 * kPjRows + in_tile;
+            const int tok0 = (g.tile % p.n_ttiles) * p.tokens, n = min(p.tokens, p.M - tok0);
+            const int t0 = first + (lane / kPjGroup) * kPjStride + lane % kPjGroup, t1 = t0 + 2 * kPjStride;
+            ProjectScales r;
+            r.u = v < p.V ? p.ws[v] : 0.0f;
+            r.b = (p.bias && v < p.V) ? p.bias[v] : 0.0f;
+            r.x0 = t0 < n ? p.xs[tok0 + t0] : 0.0f;
+            r.x1 = t1 < n ? p.xs[tok0 + t1] : 0.0f;
+            return r;
+        };
+        ProjectSegment next;
+        bool more = project_next(p, walk, s);
+        ProjectScales now = {}, then = {};
+        if (more) now = scales(s);
+        for (; more; s = next, now = then) {
+            more = project_next(p, walk, next);
+            if (more) then = scales(next);                   // on their way while this tile is written
             const int v = (s.tile / p.n_ttiles) * 2 * kPjRows + in_tile;
             const int tok0 = (s.tile % p.n_ttiles) * p.tokens, n = min(p.tokens, p.M - tok0);
-            const float u = v < p.V ? p.ws[v] : 0.0f, b = (p.bias && v < p.V) ? p.bias[v] : 0.0f;
             __syncwarp();
-            for (int i = lane; i < kPjMaxTokens * 4 / kPjWarps; i += 32) {
-                const int t = first + (i / kPjGroup) * kPjStride + i % kPjGroup;
-                xs[i] = t < n ? p.xs[tok0 + t] : 0.0f;
-            }
+            xs[lane] = now.x0;
+            xs[lane + 32] = now.x1;
             __syncwarp();
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag, p.status));
             if (!ok) {          // no result for what this block owes
@@ -453,7 +488,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                             for (int j = 0; j < kPjGroup; ++j) sum[j] += x[j] + y[j];
                         }
                     }
-                    project_emit<DT>(p, sum, xs + i, u, b, v, tok0 + c, n - c);
+                    project_emit<DT>(p, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
                 }
             }
             tc_fence_before();
