@@ -20,7 +20,8 @@
 // each pair instead of rounds 102), by operands from L2 for many (64 KB per K block of a 256 x 256 tile, 0.43 us: 12 TB/s;
 // tensor pipe 77 %), and by the power cap in long runs: 3840 x 151936 x 4096 takes 1.53 ms once and 1.77 ms for good, at
 // 1350 MHz.  The epilogue has 16 warps because it has to hide under the MMAs: with 4 warps the same product took 2.30 ms,
-// with 8 of them 1.61, and 2048 x 18944 x 1024 73 us against 46.  Sums of cut tiles added up by atomics instead of stores
+// with 8 of them 1.61, and 2048 x 18944 x 1024 73 us against 46; it
+// is what bounds short K (3840 x 151936 x 64 315 us, 3.7 TB/s of logits).  Sums of cut tiles added up by atomics instead of stores
 // and loads were slower where tiles are few (256 x 4096 x 4096: 40 us against 25): int32 atomics run at 200 G/s.
 #include "mars_fp32.cuh"
 #include "mars_hooks.cuh"
@@ -241,23 +242,30 @@ __device__ __forceinline__ void put_logit(void *out, long long at, float y)
     else ((float *)out)[at] = y;
 }
 
+// How the logits lie, out of the parameters' memory.
+struct ProjectOut {
+    char *out;
+    long long ldo;              // bytes
+    int V;
+    bool packed;
+};
+
 // Logits of a group of tokens (n of them exist) from the sums of one weight row per lane.
 template <int DT>
-__device__ __forceinline__ void project_emit(const ProjectParams &p, const int (&sum)[kPjGroup], const float4 *xs, float u, float b,
+__device__ __forceinline__ void project_emit(const ProjectOut &o, const int (&sum)[kPjGroup], const float4 *xs, float u, float b,
                                              int v, int tok, int n)
 {
+    constexpr int es = DT == MARS_BF16 ? 2 : 4;
     const float2 u2 = make_float2(u, u), b2 = make_float2(b, b);
     float y[kPjGroup];
 #pragma unroll
     for (int j = 0; j < kPjGroup; j += 4) {
         const float4 x = xs[j / 4];
-        float2 t = mul2(make_float2((float)sum[j], (float)sum[j + 1]), make_float2(x.x, x.y));
-        float2 w = mul2(make_float2((float)sum[j + 2], (float)sum[j + 3]), make_float2(x.z, x.w));
-        t = p.bias ? fma2(t, u2, b2) : mul2(t, u2);
-        w = p.bias ? fma2(w, u2, b2) : mul2(w, u2);
+        const float2 t = fma2(mul2(make_float2((float)sum[j], (float)sum[j + 1]), make_float2(x.x, x.y)), u2, b2);
+        const float2 w = fma2(mul2(make_float2((float)sum[j + 2], (float)sum[j + 3]), make_float2(x.z, x.w)), u2, b2);
         y[j] = t.x; y[j + 1] = t.y; y[j + 2] = w.x; y[j + 3] = w.y;
     }
-    if (DT == MARS_BF16 && p.packed) {
+    if (DT == MARS_BF16 && o.packed) {
         // neighbouring lanes swap: the even one takes both rows of the even token, the odd one of the odd
         const int odd = threadIdx.x & 1;
         const uint32_t pick = odd ? 0x3276u : 0x5410u;
@@ -266,33 +274,34 @@ __device__ __forceinline__ void project_emit(const ProjectParams &p, const int (
         for (int j = 0; j < kPjGroup; j += 2) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j / 2]) : "f"(y[j + 1]), "f"(y[j]));
 #pragma unroll
         for (int j = 0; j < kPjGroup / 2; ++j) w[j] = __byte_perm(w[j], __shfl_xor_sync(0xffffffffu, w[j], 1), pick);
-        if (v >= p.V) return;
-        // (two tokens of two bytes lie ldo words apart)
-        uint32_t *dst = (uint32_t *)((__nv_bfloat16 *)p.out + (tok + odd) * p.ldo + (v - odd));
+        if (v >= o.V) return;
+        char *dst = o.out + (tok + odd) * o.ldo + (long long)(v - odd) * es;
         if (n >= kPjGroup) {
 #pragma unroll
-            for (int j = 0; j < kPjGroup / 2; ++j) dst[j * p.ldo] = w[j];
+            for (int j = 0; j < kPjGroup / 2; ++j, dst += 2 * o.ldo) *reinterpret_cast<uint32_t *>(dst) = w[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < kPjGroup / 2; ++j)
-                if (2 * j + odd < n) dst[j * p.ldo] = w[j];
+            for (int j = 0; j < kPjGroup / 2; ++j, dst += 2 * o.ldo)
+                if (2 * j + odd < n) *reinterpret_cast<uint32_t *>(dst) = w[j];
         }
         return;
     }
-    if (v >= p.V) return;
-    const long long at = (long long)tok * p.ldo + v;
+    if (v >= o.V) return;
+    char *dst = o.out + tok * o.ldo + (long long)v * es;
     if (n >= kPjGroup) {
 #pragma unroll
-        for (int j = 0; j < kPjGroup; ++j) put_logit<DT>(p.out, at + j * p.ldo, y[j]);
+        for (int j = 0; j < kPjGroup; ++j, dst += o.ldo) put_logit<DT>(dst, 0, y[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < kPjGroup; ++j)
-            if (j < n) put_logit<DT>(p.out, at + j * p.ldo, y[j]);
+        for (int j = 0; j < kPjGroup; ++j, dst += o.ldo)
+            if (j < n) put_logit<DT>(dst, 0, y[j]);
     }
 }
 
-// What a tile's epilogue needs besides its sums: this lane's weight row and two of the warp's tokens.
-struct ProjectScales {
+// Where a tile lies, and what its epilogue needs besides its sums: the scales of this lane's weight row and of two of
+// the warp's tokens.
+struct ProjectPlace {
+    int v, tok0, n;             // the lane's weight row, the first of n tokens
     float u, b, x0, x1;
 };
 
@@ -397,29 +406,32 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const int in_tile = (int)rank * kPjRows + quarter * 32 + lane;
         const long long slot = (long long)p.tokens * 2 * kPjRows;
         float *xs = s_xs[mine];
+        ProjectOut o;
+        o.out = (char *)p.out; o.ldo = p.ldo * (DT == MARS_BF16 ? 2 : 4); o.V = p.V; o.packed = p.packed != 0;
         uint32_t acc = 0, acc_phase = 0;
         bool ok = sound;
         static_assert(kPjMaxTokens * 4 / kPjWarps == 64, "two scales of tokens per lane");
-        auto scales = [&](const ProjectSegment &g) {
-            const int v = (g.tile / p.n_ttiles) * 2 * kPjRows + in_tile;
-            const int tok0 = (g.tile % p.n_ttiles) * p.tokens, n = min(p.tokens, p.M - tok0);
-            const int t0 = first + (lane / kPjGroup) * kPjStride + lane % kPjGroup, t1 = t0 + 2 * kPjStride;
-            ProjectScales r;
-            r.u = v < p.V ? p.ws[v] : 0.0f;
-            r.b = (p.bias && v < p.V) ? p.bias[v] : 0.0f;
-            r.x0 = t0 < n ? p.xs[tok0 + t0] : 0.0f;
-            r.x1 = t1 < n ? p.xs[tok0 + t1] : 0.0f;
+        const int t0 = first + (lane / kPjGroup) * kPjStride + lane % kPjGroup, t1 = t0 + 2 * kPjStride;
+        auto place = [&](const ProjectSegment &g) {
+            ProjectPlace r;
+            const int row = g.tile / p.n_ttiles;
+            r.v = row * 2 * kPjRows + in_tile;
+            r.tok0 = (g.tile - row * p.n_ttiles) * p.tokens;
+            r.n = min(p.tokens, p.M - r.tok0);
+            r.u = r.v < p.V ? p.ws[r.v] : 0.0f;
+            r.b = (p.bias && r.v < p.V) ? p.bias[r.v] : 0.0f;
+            r.x0 = t0 < r.n ? p.xs[r.tok0 + t0] : 0.0f;
+            r.x1 = t1 < r.n ? p.xs[r.tok0 + t1] : 0.0f;
             return r;
         };
         ProjectSegment next;
         bool more = project_next(p, walk, s);
-        ProjectScales now = {}, then = {};
-        if (more) now = scales(s);
+        ProjectPlace now = {}, then = {};
+        if (more) now = place(s);
         for (; more; s = next, now = then) {
             more = project_next(p, walk, next);
-            if (more) then = scales(next);                   // on their way while this tile is written
-            const int v = (s.tile / p.n_ttiles) * 2 * kPjRows + in_tile;
-            const int tok0 = (s.tile % p.n_ttiles) * p.tokens, n = min(p.tokens, p.M - tok0);
+            if (more) then = place(next);                    // its scales are on their way while this tile is written
+            const int v = now.v, tok0 = now.tok0, n = now.n;
             __syncwarp();
             xs[lane] = now.x0;
             xs[lane + 32] = now.x1;
@@ -461,34 +473,35 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     __threadfence();
                 }
             }
-            if (last) {
+            // (two copies of the loop: sums that may still change would be moved between registers once more)
+            if (whole) {
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];
-                    {
-                        float x[kPjGroup];
-                        tc_ld16(taddr + c, x);
-#pragma unroll
-                        for (int j = 0; j < kPjGroup; ++j) sum[j] = __float_as_int(x[j]);
-                    }
-                    if (!whole) {
-                        // two holders' parts at a time: 32 loads of a line each in flight
-                        const int *src = p.partial + in_tile + (long long)c * (2 * kPjRows);
+                    tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
+                    project_emit<DT>(o, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
+                }
+            } else if (last) {
 #pragma unroll 1
-                        for (int o = c0; o <= c1; o += 2) {
-                            const int *part = src + (2ll * o + (o == c0 ? 1 : 0)) * slot, *next = src + 2ll * (o + 1) * slot;
-                            const bool a = o != walk.pair, b2 = o + 1 <= c1 && o + 1 != walk.pair;
-                            int x[kPjGroup], y[kPjGroup];
+                for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
+                    int sum[kPjGroup];
+                    tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
+                    // two holders' parts at a time: 32 loads of a line each in flight
+                    const int *src = p.partial + in_tile + (long long)c * (2 * kPjRows);
+#pragma unroll 1
+                    for (int h = c0; h <= c1; h += 2) {
+                        const int *part = src + (2ll * h + (h == c0 ? 1 : 0)) * slot, *other = src + 2ll * (h + 1) * slot;
+                        const bool one = h != walk.pair, two = h + 1 <= c1 && h + 1 != walk.pair;
+                        int x[kPjGroup], y[kPjGroup];
 #pragma unroll
-                            for (int j = 0; j < kPjGroup; ++j) {
-                                x[j] = a ? __ldcg(part + j * (2 * kPjRows)) : 0;
-                                y[j] = b2 ? __ldcg(next + j * (2 * kPjRows)) : 0;
-                            }
-#pragma unroll
-                            for (int j = 0; j < kPjGroup; ++j) sum[j] += x[j] + y[j];
+                        for (int j = 0; j < kPjGroup; ++j) {
+                            x[j] = one ? __ldcg(part + j * (2 * kPjRows)) : 0;
+                            y[j] = two ? __ldcg(other + j * (2 * kPjRows)) : 0;
                         }
+#pragma unroll
+                        for (int j = 0; j < kPjGroup; ++j) sum[j] += x[j] + y[j];
                     }
-                    project_emit<DT>(p, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
+                    project_emit<DT>(o, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
                 }
             }
             tc_fence_before();
