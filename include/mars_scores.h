@@ -22,6 +22,7 @@ extern "C" {
 
 #define MARS_SCORES_MAX_TOKENS 1024 /* cap on J, tokens per row        */
 #define MARS_SCORES_MAX_TOP 32      /* cap on k, alternatives per row  */
+#define MARS_PROJECT_COUNTER_BYTES 16384 /* counters at the head of mars_project_int8's workspace */
 
 /*
  * Rows as signed 8-bit codes with one scale each: with a = max |x| of a row,
@@ -57,7 +58,6 @@ mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t row
  *   that were not computed are NaN and the first uint32 of the workspace is MARS_SEQ_TIMEOUT; it is 0
  *   otherwise.  After such a call those bytes have to be zeroed before MARS_COUNTERS_ZERO is used again.
  */
-#define MARS_PROJECT_COUNTER_BYTES 16384
 size_t mars_project_int8_workspace_bytes(int64_t M, int V, int K);
 mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scale, const void *wq, int64_t ldw,
                                 const float *w_scale, const float *bias, int64_t M, int V, int K, void *out,

@@ -31,8 +31,6 @@ PROJECT_COUNTER_BYTES = 16384
 
 _LOGIT_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32}
 _ROW_DTYPES = {torch.bfloat16: mars.BF16, torch.float32: mars.FP32, torch.float16: 2}
-
-
 _I32, _F32, _I8 = torch.int32, torch.float32, torch.int8
 
 # The calls below run once a decode step or more, so their host time counts: attributes are read once, devices
@@ -64,6 +62,8 @@ def _logits(logits, V):
     if inner != 1 and width != 1:
         raise MarsError("logits must have unit inner stride")
     V = width if V is None else int(V)
+    if V > width:
+        raise MarsError(f"logits have {width} columns, not {V}")
     # a single row has no second one to be apart from
     return _LOGIT_DTYPES[dtype], rows, max(ld, V) if rows == 1 else ld, V, index
 

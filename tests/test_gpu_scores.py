@@ -320,6 +320,9 @@ def test_refusals_of_the_binding():
                 lambda: scores.token_logprobs(z, tok, k=101), lambda: scores.token_logprobs(z, tok, temperature=0.0),
                 lambda: scores.token_logprobs(z, tok, temperature=float("nan")), lambda: scores.token_logprobs(z.cpu(), tok),
                 lambda: scores.token_logprobs(z, torch.zeros((4, 1025), dtype=torch.int32, device=DEV)),
+                lambda: scores.token_logprobs(z, tok, V=101), lambda: scores.token_logprobs(z[:1], tok[:1], V=101),
+                lambda: scores.token_logprobs(z[:, :50], tok, V=60), lambda: scores.token_logprobs(z[:1].expand(4, 100), tok),
+                lambda: scores.token_logprobs_backward(z[:, :50], tok, f, torch.zeros((4, 2), device=DEV), V=51),
                 lambda: scores.token_logprobs(z, tok, out={"logprob": torch.empty((4, 3), device=DEV)}),
                 lambda: scores.token_logprobs_backward(z, tok, f, torch.zeros((4, 3), device=DEV)),
                 lambda: scores.token_logprobs_backward(z, tok, {"stats": f["stats"]}, torch.zeros((4, 2), device=DEV), torch.zeros(4, device=DEV)),
