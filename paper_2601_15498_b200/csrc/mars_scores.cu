@@ -649,15 +649,16 @@ static bool scores_sizes_ok(int64_t rows, int V) { return rows <= (1ll << 27) &&
 // Blocks per row: rows are split while the GPU is not full.  How full it has to be depends on what is left of a slice,
 // since a block also takes some microseconds whatever its slice.  us split into 1 / 2 / 4 / 8 (bf16): 8 rows of 151936
 // 12.0 / 8.2 / 5.8 / 4.8, 60 rows 16.4 / 11.4 / 10.4 / 9.3, 120 rows 21.9 / 19.7 / 16.9 / 21.8, 300 rows 29.6 / 25.0 /
-// 25.1 / 30.6, 700 rows 44.8 / 42.8 / 48.2 / 63.2, 1000 rows 61.6 / 69.2; 200 rows of 32000 7.6 / 7.9 / 9.3 / 12.8.
-static int logprob_split(int64_t rows, int V, int es)
+// 25.1 / 30.6, 700 rows 44.8 / 42.8 / 48.2 / 63.2, 1000 rows 61.6 / 69.2; 200 rows of 32000 7.6 / 7.9 / 9.3 / 12.8.  Joining
+// eight lists of many alternatives costs more than the split gains: 60 rows with 32 of them, split into 4 / 8, 18.4 / 24.7.
+static int logprob_split(int64_t rows, int V, int es, int k)
 {
     const int force = hook(kHookForceSplit);
     int S = 1;
     for (; S < kScMaxSplit; S *= 2) {
         const int64_t blocks = rows * S * 2, slice = (int64_t)V * es / (S * 2);
         const bool more = force >= 1 ? 2 * S <= force
-                                     : slice >= 24 * 1024 && blocks <= 148 * (slice >= 128 * 1024 ? 8 : 4);
+                                     : slice >= 24 * 1024 && blocks <= 148 * (slice >= 128 * 1024 ? 8 : slice >= 64 * 1024 || k <= 16 ? 4 : 2);
         if (!more) break;
     }
     return S;
@@ -705,7 +706,7 @@ mars_status_t mars_token_logprobs(const void *logits, int64_t ld, mars_dtype_t d
     if ((uintptr_t)logits % es) return MARS_ERR_INVALID_ARG;
     LogprobParams p;
     p.logits = logits; p.ld = ld; p.n = n; p.row_ids = row_ids; p.V = V;
-    p.S = logprob_split(rows, V, es);
+    p.S = logprob_split(rows, V, es, k);
     p.L = slice_columns(V, p.S);
     p.temperature = temperature;
     p.c = (float)(1.4426950408889634 / (double)temperature);
