@@ -4,7 +4,7 @@
 //   s = sum 2^x,  u = sum 2^x x,  ln p_v = (z_v - m) / T - ln s,  entropy = ln s - ln2 u / s,
 // so one pass suffices: every thread keeps (m, s, u) of what it has seen and rescales them when its
 // maximum rises by d (in units of x): s 2^d, (u + s d) 2^d.  Maxima are kept unscaled and differences of them
-// taken before the scaling, so logits of any size keep their distances.  The gradient of g = sum_j grad_logprob_j and
+// taken before the scaling (after it where they pass fp32's range), so logits of any size keep their distances.  The gradient of g = sum_j grad_logprob_j and
 // h = grad_entropy is, without the tokens' own terms,
 //   -p (g + h (ln p + entropy)) / T = 2^x (a + b x),  a = -(g + h (entropy - ln s)) / (T s),  b = -h ln2 / (T s).
 //
@@ -61,10 +61,12 @@ __device__ __forceinline__ void soft_move(Soft &a, float d)
     a.sum *= f;
 }
 
-// Distance of a reference to a larger one; 2^-1000 is 0, and 0 * 1000 is, unlike 0 * infinity.
+// Distance of a reference to a larger one; 2^-1000 is 0, and 0 * 1000 is, unlike 0 * infinity.  A difference that passes
+// fp32's range is one of opposite signs (or of an infinity), so scaling its parts first loses nothing.
 __device__ __forceinline__ float soft_distance(float from, float to, float c)
 {
-    return from == to ? 0.0f : fmaxf((from - to) * c, -1000.0f);
+    const float d = from - to;
+    return from == to ? 0.0f : fmaxf(d > -INFINITY ? d * c : fmaf(from, c, -(to * c)), -1000.0f);
 }
 
 // The union of a warp's 32 sets, in all lanes: everybody moves to the largest reference, then plain sums.
@@ -347,7 +349,9 @@ struct RowScore {
 __device__ __forceinline__ float row_logprob(const RowScore &r, float z, float temperature)
 {
     if (!r.ok) return NAN;
-    return (z > -INFINITY) ? __fdiv_rn(z - r.m, temperature) - r.ln_s : -INFINITY;
+    if (!(z > -INFINITY)) return -INFINITY;
+    const float d = z - r.m;             // (beyond fp32's range: see soft_distance)
+    return (d > -INFINITY ? __fdiv_rn(d, temperature) : __fdiv_rn(z, temperature) - __fdiv_rn(r.m, temperature)) - r.ln_s;
 }
 
 // Forward: a cluster of S blocks (S = 1: a block) streams one row, each block a contiguous slice; the

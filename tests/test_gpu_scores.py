@@ -118,6 +118,28 @@ def test_extreme_temperatures_and_sizes_of_logits(T, dtype):
             sc.check_grad(z, grad, sc.reference(z, tok, T), tok, g, g[:, 0], T)
 
 
+@pytest.mark.parametrize("T", [2.0, 4.0, 1e3, 1e37, 1e38, 3e38])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_logits_further_apart_than_the_largest_number(T, dtype):
+    """Logits of both signs at the end of the range: their difference passes it, divided by T it need not."""
+    big = torch.finfo(dtype).max
+    for V in (2, 37, 4099, 151936):
+        z, tok = rows_of(5, V, dtype, 6), tokens(5, 4, V, 2)
+        z[0] = -big; z[0, V // 2] = big
+        z[1] = big; z[1, ::2] = -big
+        z[2] = torch.linspace(-1, 1, V, device=DEV) * big
+        z[3] = torch.linspace(1, -1, V, device=DEV) * big; z[3, V // 3] = float("-inf")
+        z[4, 0] = big; z[4, -1] = -big
+        tok[:, 0], tok[:, 3] = 0, V // 2
+        k = min(V, 9)
+        got = scores.token_logprobs(z, tok, temperature=T, k=k)
+        ref = sc.check_forward(z, got, tok, T, k)
+        assert torch.isfinite(got["logprob"][:3, [0, 3]]).all()             # twice the largest number over T >= 2
+        g = torch.randn((5, 4), generator=gen(2), device=DEV)
+        h = torch.randn((5,), generator=gen(3), device=DEV)
+        sc.check_grad(z, scores.token_logprobs_backward(z, tok, got, g, h, temperature=T), ref, tok, g, h, T)
+
+
 def test_alternatives_follow_the_order_of_topk_rows():
     for V, dtype in ((4099, BF16), (4099, FP32), (37, FP32)):
         z = special_rows(V, dtype)
