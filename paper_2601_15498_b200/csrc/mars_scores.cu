@@ -575,8 +575,10 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
     const bool ok = fabsf(m) < INFINITY && s > 0.0f;
     const float ts = p.temperature * s;
     const float h = p.h ? p.h[row] : 0.0f;
-    float a = -g / ts, b = 0.0f;
-    if (p.h) { a = -fmaf(h, p.entropy[row] - logf(s), g) / ts; b = -(h * kLn2) / ts; }
+    float a = -g, b = 0.0f;
+    if (p.h) { a = -fmaf(h, p.entropy[row] - logf(s), g); b = -(h * kLn2); }
+    if (ts < INFINITY) { a /= ts; b /= ts; }
+    else { a = a / s / p.temperature; b = b / s / p.temperature; }       // T s passes fp32's range, the quotient need not
     if (!ok) { a = 0.0f; b = 0.0f; }
 
     // the tokens' logits, before anything is overwritten

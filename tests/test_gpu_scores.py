@@ -140,6 +140,21 @@ def test_logits_further_apart_than_the_largest_number(T, dtype):
         sc.check_grad(z, scores.token_logprobs_backward(z, tok, got, g, h, temperature=T), ref, tok, g, h, T)
 
 
+@pytest.mark.parametrize("T", [1e34, 1e38, 3e38])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_gradient_where_temperature_times_sum_overflows(T, dtype):
+    z, tok = rows_of(5, 40007, dtype, 4, spread=T / 8), tokens(5, 3, 40007, 1)
+    z.clamp_(-0.4 * 3e38, 0.4 * 3e38)
+    got = scores.token_logprobs(z, tok, temperature=T)
+    ref = sc.check_forward(z, got, tok, T)
+    g = torch.randn((5, 3), generator=gen(2), device=DEV) * 1e14
+    h = torch.randn((5,), generator=gen(3), device=DEV) * 1e14
+    for ge in (None, h):
+        grad = scores.token_logprobs_backward(z, tok, got, g, ge, temperature=T)
+        sc.check_grad(z, grad, ref, tok, g, ge, T)
+        assert (grad != 0).all()
+
+
 def test_alternatives_follow_the_order_of_topk_rows():
     for V, dtype in ((4099, BF16), (4099, FP32), (37, FP32)):
         z = special_rows(V, dtype)
