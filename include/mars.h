@@ -27,7 +27,10 @@
  *     drains and waits for it only before it reads anything else or writes workspace and
  *     outputs.  This pays where several resident batches are verified back to back (a few
  *     hundred rows: 30 -> 21 us per call); it must not be set when the operation right before the
- *     call on the stream produces, or may still be writing, the call's logits.  Rows may start at any element-aligned address;
+ *     call on the stream produces, or may still be writing, the call's logits.  Operations before
+ *     that one have completed, except behind a row of calls that carry the flag themselves: these
+ *     reach over one another, so their logits must not come from the operation before the first
+ *     of them either.  Rows may start at any element-aligned address;
  *     16-byte-aligned rows (ld*sizeof(elem) % 16 == 0 and an aligned base) take the
  *     vector path end to end.
  *   - Decisions are taken in fp32: bf16 logits widen exactly, the ratio is one IEEE

@@ -96,8 +96,7 @@ constexpr size_t rows_smem_bytes(int rows)
 template <int D, int DT, int kRows>
 __global__ void __launch_bounds__(kRowsThreads, rows_occ(kRows, D)) attn_rows_kernel(const AttnParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     using Shape = RowsShape<kRows>;
     constexpr int kNT = kRows / 8;            // n-tiles of query rows
     constexpr bool kQShared = rows_q_shared(kRows);   // Q fragments in shared memory (48, 64 registers less)

@@ -668,8 +668,7 @@ __device__ __forceinline__ void tile_softmax(const AttnParams &p, AttnRange r, T
 template <int D, int DT>
 __global__ void __launch_bounds__(kTileThreads, 1) attn_tile_kernel(const AttnParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;

@@ -154,8 +154,7 @@ __host__ __device__ inline int rows_at_once(int per_row) { return per_row >= 256
 template <int D, int DT>
 __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     constexpr int kG = D / 16;   // groups of a row
     const int b = blockIdx.y;
     const int count = p.count ? p.count[b] : p.N, len = p.kv.seq_len[b], cap = kv_capacity(p.kv, b);
@@ -231,8 +230,7 @@ __device__ __forceinline__ float product_to_odd(float f, float g, uint32_t last)
 template <int D, int DT>
 __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     constexpr int kG = D / 16;
     const int b = blockIdx.y, lay = blockIdx.z, H = p.kv.kv_heads;
     const int count = p.count ? p.count[b] : p.rows, start = p.start ? p.start[b] : 0, cap = kv_capacity(p.kv, b);
@@ -327,8 +325,7 @@ __device__ bool commit_path_ok(const CommitParams &p, int b, int lane, int *a_ou
 template <int D>
 __global__ void __launch_bounds__(128) kv_commit_kernel(const CommitParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const int lane = threadIdx.x & 31;
     const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
     const int64_t per_seq = (int64_t)p.layers * p.kv.kv_heads;
@@ -404,8 +401,7 @@ __global__ void __launch_bounds__(128) kv_commit_kernel(const CommitParams p)
 // Lengths in place: only after every warp of the kernel above has read the old ones.
 __global__ void __launch_bounds__(256) kv_commit_len_kernel(const CommitParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const int lane = threadIdx.x & 31, b = (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
     if (b >= p.B) return;
     int a;
@@ -587,8 +583,7 @@ __device__ __forceinline__ int resize_want(const PoolParams &p, int extra, int l
 // found by a prefix sum over the bit set.  No order of threads shows in the result.
 __global__ void __cluster_dims__(kPoolCluster, 1, 1) __launch_bounds__(kPoolThreads) kv_resize_kernel(const PoolParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     extern __shared__ int s_first[];   // [n]
     __shared__ int s_warp[32];
     __shared__ FreeTile s_free;
@@ -666,8 +661,7 @@ constexpr int kForkEmpty = -1;   // status inside the kernel: a sound pair whose
 // One block: validate and claim, find the new last pages, write tables and counts.
 __global__ void __launch_bounds__(kPoolThreads) kv_fork_kernel(const PoolParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     extern __shared__ int s_first[];   // [n]
     __shared__ int s_warp[32];
     __shared__ FreeTile s_free;
@@ -763,8 +757,7 @@ struct ForkCopyParams {
 template <int D>
 __global__ void __launch_bounds__(256) kv_fork_copy_kernel(const ForkCopyParams p)
 {
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const int i = blockIdx.x, lay = blockIdx.y;
     if (p.status[i] != MARS_SEQ_OK) return;
     const int s = p.src[i], d = p.dst[i], len = p.kv.seq_len[d];

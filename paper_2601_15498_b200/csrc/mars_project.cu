@@ -88,8 +88,7 @@ __global__ void __launch_bounds__(kQzThreads) quantize_rows_kernel(const void *x
 {
     typedef QzElem<DT> E;
     __shared__ uint32_t s_max[kQzThreads / 32];
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const int tid = threadIdx.x % kGroup;
     const long long row = (long long)blockIdx.x * (kQzThreads / kGroup) + threadIdx.x / kGroup;
     if (row >= rows) return;             // the same for a whole group
@@ -324,7 +323,6 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     ProjectWalk walk(p);
     ProjectSegment s;
 
-    pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 2 * kPjWarps); }
@@ -342,7 +340,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = s_tmem_base;
     volatile int *abort_flag = &s_abort;
-    pdl_wait();                    // the set-up above lies under the predecessor's end
+    pdl_begin();                   // the set-up above lies under the predecessor's end
     const bool sound = walk.pair < p.give_up;
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0 && p.give_up == INT_MAX) *p.status = 0;      // (a wait gives up after a second at the earliest)

@@ -372,8 +372,7 @@ __global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobPar
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = p.k;
     const long long out_row = blockIdx.x / p.S;
     const int rank = (int)(blockIdx.x - out_row * p.S);
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const long long row = p.row_ids ? (long long)p.row_ids[out_row] : out_row;
     if (row < 0 || row >= p.n) {
         // absent: the whole cluster leaves here
@@ -553,8 +552,7 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
 {
     typedef Elem<DT> E;
     __shared__ float s_z[MARS_SCORES_MAX_TOKENS];
-    pdl_launch_dependents();
-    pdl_wait();
+    pdl_begin();
     const int tid = threadIdx.x, lane = tid & 31;
     // the last rows first: a forward pass that came just before has left them in L2
     const long long block = (long long)gridDim.x - 1 - blockIdx.x, row = block / p.S;

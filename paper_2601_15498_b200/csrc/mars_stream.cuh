@@ -35,8 +35,18 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b)
 // logits do not come from the predecessor: then only workspaces and outputs are at stake, and the
 // wait moves behind the streaming loop.  Without the launch attribute, or without a predecessor
 // that triggers early, both calls do nothing.
+//
+// A kernel lets its dependents be scheduled only after it has waited itself (pdl_begin()): a dependent that reads
+// before it waits (MARS_LOGITS_READY) may then take everything that precedes this kernel for complete.  In the other
+// order such a call could overtake the producer of its logits when one more call stands between them.  Only the
+// MARS_LOGITS_READY calls themselves trigger first, so their promise reaches back over one another.
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_begin()
+{
+    pdl_wait();
+    pdl_launch_dependents();
+}
 
 // Launch with programmatic stream serialisation allowed (see above); `allow` = false gives the
 // plain stream order (a measurement aid: the cost of a call without any overlap).

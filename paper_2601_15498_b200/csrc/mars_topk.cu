@@ -86,8 +86,7 @@ __global__ void __launch_bounds__(kTkThreads, MINB) topk_slice_kernel(const Topk
     constexpr int kBatchVecs = kTkThreads * U;
     const int nfull = nvec / kBatchVecs;
 
-    pdl_launch_dependents();    // the next call's kernel may be scheduled; it waits for this one first thing
-    pdl_wait();     // scheduled early itself (behind the previous call's last kernel), reads nothing before that is done
+    pdl_begin();    // scheduled early (behind the previous call's last kernel), reads nothing before that is done
     uint4 v[U];
     typename E::packed_t q[U];
     // batch 0: issue its loads first, so that the set-up below overlaps their latency
@@ -269,7 +268,7 @@ __global__ void __launch_bounds__(kTkMergeThreads) topk_merge_kernel(const TopkP
     extern __shared__ Cand s_c[];            // [n] the slices' lists, then [n] the entries kept
     __shared__ int s_found, s_nkeep;
     __shared__ unsigned s_thr;
-    pdl_launch_dependents();     // the next call's slice kernel may be scheduled (it waits for this one)
+    pdl_launch_dependents();     // the next call's kernel may be scheduled: what precedes this call has completed (the slices waited)
     const int k = p.k, n = p.S * k;
     Cand *s_keep = s_c + n;
     const long long row = blockIdx.x;

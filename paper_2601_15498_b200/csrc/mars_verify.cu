@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(kThreads, MINB) verify_kernel(const Params p)
     // waits for its predecessor right here unless the caller vouched that the logits do not come
     // from it (MARS_LOGITS_READY); then the wait moves to the point where the workspace is first
     // touched.
-    pdl_launch_dependents();
-    if (!p.early) pdl_wait();
+    if (p.early) pdl_launch_dependents();
+    else pdl_begin();
     const int tid = threadIdx.x;
     const long long blk = blockIdx.x;
     const long long row = blk / p.S;

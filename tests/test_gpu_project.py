@@ -6,7 +6,7 @@ import torch
 
 import hookctl as hooks
 import scores_checks as sc
-from paper_2601_15498_b200 import mars, scores
+from paper_2601_15498_b200 import kv_cache, mars, scores
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -102,6 +102,60 @@ def test_streams_and_graph():
         graphs[i % 2].replay()
         torch.cuda.synchronize()
         assert torch.equal(out, plain(*scores.quantize_rows(x), w, u, None, BF16))
+
+
+@pytest.mark.parametrize("between", ["quantize_rows", "token_logprobs", "topk_rows", "project_int8", "verify_tree", "append"])
+@pytest.mark.parametrize("use_graph", [False, True])
+def test_logits_of_the_call_before_last_are_complete(between, use_graph):
+    """MARS_LOGITS_READY vouches that the operation right before the call does not produce its logits.  The projection
+    two calls before may: whatever stands between them, the verification sees all of its logits."""
+    B, N, V, K = 24, 8, 30000, 640
+    (w, u), (small, su) = codes(V, K, 1), codes(300, 64, 2)
+    xs = [codes(B * N, K, 10 + i) for i in range(2)]
+    want = [plain(*x, w, u, None, BF16) for x in xs]
+    tok = want[0].argmax(1).view(B, N).int()
+    parent = torch.arange(-1, N - 1, device=DEV, dtype=torch.int32)
+    rounds, flags = 12, mars.COUNTERS_ZERO | mars.LOGITS_READY
+    ws = torch.zeros(mars.workspace_bytes(B, N, V, mars.BF16), dtype=torch.uint8, device=DEV)
+    ws2 = torch.zeros_like(ws)
+    ref = [{k: t.clone() for k, t in mars.verify_tree(z, tok, parent, 0.9, debug=True).items() if k != "_keepalive"} for z in want]
+    outs = [mars.alloc_outputs(B, N, N - 1, DEV, debug=True) for _ in range(rounds)]
+    spare = mars.alloc_outputs(B, N, N - 1, DEV)
+    logits = torch.zeros((B * N, V), dtype=BF16, device=DEV)
+    work, work2 = scores.project_workspace(B * N, V, K, DEV), scores.project_workspace(1, 300, 64, DEV)
+    row = torch.randn((1, 64), generator=gen(3), device=DEV)
+    pair, few = scores.quantize_rows(row), torch.randn((1, 5000), generator=gen(4), device=DEV)
+    lp = scores.token_logprobs(few)
+    topk = (torch.empty((1, 4), device=DEV), torch.empty((1, 4), dtype=torch.int32, device=DEV))
+    work_k = torch.empty(int(mars.lib().mars_topk_workspace_bytes(1, 5000, mars.FP32, 4)), dtype=torch.uint8, device=DEV)
+    cache = kv_cache.KVCache.empty(1, 2, 1, 64, 16, 1, 2, DEV)
+    kv_cache.resize(cache, torch.tensor([8], dtype=torch.int32, device=DEV))
+    kv = torch.randn((1, 1, 1, 64), generator=gen(5), device=DEV).to(BF16)
+    other = {"quantize_rows": lambda: scores.quantize_rows(row, out=pair), "token_logprobs": lambda: scores.token_logprobs(few, out=lp),
+             "topk_rows": lambda: mars.topk_rows(few, 4, out=topk, workspace=work_k),
+             "project_int8": lambda: scores.project_int8(*pair, small, su, workspace=work2),
+             "verify_tree": lambda: mars.verify_tree(want[1], tok, parent, 0.9, flags=mars.COUNTERS_ZERO, workspace=ws2, out=spare),
+             "append": lambda: kv_cache.append(cache, 0, kv, kv)}[between]
+    mars.verify_tree(want[0], tok, parent, 0.9, workspace=ws)
+    torch.cuda.synchronize()
+
+    def run_all():
+        for i in range(rounds):
+            scores.project_int8(*xs[i % 2], w, u, out=logits, workspace=work)
+            other()
+            mars.verify_tree(logits, tok, parent, 0.9, flags=flags, workspace=ws, out=outs[i])
+    if use_graph:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run_all()
+        graph.replay()
+        graph.replay()
+    else:
+        run_all()
+    torch.cuda.synchronize()
+    for i in range(rounds):
+        for k, t in ref[i % 2].items():
+            assert torch.equal(outs[i][k], t), (i, k)
 
 
 def quantised(x):
