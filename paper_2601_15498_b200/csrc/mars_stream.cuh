@@ -10,10 +10,12 @@
 
 namespace mars {
 
+// A load of the ordinary, coherent kind that the compiler keeps behind the waits before it: the logits may be what the
+// predecessor on the stream writes, into memory that this kernel was given while that one still ran (see pdl_wait).
 __device__ __forceinline__ uint4 ld_stream(const uint4 *p)
 {
     uint4 v;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
         : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
         : "l"(p));
     return v;

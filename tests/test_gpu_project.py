@@ -158,6 +158,49 @@ def test_logits_of_the_call_before_last_are_complete(between, use_graph):
             assert torch.equal(outs[i][k], t), (i, k)
 
 
+@pytest.mark.parametrize("M,V,K", [(1, 151936, 256), (40, 32000, 1024), (333, 5001, 300)])
+@pytest.mark.parametrize("use_graph", [False, True])
+def test_calls_read_what_their_predecessor_writes(M, V, K, use_graph):
+    """Projection, log probabilities, a gradient in the logits' place and the log probabilities of that, over and over with
+    nothing in between: bit for bit what the calls give one at a time."""
+    (w, u) = codes(V, K, 1)
+    xs = [codes(M, K, 10 + i) for i in range(3)]
+    tok = torch.randint(0, V, (M, 2), generator=gen(2), device=DEV).to(torch.int32)
+    g = torch.randn((M, 2), generator=gen(3), device=DEV)
+    work, logits = scores.project_workspace(M, V, K, DEV), torch.zeros((M, V), dtype=BF16, device=DEV)
+
+    def step(x):
+        scores.project_int8(*x, w, u, out=logits, workspace=work)
+        first = scores.token_logprobs(logits, tok, k=3)
+        yield first
+        scores.token_logprobs_backward(logits, tok, first, g, out=logits)
+        yield scores.token_logprobs(logits, tok)
+    want = []
+    for x in xs:
+        one = []
+        for got in step(x):
+            torch.cuda.synchronize()
+            one.append({n: t.clone() for n, t in got.items()})
+        want.append(one)
+    assert not torch.equal(want[0][0]["logprob"], want[1][0]["logprob"])
+
+    def run_all():
+        return [list(step(xs[i % 3])) for i in range(12)]
+    if use_graph:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            many = run_all()
+        graph.replay()
+        graph.replay()
+    else:
+        many = run_all()
+    torch.cuda.synchronize()
+    for i, pair in enumerate(many):
+        for got, ref in zip(pair, want[i % 3]):
+            for n in ref:
+                assert torch.equal(torch.nan_to_num(got[n]), torch.nan_to_num(ref[n])), (i, n)
+
+
 def quantised(x):
     x = x.float()
     a = x.abs().amax(1)
