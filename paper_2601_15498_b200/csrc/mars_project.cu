@@ -335,6 +335,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                      ::"r"(smem_u32(&s_tmem_base)), "r"(kPjTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
+    __syncwarp();                  // (single lanes worked above; what follows is for whole warps)
     tc_fence_before();
     cluster_sync_all();            // both blocks' barriers exist before anything signals them
     tc_fence_after();
@@ -460,22 +461,25 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 #pragma unroll
                     for (int j = 0; j < kPjGroup; ++j) __stcg(dst + (c + j) * (2 * kPjRows), __float_as_int(x[j]));
                 }
-                __threadfence();
+                // every lane's sums, then the warp's arrival: lane 0 orders both for all of them, before and behind
                 __syncwarp();
                 unsigned *counter = p.counters + (c0 * 2 + (int)rank) * kPjWarps + mine;
                 unsigned seen = 0;
-                if (lane == 0) seen = atomicAdd(counter, 1u);
-                last = __shfl_sync(0xffffffffu, seen, 0) == (unsigned)(c1 - c0);
-                if (last) {
-                    if (lane == 0) *counter = 0;             // as it was found: the workspace serves the next call
+                if (lane == 0) {
+                    __threadfence();
+                    seen = atomicAdd(counter, 1u);
+                    if (seen == (unsigned)(c1 - c0)) *counter = 0;       // as it was found: the workspace serves the next call
                     __threadfence();
                 }
+                __syncwarp();
+                last = __shfl_sync(0xffffffffu, seen, 0) == (unsigned)(c1 - c0);
             }
             // (two copies of the loop: sums that may still change would be moved between registers once more)
             if (whole) {
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];
+                    __syncwarp();                            // (lanes without a weight row left the last group early)
                     tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
                     project_emit<DT>(o, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
                 }
@@ -483,6 +487,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];
+                    __syncwarp();                            // (lanes without a weight row left the last group early)
                     tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
                     // two holders' parts at a time: 32 loads of a line each in flight
                     const int *src = p.partial + in_tile + (long long)c * (2 * kPjRows);
@@ -514,6 +519,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const long long t0 = clock64();
         while (!mbar_try_wait(drain, 0) && clock64() - t0 < kWaitCycles) {}
     }
+    __syncwarp();
     tc_fence_before();
     cluster_sync_all();
     if (warp == 1) {

@@ -50,6 +50,19 @@ def test_product(M, V, K, dtype):
     assert (wide[M] == -777).all() and (wide[:, :at] == -777).all() and (wide[:, at + V:] == -777).all()
 
 
+@pytest.mark.parametrize("V", [1, 15, 33, 255, 257, 1001, 4111])
+@pytest.mark.parametrize("M,K", [(256, 128), (130, 4000), (33, 20000)])
+def test_warps_with_lanes_beyond_the_last_weight_row(M, V, K):
+    """Several groups of tokens per warp, whole and cut tiles, a last weight tile of any width: lanes that have no
+    weight row are back for the next group's load."""
+    (q, s), (w, u) = codes(M, K, 1), codes(V, K, 2)
+    work = scores.project_workspace(M, V, K, DEV)
+    for dtype in (BF16, FP32):
+        want = plain(q, s, w, u, None, dtype)
+        for _ in range(3):
+            assert torch.equal(scores.project_int8(q, s, w, u, dtype=dtype, workspace=work), want)
+
+
 def test_largest_sums_are_exact():
     """127 * 127 * 2^17 stays below 2^31, and a float that is halfway goes to the even one."""
     K = 1 << 17
