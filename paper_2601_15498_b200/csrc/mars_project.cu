@@ -431,6 +431,8 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             more = project_next(p, walk, next);
             if (more) then = place(next);                    // its scales are on their way while this tile is written
             const int v = now.v, tok0 = now.tok0, n = now.n;
+            // lanes without a weight row leave a group early and have to be back before the next load from tensor memory
+            const bool ragged = v - lane + 31 >= p.V;
             __syncwarp();
             xs[lane] = now.x0;
             xs[lane + 32] = now.x1;
@@ -479,7 +481,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];
-                    __syncwarp();                            // (lanes without a weight row left the last group early)
+                    if (ragged) __syncwarp();
                     tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
                     project_emit<DT>(o, sum, reinterpret_cast<const float4 *>(xs + i), now.u, now.b, v, tok0 + c, n - c);
                 }
@@ -487,7 +489,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];
-                    __syncwarp();                            // (lanes without a weight row left the last group early)
+                    if (ragged) __syncwarp();
                     tc_ld16(taddr + c, reinterpret_cast<float (&)[kPjGroup]>(sum));
                     // two holders' parts at a time: 32 loads of a line each in flight
                     const int *src = p.partial + in_tile + (long long)c * (2 * kPjRows);
@@ -519,10 +521,12 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const long long t0 = clock64();
         while (!mbar_try_wait(drain, 0) && clock64() - t0 < kWaitCycles) {}
     }
-    __syncwarp();
     tc_fence_before();
-    cluster_sync_all();
+    // Single lanes of warps 0 and 1 come from loops of their own, so every thread arrives for itself (a __syncwarp() here,
+    // where 31 lanes wait for the whole kernel, made 3840 x 151936 x 4096 1.7 % slower).
+    cluster_sync_threads();
     if (warp == 1) {
+        __syncwarp();
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kPjTmemCols) : "memory");
     }
