@@ -49,14 +49,14 @@ mars_status_t mars_quantize_rows(const void *x, int64_t ldx, int dt, int64_t row
  *            Both matrices start on 16-byte boundaries, ldx and ldw are multiples of 16; K <= 2^17 is any.
  *   out      `dt` (MARS_BF16 or MARS_FP32) [M, ldo], any alignment; columns 0 .. V-1 are written.
  *   flags    MARS_COUNTERS_ZERO: the caller vouches that the first MARS_PROJECT_COUNTER_BYTES bytes of `workspace`
- *            were zeroed once and it was used by completed calls of this function only since; otherwise the call
- *            clears them (one stream operation more).
+ *            were zeroed once and it was used by completed calls of this function only since, whatever their
+ *            outcome; otherwise the call clears them (one stream operation more).
  *   workspace  mars_project_int8_workspace_bytes() bytes (0 for unsupported sizes; never less for a larger M,
  *            whatever V and K), 256-byte aligned; two calls that may overlap on the GPU need separate ones.
  *   The first call on a device sets function attributes: make it outside any stream capture.
  *   If a bounded device-side wait gives up (a fault in the pipeline, not a property of the data), logits
- *   that were not computed are NaN and the first uint32 of the workspace is MARS_SEQ_TIMEOUT; it is 0
- *   otherwise.  After such a call those bytes have to be zeroed before MARS_COUNTERS_ZERO is used again.
+ *   that were not computed are NaN and the first uint32 of the workspace is MARS_SEQ_TIMEOUT until the next
+ *   call; it is 0 otherwise.  The workspace serves further calls all the same.
  */
 size_t mars_project_int8_workspace_bytes(int64_t M, int V, int K);
 mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scale, const void *wq, int64_t ldw,

@@ -10,7 +10,8 @@
 // alignment.  Tiles go round by round over the pairs, token tiles first, so that the pairs that run together
 // share weight tiles in L2.  The tiles that are left for no whole round are cut along K: laid end to end in
 // 128-byte blocks of K, every pair takes an equal contiguous range.  The holders of a cut tile leave their
-// int32 sums in the workspace, and the last one to arrive adds them up.
+// int32 sums in the workspace, and the last one to arrive adds them up.  Every holder arrives, one that gave up
+// with a mark that makes the tile NaN, so the counters are zero after every call.
 //   warp 0      TMA: 128 weight rows and half of the tokens per K block into a shared-memory ring
 //   warp 1      allocates tensor memory, issues the MMAs (the leader's, for both blocks)
 //   warps 2..17 epilogue, from one of two accumulators while the next tile is computed
@@ -168,6 +169,7 @@ constexpr uint32_t kPjTmemCols = 512;
 constexpr size_t kPjRing = 200 * 1024;
 constexpr size_t kPjSmemBytes = kPjRing + 1024 /*align*/ + 256 /*barriers*/;
 constexpr size_t kPjHead = MARS_PROJECT_COUNTER_BYTES;   // workspace: status word, then a counter per (pair, block, warp)
+constexpr unsigned kPjLost = 1u << 16;      // in a counter of holders: one of them has no sums
 
 struct ProjectParams {
     int M, V, kblocks;
@@ -438,17 +440,10 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             xs[lane + 32] = now.x1;
             __syncwarp();
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, acc_phase, abort_flag, p.status));
-            if (!ok) {          // no result for what this block owes
-                if (v < p.V)
-                    for (int c = first; c < n; c += kPjStride)
-                        for (int j = 0; j < kPjGroup && c + j < n; ++j)
-                            put_logit<DT>(p.out, (long long)(tok0 + c + j) * p.ldo + v, NAN);
-                continue;
-            }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * kPjMaxTokens;
             const bool whole = s.cut < 0;
-            bool last = true;
+            bool last = true, lost = !ok;                    // a block that gave up owes NaN
             int c0 = 0, c1 = 0;                              // first and last pair that hold a part of the tile
             if (!whole) {
                 const long long t0 = (long long)s.cut * p.kblocks;
@@ -457,7 +452,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 // the first holder has the tile at its range's end, the others at their begin
                 int *dst = p.partial + (2ll * walk.pair + (walk.pair == c0 ? 1 : 0)) * slot + in_tile;
 #pragma unroll 1
-                for (int c = first; c < n; c += kPjStride) {
+                for (int c = first; c < n && ok; c += kPjStride) {
                     float x[kPjGroup];
                     tc_ld16(taddr + c, x);
 #pragma unroll
@@ -469,15 +464,23 @@ project_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 unsigned seen = 0;
                 if (lane == 0) {
                     __threadfence();
-                    seen = atomicAdd(counter, 1u);
-                    if (seen == (unsigned)(c1 - c0)) *counter = 0;       // as it was found: the workspace serves the next call
+                    seen = atomicAdd(counter, ok ? 1u : kPjLost + 1u);   // also without sums: the others count on it
+                    if (seen % kPjLost == (unsigned)(c1 - c0)) *counter = 0;     // as it was found: the workspace serves the next call
                     __threadfence();
                 }
                 __syncwarp();
-                last = __shfl_sync(0xffffffffu, seen, 0) == (unsigned)(c1 - c0);
+                seen = __shfl_sync(0xffffffffu, seen, 0);
+                last = seen % kPjLost == (unsigned)(c1 - c0);
+                lost = lost || seen >= kPjLost;
             }
             // (two copies of the loop: sums that may still change would be moved between registers once more)
-            if (whole) {
+            if (lost) {
+                if (last && v < p.V)
+                    for (int c = first; c < n; c += kPjStride)
+                        for (int j = 0; j < kPjGroup && c + j < n; ++j)
+                            put_logit<DT>(p.out, (long long)(tok0 + c + j) * p.ldo + v, NAN);
+                if (!ok) continue;
+            } else if (whole) {
 #pragma unroll 1
                 for (int c = first, i = 0; c < n; c += kPjStride, i += kPjGroup) {
                     int sum[kPjGroup];

@@ -141,7 +141,8 @@ def quantize_rows(x: torch.Tensor, out=None):
 
 def project_workspace(tokens: int, V: int, K: int, device) -> torch.Tensor:
     """A workspace for project_int8 calls of up to so many tokens (V and K do not matter to its size), its counters
-    zeroed; it serves any number of calls that do not overlap."""
+    zeroed; it serves any number of calls that do not overlap.  Its first int32 is the last call's status: 0, or 3
+    (timeout) where a wait on the device gave up and logits are NaN."""
     need = int(lib().mars_project_int8_workspace_bytes(tokens, V, K))
     if need == 0:
         raise MarsError("unsupported sizes")
@@ -155,7 +156,7 @@ def project_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_sc
     """mars_project_int8 on the current stream: logits [tokens, V] of codes xq [tokens, K] and wq [V, K] with
     their scales (quantize_rows of the hidden states, and once of the weights).  `out` [tokens, >= V] (its dtype
     is used).  `workspace` comes from project_workspace and is used by these calls only; without one, a call
-    allocates and clears its own."""
+    allocates and clears its own.  Logits that a wait which gave up left uncomputed are NaN."""
     M, K, ldx, index = _codes(xq, x_scale, "xq")
     V, wk, ldw, wi = _codes(wq, w_scale, "wq")
     if wk != K or wi != index:

@@ -315,6 +315,31 @@ def test_pairs_that_give_up_leave_nan_and_a_status(M, V, K):
     assert int(work[:4].view(torch.int32)) == 0
 
 
+@pytest.mark.parametrize("M,V,K", [(40, 900, 6000), (300, 25000, 512), (1, 20000, 4096), (256, 4096, 4096)])
+def test_workspace_serves_calls_after_one_whose_pairs_gave_up(M, V, K):
+    """The counters come back to zero whichever pairs give up, so a call that follows has every logit right without any
+    clearing, and a status of its own."""
+    (q, s), (w, u) = codes(M, K, 1), codes(V, K, 2)
+    (q2, s2) = codes(M, K, 3)
+    want, want2 = plain(q, s, w, u, None, FP32), plain(q2, s2, w, u, None, FP32)
+    work = scores.project_workspace(M, V, K, DEV)
+    counters = work[256:scores.PROJECT_COUNTER_BYTES].view(torch.int32)
+    for first in (1, 2, 3, 17, 40, 60, 74, 75):
+        try:
+            mars.test_hook(mars.HOOK_PROJECT_GIVE_UP, first)
+            got = scores.project_int8(q, s, w, u, dtype=FP32, workspace=work)
+            torch.cuda.synchronize()
+        finally:
+            mars.test_hook(mars.HOOK_PROJECT_GIVE_UP, 0)
+        gone = torch.isnan(got)
+        assert torch.equal(got[~gone], want[~gone]), first
+        assert int(work[:4].view(torch.int32)) == (3 if gone.any() else 0)
+        assert not counters.any(), first
+        got = scores.project_int8(q2, s2, w, u, dtype=FP32, workspace=work)
+        assert torch.equal(got, want2), first
+        assert int(work[:4].view(torch.int32)) == 0
+
+
 def test_refusals_of_the_binding():
     (q, s), (w, u) = codes(4, 64, 1), codes(10, 64, 2)
     good = scores.project_workspace(4, 10, 64, DEV)
