@@ -178,6 +178,9 @@ def _dtype_code(t: torch.Tensor) -> int:
 def _dev_i32(x, device) -> torch.Tensor:
     t = torch.as_tensor(x)
     if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
+        if t.dtype in (torch.int64, torch.uint32, torch.uint64):
+            # what 32 bits do not hold stays out of every range (2^32 + 5 is no token, and not token 5)
+            t = t.to(torch.int64).clamp(-2 ** 31, 2 ** 31 - 1)
         t = t.to(device=device, dtype=torch.int32).contiguous()
     return t
 

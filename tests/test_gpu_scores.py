@@ -348,6 +348,20 @@ def test_numbers_of_other_kinds_as_arguments():
     assert one["logprob"].shape == (1, 0) and torch.isfinite(one["entropy"]).all()
 
 
+def test_ids_beyond_32_bits_are_outside():
+    z = rows_of(6, 500, FP32, 1)
+    tok = torch.tensor([[3, 2 ** 32 + 3], [2 ** 32, 7], [-2 ** 32, 2 ** 40 + 1]] * 2, device=DEV)
+    ids = torch.tensor([0, 1, 2 ** 32, 2, 2 ** 33 + 1, -2 ** 32], device=DEV)
+    got = scores.token_logprobs(z, tok, rows=ids)
+    ref = sc.reference(z)["logp"]
+    want = torch.zeros((6, 2), dtype=torch.float64, device=DEV)
+    want[0, 0], want[1, 1], want[3, 0] = ref[0, 3], ref[1, 7], ref[2, 3]
+    assert ((got["logprob"].double() - want).abs() <= sc.UNIT * (sc.SUM + 100)).all() and ((got["logprob"] == 0) == (want == 0)).all()
+    assert (got["entropy"][[2, 4, 5]] == 0).all() and (got["entropy"][[0, 1, 3]] > 0).all()
+    grad = scores.token_logprobs_backward(z, tok, scores.token_logprobs(z, tok), torch.ones((6, 2), device=DEV))
+    assert (grad[2] == 0).all() and (grad[5] == 0).all() and (grad[0] != 0).any()
+
+
 def test_refusals_of_the_binding():
     z = torch.zeros((4, 100), device=DEV)
     tok = torch.zeros((4, 2), dtype=torch.int32, device=DEV)

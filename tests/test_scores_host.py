@@ -2,7 +2,9 @@
 import ctypes
 import math
 
+import numpy as np
 import pytest
+import torch
 
 from paper_2601_15498_b200 import mars
 
@@ -83,3 +85,17 @@ def test_project_refusals_and_workspace(lib):
         assert f(**{k: bad}) == UNSUPPORTED, (k, bad)
     for k, bad in (("work", N), ("work", ctypes.c_void_p(8192 + 128)), ("bytes", need - 1)):
         assert f(**{k: bad}) == WORKSPACE, (k, bad)
+
+
+@pytest.mark.parametrize("kind", ["numpy", "torch", "list", "uint64", "strided"])
+def test_ids_beyond_32_bits_stay_outside(kind):
+    ids = [0, 5, -1, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 62 + 7] + ([] if kind == "uint64" else [-2 ** 31 - 1, -2 ** 32, -2 ** 40 + 3])
+    x = {"numpy": lambda: np.array(ids), "torch": lambda: torch.tensor(ids), "list": lambda: ids,
+         "uint64": lambda: np.array([max(i, 0) for i in ids] + [2 ** 63 + 5], dtype=np.uint64),
+         "strided": lambda: torch.tensor(ids)[:, None].expand(len(ids), 3)[:, 1]}[kind]()
+    t = mars._dev_i32(x, torch.device("cpu"))
+    assert t.dtype == torch.int32 and t.is_contiguous()
+    for got, i in zip(t.tolist(), ids):
+        want = max(i, 0) if kind == "uint64" else i
+        assert got == want if -2 ** 31 <= want < 2 ** 31 else (got == 2 ** 31 - 1 if want > 0 else got == -2 ** 31)
+    assert kind != "uint64" or t[-1] < 0
