@@ -50,6 +50,25 @@ def test_product(M, V, K, dtype):
     assert (wide[M] == -777).all() and (wide[:, :at] == -777).all() and (wide[:, at + V:] == -777).all()
 
 
+@pytest.mark.parametrize("M,V,K", [(33, 640, 4096), (256, 4096, 512), (700, 256, 16), (64, 20000, 2048), (40, 900, 6000),
+                                   (1025, 130, 8192), (300, 25000, 512), (17, 2, 100), (272, 1000, 129), (1, 151936, 256)])
+@pytest.mark.parametrize("pad", [0, 2, 5])
+@pytest.mark.parametrize("biased", [False, True])
+def test_pairs_of_logits_in_one_word(M, V, K, pad, biased):
+    """bf16 logits of even V, row stride and 4-byte alignment are written two at a time: whole and partial groups of tokens,
+    several groups and tiles, whole and cut tiles; a padding of 5 takes the other way to the same bits."""
+    (q, s), (w, u) = codes(M, K, M + K), codes(V, K, V + 7)
+    bias = torch.randn((V,), generator=gen(3), device=DEV) if biased else None
+    want = plain(q, s, w, u, bias, BF16)
+    wide = torch.full((M + 2, V + pad), -777.0, dtype=BF16, device=DEV)
+    for at in (0,) if not pad else (0, pad - 1, pad):
+        wide.fill_(-777.0)
+        out = wide[1:M + 1, at:at + V]
+        scores.project_int8(q, s, w, u, bias=bias, out=out)
+        assert torch.equal(out, want)
+        assert (wide[[0, -1]] == -777).all() and (wide[:, :at] == -777).all() and (wide[:, at + V:] == -777).all()
+
+
 @pytest.mark.parametrize("V", [1, 15, 33, 255, 257, 1001, 4111])
 @pytest.mark.parametrize("M,K", [(256, 128), (130, 4000), (33, 20000)])
 def test_warps_with_lanes_beyond_the_last_weight_row(M, V, K):
