@@ -224,6 +224,8 @@ def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logpr
     stats, entropy = _checked(forward["stats"], "forward['stats']", (R, 2), _F32, index), forward.get("entropy")
     if tok is None or g.numel() != R * J or (h is not None and (h.numel() != R or entropy is None)):
         raise MarsError("grad_logprob must have the shape of tok, grad_entropy one value a row")
+    if J == 0 and h is not None:         # no tokens, the entropy's gradient alone: a place without a token
+        tok, g, J = torch.full((R, 1), -1, dtype=_I32, device=logits.device), torch.zeros((R, 1), dtype=_F32, device=logits.device), 1
     if entropy is not None:
         _checked(entropy, "forward['entropy']", (R,), _F32, index)
     if out is None:

@@ -348,6 +348,19 @@ def test_numbers_of_other_kinds_as_arguments():
     assert one["logprob"].shape == (1, 0) and torch.isfinite(one["entropy"]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_gradient_of_the_entropy_alone(dtype):
+    z = rows_of(5, 3001, dtype, 2).contiguous().requires_grad_()
+    none = torch.empty((5, 0), dtype=torch.int32, device=DEV)
+    lp, H = scores.logprobs(z, none, 0.8)
+    assert lp.shape == (5, 0)
+    w = torch.randn((5,), generator=gen(1), device=DEV)
+    (H * w).sum().backward()
+    tok = torch.full((5, 1), -1, dtype=torch.int32, device=DEV)
+    sc.check_grad(z.detach(), z.grad, sc.reference(z.detach(), tok, 0.8), tok, torch.zeros((5, 1), device=DEV), w, 0.8)
+    assert (z.grad != 0).any(1).all()
+
+
 def test_ids_beyond_32_bits_are_outside():
     z = rows_of(6, 500, FP32, 1)
     tok = torch.tensor([[3, 2 ** 32 + 3], [2 ** 32, 7], [-2 ** 32, 2 ** 40 + 1]] * 2, device=DEV)
