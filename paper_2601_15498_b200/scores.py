@@ -222,7 +222,8 @@ def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logpr
     g = _dev_f32(grad_logprob, logits.device)
     h = None if grad_entropy is None else _dev_f32(grad_entropy, logits.device)
     stats, entropy = _checked(forward["stats"], "forward['stats']", (R, 2), _F32, index), forward.get("entropy")
-    if tok is None or g.numel() != R * J or (h is not None and (h.numel() != R or entropy is None)):
+    # (a number of weights is not enough: [J, rows] would give every row those of others; in one dimension they are row by row)
+    if tok is None or (g.shape != (R, J) and g.shape != (R * J,)) or (h is not None and (h.numel() != R or entropy is None)):
         raise MarsError("grad_logprob must have the shape of tok, grad_entropy one value a row")
     if J == 0 and h is not None:         # no tokens, the entropy's gradient alone: a place without a token
         tok, g, J = torch.full((R, 1), -1, dtype=_I32, device=logits.device), torch.zeros((R, 1), dtype=_F32, device=logits.device), 1

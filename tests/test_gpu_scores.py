@@ -361,6 +361,21 @@ def test_gradient_of_the_entropy_alone(dtype):
     assert (z.grad != 0).any(1).all()
 
 
+def test_weights_of_another_shape_are_refused():
+    z, tok = rows_of(4, 100, FP32, 1), tokens(4, 2, 100, 1)
+    f, f1 = scores.token_logprobs(z, tok), scores.token_logprobs(z, tok[:, 0])
+    g, h = torch.randn((4, 2), generator=gen(1), device=DEV), torch.randn((4,), generator=gen(2), device=DEV)
+    for bad in ((g.T, None), (g[:, 0], None), (g.view(2, 4), h), (g, h[:3]), (g[:, :1], h)):
+        with pytest.raises(mars.MarsError):
+            scores.token_logprobs_backward(z, tok, f, *bad)
+    with pytest.raises(mars.MarsError):
+        scores.token_logprobs_backward(z, tok[:, 0], f1, g[:, :1].T)
+    assert torch.equal(scores.token_logprobs_backward(z, tok, f, g.flatten(), h[:, None]), scores.token_logprobs_backward(z, tok, f, g, h))
+    one = scores.token_logprobs_backward(z, tok[:, 0], f1, g[:, 0])
+    for t, w in ((tok[:, 0], g[:, :1]), (tok[:, :1], g[:, 0]), (tok[:, :1], g[:, :1])):
+        assert torch.equal(scores.token_logprobs_backward(z, t, f1, w), one)
+
+
 def test_ids_beyond_32_bits_are_outside():
     z = rows_of(6, 500, FP32, 1)
     tok = torch.tensor([[3, 2 ** 32 + 3], [2 ** 32, 7], [-2 ** 32, 2 ** 40 + 1]] * 2, device=DEV)
