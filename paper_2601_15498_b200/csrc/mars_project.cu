@@ -605,11 +605,15 @@ static int project_pairs()
     at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, project_kernel<MARS_BF16>, &cfg) != cudaSuccess || n < 1) {
-        (void)cudaGetLastError();
-        return 0;
-    }
+    if (cudaOccupancyMaxActiveClusters(&n, project_kernel<MARS_BF16>, &cfg) != cudaSuccess || n < 1) return 0;
     return g_pj_pairs[dev] = n < kPjPairs ? n : kPjPairs;
+}
+
+// The runtime's record of the error is cleared, so that no later call takes it for its own.
+static mars_status_t project_failed()
+{
+    (void)cudaGetLastError();
+    return MARS_ERR_CUDA;
 }
 
 }  // namespace mars
@@ -663,7 +667,7 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
     p.M = (int)M; p.V = V;
     p.kblocks = (K + kPjBK - 1) / kPjBK;
     const int resident = project_pairs();
-    if (resident < 1) return MARS_ERR_CUDA;
+    if (resident < 1) return project_failed();
     const ProjectPlan plan = project_plan(M, V, K, resident);
     p.tokens = plan.tokens;
     p.n_ttiles = (int)((M + p.tokens - 1) / p.tokens);
@@ -680,17 +684,17 @@ mars_status_t mars_project_int8(const void *xq, int64_t ldx, const float *x_scal
     CUtensorMap map_w, map_x;
     if (!tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, wq, (uint64_t)V, (uint64_t)K, (uint64_t)ldw, kPjRows, kPjBK) ||
         !tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, xq, (uint64_t)M, (uint64_t)K, (uint64_t)ldx, (uint32_t)p.tokens / 2, kPjBK))
-        return MARS_ERR_CUDA;
+        return project_failed();
     const int give_up = hook(kHookProjectGiveUp);
     p.give_up = give_up ? give_up - 1 : INT_MAX;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (give_up && cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return MARS_ERR_CUDA;
-    if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kPjHead, st) != cudaSuccess) return MARS_ERR_CUDA;
+    if (give_up && cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return project_failed();
+    if (!(flags & MARS_COUNTERS_ZERO) && cudaMemsetAsync(workspace, 0, kPjHead, st) != cudaSuccess) return project_failed();
     void (*kernel)(const CUtensorMap, const CUtensorMap, const ProjectParams) =
         dt == MARS_BF16 ? project_kernel<MARS_BF16> : project_kernel<MARS_FP32>;
     const cudaError_t e = launch_pdl(hook(kHookNoOverlap) == 0, kernel, dim3(2 * plan.pairs), dim3(kPjThreads), kPjSmemBytes, st,
                                      map_w, map_x, p);
-    if (e != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
+    if (e != cudaSuccess) return project_failed();
     return MARS_OK;
 }
 

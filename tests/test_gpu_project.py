@@ -1,5 +1,7 @@
 """The 8-bit output projection on the device.  Codes, sums and every rounding of the call are defined, so all
 comparisons are bit for bit."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -357,6 +359,33 @@ def test_workspace_serves_calls_after_one_whose_pairs_gave_up(M, V, K):
         got = scores.project_int8(q2, s2, w, u, dtype=FP32, workspace=work)
         assert torch.equal(got, want2), first
         assert int(work[:4].view(torch.int32)) == 0
+
+
+def test_a_failed_call_leaves_no_error_behind():
+    """A stream operation that the runtime refuses (on the legacy stream, while a stream that waits for it is captured) is
+    that call's error and no later one's."""
+    with open("/proc/self/maps") as f:
+        rt = ctypes.CDLL(next(line.split()[-1] for line in f if "libcudart" in line))
+    (q, s), (w, u) = codes(4, 64, 1), codes(10, 64, 2)
+    want = scores.project_int8(q, s, w, u)
+    out, work = torch.empty_like(want), scores.project_workspace(4, 10, 64, DEV)
+    z = torch.randn((3, 100), generator=gen(1), device=DEV)
+    val, idx = mars.topk_rows(z, 2)
+    torch.cuda.synchronize()
+    stream, graph = ctypes.c_void_p(), ctypes.c_void_p()
+    assert rt.cudaStreamCreate(ctypes.byref(stream)) == 0
+    assert rt.cudaStreamBeginCapture(stream, 0) == 0
+    try:
+        code = mars.lib().mars_project_int8(q.data_ptr(), q.stride(0), s.data_ptr(), w.data_ptr(), w.stride(0), u.data_ptr(), None, 4, 10,
+                                            64, out.data_ptr(), 10, mars.BF16, 0, work.data_ptr(), work.nbytes, None)
+    finally:
+        rt.cudaStreamEndCapture(stream, ctypes.byref(graph))
+        rt.cudaStreamDestroy(stream)
+        rt.cudaGetLastError()
+    assert code == 4                                                         # MARS_ERR_CUDA
+    again = mars.topk_rows(z, 2)
+    assert torch.equal(again[0], val) and torch.equal(again[1], idx)
+    assert torch.equal(scores.project_int8(q, s, w, u), want)
 
 
 def test_refusals_of_the_binding():
