@@ -643,10 +643,10 @@ static mars_status_t lm_launch_gemm(const void *hidden, const void *w_vocab, con
     // Function attributes and occupancy belong to a device: set them up once for each device
     // that this process calls from, with that device current.
     LmDeviceState dstate;
-    if (!lm_device_state(&dstate)) return MARS_ERR_CUDA;
+    if (!lm_device_state(&dstate)) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     const int sms = dstate.sms;
 
-    if (cudaMemsetAsync(p.status, 0, 256, st) != cudaSuccess) return MARS_ERR_CUDA;
+    if (cudaMemsetAsync(p.status, 0, 256, st) != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     if (lm_pair_mode()) {
         // persistent pairs: never launch more clusters than can be resident together
         const int max_pairs = dstate.max_pairs;
@@ -697,7 +697,7 @@ mars_status_t mars_selftest_bounded_wait(int64_t budget_cycles, void *scratch32,
     if (!scratch32 || ((uintptr_t)scratch32 & 7) || budget_cycles < 1 || budget_cycles > 2000000000ll)
         return MARS_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(scratch32, 0, 32, st) != cudaSuccess) return MARS_ERR_CUDA;
+    if (cudaMemsetAsync(scratch32, 0, 32, st) != cudaSuccess) { (void)cudaGetLastError(); return MARS_ERR_CUDA; }
     mars::bounded_wait_selftest_kernel<<<1, 32, 0, st>>>((unsigned *)scratch32, (long long)budget_cycles,
                                                          (long long *)((char *)scratch32 + 8));
     return cudaGetLastError() == cudaSuccess ? MARS_OK : MARS_ERR_CUDA;

@@ -85,8 +85,11 @@ extern "C" mars_status_t mars_top2_histograms(const float *top2_val, int64_t row
     p.edge[0] = INFINITY;
     for (int k = 1; k < kMaxBins; ++k) p.edge[k] = k < nbins ? (float)(-log((double)k / (double)nbins)) : 0.0f;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(hist, 0, sizeof(uint32_t) * 3 * (size_t)nbins, st) != cudaSuccess) return MARS_ERR_CUDA;
-    if (cudaMemsetAsync(outliers, 0, sizeof(uint32_t) * 3, st) != cudaSuccess) return MARS_ERR_CUDA;
+    if (cudaMemsetAsync(hist, 0, sizeof(uint32_t) * 3 * (size_t)nbins, st) != cudaSuccess ||
+        cudaMemsetAsync(outliers, 0, sizeof(uint32_t) * 3, st) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MARS_ERR_CUDA;
+    }
     if (rows == 0) return MARS_OK;
     long long blocks = (rows + 255) / 256;
     if (blocks > 148 * 8) blocks = 148 * 8;

@@ -251,8 +251,10 @@ static mars_status_t run(const void *logits, int64_t ld, mars_dtype_t dt, const 
     // Arrival counters start at zero.  Every sequence's last block puts its counter back to
     // zero, so a caller that knows the counters are clean may skip the memset node.
     if (!(flags & MARS_COUNTERS_ZERO) &&
-        cudaMemsetAsync(p.counters, 0, (size_t)B * sizeof(unsigned), st) != cudaSuccess)
+        cudaMemsetAsync(p.counters, 0, (size_t)B * sizeof(unsigned), st) != cudaSuccess) {
+        (void)cudaGetLastError();
         return MARS_ERR_CUDA;
+    }
     const unsigned grid = (unsigned)(R * sp.S);
     // dynamic shared memory: the tail's arrays, then (if it fits in 48 KB) room for N*S records
     const size_t tail_bytes = (tail_smem_bytes(N) + 15) / 16 * 16;

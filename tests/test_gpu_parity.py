@@ -3,6 +3,7 @@
 Bar: bit-exact for token ids, lengths, paths, flags and statuses; the fp32 top-2 values are
 compared as bit patterns too (both sides take every decision in fp32).
 """
+import ctypes
 import os
 
 import numpy as np
@@ -573,3 +574,40 @@ def test_default_calls_are_ordered_behind_a_producer_that_rewrites_the_logits():
         assert np.array_equal(o_topk[i][0].cpu().numpy().view(np.uint32), ref_topk[j][0].view(np.uint32)), i
         ts.compare(mars.to_host(o_st[i]), ref_st[j], ws[0].tok, ws[0].parent,
                    ws[j].logits.float().cpu().numpy().astype(np.float64), u, 1.0, f"round {i} stochastic")
+
+
+@pytest.mark.parametrize("entry", ["verify_tree", "lmhead", "telemetry"])
+def test_a_refused_stream_operation_is_no_later_calls_error(entry):
+    """The legacy stream takes no work while a stream that waits for it is captured: the call that meets this reports
+    it, the next one on a sound stream does not."""
+    with open("/proc/self/maps") as f:
+        rt = ctypes.CDLL(next(line.split()[-1] for line in f if "libcudart" in line))
+    w = synth.tree_workload("refused", 2, 6, 3, 2, 4000, torch.bfloat16, DEV, 5, 0.9, 3.0, 15.0, 30.0, 0.3)
+    tok, par = torch.as_tensor(w.tok, device=DEV), torch.as_tensor(w.parent, device=DEV)
+    o, work = mars.alloc_outputs(2, 6, 5, DEV), torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    hidden = torch.zeros((12, 64), dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros((4000, 64), dtype=torch.bfloat16, device=DEV)
+    mars.lmhead_verify(hidden, table, None, tok, par, 0.9)
+    val, idx = mars.topk_rows(w.logits, 3)
+    outs = [o[k].data_ptr() for k in ("accept_len", "out_tokens", "path_nodes", "out_len")]
+    top2 = torch.zeros((12, 2), device=DEV)
+    hist, outliers = torch.zeros(30, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    L = mars.lib()
+    call = {"verify_tree": lambda: L.mars_verify_tree(w.logits.data_ptr(), 4000, mars.BF16, tok.data_ptr(), par.data_ptr(), 2, 6, 4000, 0.9,
+                                                      0, *outs, 5, o["seq_status"].data_ptr(), None, work.data_ptr(), work.nbytes, None),
+            "lmhead": lambda: L.mars_lmhead_verify(hidden.data_ptr(), table.data_ptr(), None, 64, tok.data_ptr(), par.data_ptr(), 2, 6, 4000,
+                                                   0.9, 0, *outs, 5, o["seq_status"].data_ptr(), None, work.data_ptr(), work.nbytes, None),
+            "telemetry": lambda: L.mars_top2_histograms(top2.data_ptr(), 12, 0.0, 1.0, 10, hist.data_ptr(), outliers.data_ptr(), None)}[entry]
+    torch.cuda.synchronize()
+    stream, graph = ctypes.c_void_p(), ctypes.c_void_p()
+    assert rt.cudaStreamCreate(ctypes.byref(stream)) == 0
+    assert rt.cudaStreamBeginCapture(stream, 0) == 0
+    try:
+        code = call()
+    finally:
+        rt.cudaStreamEndCapture(stream, ctypes.byref(graph))
+        rt.cudaStreamDestroy(stream)
+        rt.cudaGetLastError()
+    assert code == 4
+    again = mars.topk_rows(w.logits, 3)
+    assert torch.equal(again[0], val) and torch.equal(again[1], idx)
