@@ -113,7 +113,8 @@ def _codes(q, scale, name: str):
         raise MarsError(f"{name}: codes must have unit inner stride")
     if scale.dtype is not _F32 or scale.shape != (rows,) or not scale.is_contiguous() or scale.get_device() != index:
         raise MarsError(f"{name}: scales must be contiguous float32, one a row, beside the codes")
-    return rows, K, ld if rows > 1 else max(ld, -(-K // 16) * 16), index
+    # a single row has no second one to be apart from
+    return rows, K, ld if rows > 1 else -(-K // 16) * 16, index
 
 
 def quantize_rows(x: torch.Tensor, out=None):

@@ -361,6 +361,20 @@ def test_workspace_serves_calls_after_one_whose_pairs_gave_up(M, V, K):
         assert int(work[:4].view(torch.int32)) == 0
 
 
+def test_one_row_of_codes_out_of_a_matrix_of_any_stride():
+    """A single row's stride is no distance between rows: 1 token, 1 weight row, 1 quantised row."""
+    (q, s), (w, u) = codes(1, 100, 1), codes(40, 100, 2)
+    odd = torch.zeros((3, 201), dtype=torch.int8, device=DEV)
+    odd[0, :100] = q[0]
+    assert torch.equal(scores.project_int8(odd[:1, :100], s, w, u), plain(q, s, w, u, None, BF16))
+    assert torch.equal(scores.project_int8(w, u, odd[:1, :100], s, dtype=FP32), plain(w, u, q, s, None, FP32))
+    x = torch.randn((1, 100), generator=gen(3), device=DEV)
+    want = scores.quantize_rows(x)
+    odd.fill_(99)
+    got = scores.quantize_rows(x, out=(odd[:1, :100], torch.empty((1,), device=DEV)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and (odd[1:] == 99).all() and (odd[0, 100:] == 99).all()
+
+
 def test_a_failed_call_leaves_no_error_behind():
     """A stream operation that the runtime refuses (on the legacy stream, while a stream that waits for it is captured) is
     that call's error and no later one's."""
