@@ -575,9 +575,13 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
     const float h = p.h ? p.h[row] : 0.0f;
     float a = -g, b = 0.0f;
     if (p.h) { a = -fmaf(h, p.entropy[row] - logf(s), g); b = -(h * kLn2); }
+    const float as = a / s, bs = b / s;
     if (ts < INFINITY) { a /= ts; b /= ts; }
-    else { a = a / s / p.temperature; b = b / s / p.temperature; }       // T s passes fp32's range, the quotient need not
+    else { a = as / p.temperature; b = bs / p.temperature; }             // T s passes fp32's range, the quotient need not
     if (!ok) { a = 0.0f; b = 0.0f; }
+    // factors near the range's end (tiny T): 2^x (a + b x) is divided by T after the product, since infinity * 0 is no 0
+    const bool far = !(fabsf(a) < 0x1p100f && fabsf(b) < 0x1p100f);
+    if (far) { a = as; b = bs; }
 
     // the tokens' logits, before anything is overwritten
     bool hit = false;
@@ -589,6 +593,7 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
 
     GradLine line;
     soft_reference<DT>(line.f, m, c, p.reach);
+    if (far) { line.f.fast = false; line.f.d = 0.0f; }
     const SoftState &f = line.f;
     const float fd = ex2f(-f.d);
     line.m = m; line.c = c; line.a = a; line.b = b;
@@ -597,7 +602,7 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
     if (((a0 ^ b0) & 15) || !ok || !f.fast) {
         // rows that lie differently on 16-byte boundaries, and rows without fast form: one by one
         for (int i = lo + tid; i < hi; i += kTkThreads)
-            store_scalar<DT>(grow, i, ok ? grad_term<DT>(E::scalar(zrow, i), line) : 0.0f);
+            store_scalar<DT>(grow, i, ok ? grad_term<DT>(E::scalar(zrow, i), line) / (far ? p.temperature : 1.0f) : 0.0f);
     } else {
         const int nhead = min((int)(((16 - (a0 & 15)) & 15) / E::kBytes), hi - lo);
         const int vlo = lo + nhead, nvec = (hi - vlo) / E::kVec, tlo = vlo + nvec * E::kVec, ntail = hi - tlo;
@@ -644,7 +649,8 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
         if (!first) continue;
         float own = 0.0f;
         for (int i = j; i < p.J; ++i) own += tok[i] == t ? gj[i] : 0.0f;
-        store_scalar<DT>(grow, t, grad_term<DT>(s_z[j], line) + own / p.temperature);
+        const float term = grad_term<DT>(s_z[j], line);
+        store_scalar<DT>(grow, t, far ? (term + own) / p.temperature : term + own / p.temperature);
     }
 }
 

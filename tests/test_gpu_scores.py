@@ -155,6 +155,24 @@ def test_gradient_where_temperature_times_sum_overflows(T, dtype):
         assert (grad != 0).all()
 
 
+@pytest.mark.parametrize("T", [1e-34, 1e-36, 4e-38])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_gradient_whose_factors_end_the_range(T, dtype):
+    """g / T passes fp32's largest number; what is multiplied by a probability of 0 is 0 all the same, a nearly certain
+    token's gradient finite."""
+    z, tok = rows_of(4, 1001, dtype, 4, spread=2 * T), tokens(4, 3, 1001, 1)
+    z[1] = 0.0                                                         # uniform: every part is g / (1001 T)
+    z[2, ::2] = float("-inf")
+    z[3] = -1.0; z[3, 5] = 1.0; tok[3] = 5                             # certain
+    got = scores.token_logprobs(z, tok, temperature=T)
+    ref = sc.check_forward(z, got, tok, T)
+    g, h = torch.randn((4, 3), generator=gen(2), device=DEV) * 40, torch.randn((4,), generator=gen(3), device=DEV) * 40
+    for ge in (None, h):
+        grad = scores.token_logprobs_backward(z, tok, got, g, ge, temperature=T)
+        assert not torch.isnan(grad).any() and (grad[3] == 0).all() and (grad[2, ::2] == 0).all()
+        sc.check_grad(z, grad, ref, tok, g, ge, T)
+
+
 def test_alternatives_follow_the_order_of_topk_rows():
     for V, dtype in ((4099, BF16), (4099, FP32), (37, FP32)):
         z = special_rows(V, dtype)
