@@ -379,6 +379,30 @@ def test_gradient_of_the_entropy_alone(dtype):
     assert (z.grad != 0).any(1).all()
 
 
+def test_captured_training_step():
+    """Forward and backward of the autograd form in one graph, replayed over other logits, tokens and weights."""
+    z, tok = rows_of(30, 5001, BF16, 2).contiguous().requires_grad_(), tokens(30, 2, 5001, 1)
+    w, c = torch.randn((30, 2), generator=gen(1), device=DEV), torch.randn((30,), generator=gen(2), device=DEV)
+
+    def step():
+        lp, H = scores.logprobs(z, tok, 0.9)
+        return torch.autograd.grad((lp * w).sum() + (H * c).sum(), z)[0]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grad = step()
+    for i in range(3):
+        with torch.no_grad():
+            z.copy_(rows_of(30, 5001, BF16, 30 + i))
+        tok.copy_(tokens(30, 2, 5001, 40 + i))
+        w.copy_(torch.randn((30, 2), generator=gen(50 + i), device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        sc.check_grad(z.detach(), grad, sc.reference(z.detach(), tok, 0.9), tok, w, c, 0.9)
+        assert torch.equal(grad, step())
+
+
 def test_weights_of_another_shape_are_refused():
     z, tok = rows_of(4, 100, FP32, 1), tokens(4, 2, 100, 1)
     f, f1 = scores.token_logprobs(z, tok), scores.token_logprobs(z, tok[:, 0])
