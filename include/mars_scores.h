@@ -100,7 +100,8 @@ mars_status_t mars_token_logprobs(const void *logits, int64_t ld, mars_dtype_t d
  *   stats, entropy   of the forward call on these logits (entropy may be NULL if grad_entropy is).
  *   grad_logprob     float [rows, J]; grad_entropy float [rows] or NULL.
  *   grad             [rows, ld_grad] of `dt`, columns 0 .. V-1 are written; may be the logits themselves
- *                    (then ld_grad == ld), may not overlap them otherwise.
+ *                    (then ld_grad == ld), may not overlap them otherwise.  Rows of it that lie on 16-byte
+ *                    boundaries like the logits' rows are written in 16-byte steps, others an element at a time.
  */
 mars_status_t mars_token_logprobs_backward(const void *logits, int64_t ld, mars_dtype_t dt, int64_t rows, int V,
                                            float temperature, const int32_t *tok, int J, const float *stats,

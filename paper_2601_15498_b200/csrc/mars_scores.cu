@@ -356,6 +356,7 @@ __device__ __forceinline__ float row_logprob(const RowScore &r, float z, float t
 
 // Forward: a cluster of S blocks (S = 1: a block) streams one row, each block a contiguous slice; the
 // block of rank 0 joins the slices' (m, s, u) and lists through distributed shared memory and writes.
+// Four blocks per SM leave 64 registers; fp32 with alternatives spills 18 bytes at that.
 template <int DT, bool TOP>
 __global__ void __launch_bounds__(kTkThreads, 4) logprob_kernel(const LogprobParams p)
 {
@@ -518,7 +519,8 @@ struct GradParams {
 };
 
 // Vectors per thread at a time, blocks per SM.  2048 rows of 151936 (bf16), us: 2 at 6 blocks 205, at 5 209, at 7 216;
-// 4 at 6 blocks 210, at 5 (47 registers) 217; 1 at 6 blocks 234, at 8 224.  Stores that stay in L2 228.
+// 4 at 6 blocks 210, at 5 (47 registers) 217; 1 at 6 blocks 234, at 8 224.  Stores that stay in L2 228.  Six blocks leave
+// 40 registers, at which 4 bytes are spilled.
 constexpr int kGrU = 2, kGrBlocks = 6;
 
 template <int DT>
@@ -600,7 +602,9 @@ __global__ void __launch_bounds__(kTkThreads, kGrBlocks) logprob_grad_kernel(con
     line.fa = fd * fmaf(-b, f.d, a); line.fb = fd * b;
     const uintptr_t a0 = (uintptr_t)(zrow + (size_t)lo * E::kBytes), b0 = (uintptr_t)(grow + (size_t)lo * E::kBytes);
     if (((a0 ^ b0) & 15) || !ok || !f.fast) {
-        // rows that lie differently on 16-byte boundaries, and rows without fast form: one by one
+        // rows that lie differently on 16-byte boundaries, and rows without fast form: one by one.  The former are 7 of 8
+        // bf16 rows where logits of odd stride get a dense gradient: 2048 rows of 151936 756 us, 1000 fp32 rows 385; with
+        // the logits' own stride 209 and 199
         for (int i = lo + tid; i < hi; i += kTkThreads)
             store_scalar<DT>(grow, i, ok ? grad_term<DT>(E::scalar(zrow, i), line) / (far ? p.temperature : 1.0f) : 0.0f);
     } else {

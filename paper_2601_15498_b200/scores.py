@@ -216,8 +216,9 @@ def token_logprobs(logits: torch.Tensor, tok=None, temperature: float = 1.0, k: 
 def token_logprobs_backward(logits: torch.Tensor, tok, forward: dict, grad_logprob, grad_entropy=None,
                             temperature: float = 1.0, V: int | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """mars_token_logprobs_backward on the current stream: the gradient by `logits` (columns 0 .. V-1, dtype of
-    the logits; a new [rows, V] tensor, or `out`, which may be the logits).  `forward` is what token_logprobs
-    returned for these logits; grad_logprob has the shape of tok, grad_entropy [rows] or None."""
+    the logits; a new dense [rows, V] tensor, or `out`, which may be the logits).  `forward` is what token_logprobs
+    returned for these logits; grad_logprob has the shape of tok, grad_entropy [rows] or None.  Logits whose row stride
+    is no multiple of 16 bytes want an `out` of the same stride (a dense one takes two to four times as long)."""
     dt, R, ld, V, index = _logits(logits, V)
     tok, J = _tokens(tok, R, logits)
     g = _dev_f32(grad_logprob, logits.device)
@@ -258,7 +259,7 @@ class _Logprobs(torch.autograd.Function):
 
 def logprobs(logits: torch.Tensor, tok, temperature: float = 1.0):
     """(log probabilities of tok [rows, J] or [rows], entropies [rows]) of logits [rows, V], differentiable by
-    the logits (once)."""
+    the logits (once).  Rows are not picked by index here: gather those that a loss needs."""
     return _Logprobs.apply(logits, _dev_i32(tok, logits.device), float(temperature))
 
 
@@ -267,7 +268,7 @@ def emitted_logprobs(logits: torch.Tensor, verified: dict, temperature: float = 
     """token_logprobs of the tokens that a verification emitted, from its logits [B*N, ld] and its result:
     out_tokens[b, i] was judged by, or drawn from, the row of node path_nodes[b, i] (with `chain`, for the
     results of the chain calls, which have no path: of row i).  Results are [B, W] (and [B, W, k]) for
-    out_tokens [B, W]; places behind a sequence's out_len hold no token."""
+    out_tokens [B, W]; places behind a sequence's out_len hold no token.  Not differentiable (see logprobs)."""
     tok = verified["out_tokens"]
     B, W = tok.shape
     if logits.shape[0] % B:
